@@ -311,6 +311,116 @@ int tbs_last_hip_error(const tbs_ctx *ctx);
 int tbs_gemm_bf16(const void *A, const void *B, const float *bias, float *C, int32_t M, int32_t N,
                   int32_t K, int32_t kernel, void *stream);
 
+/* ---- operators of an autoregressive model beside the search ----
+ * One step of a transformer's beam decode (a language model or an attention decoder that continues or rescores
+ * hypotheses), without a context: products with their epilogue, attention of one new token per hypothesis over a paged cache, the
+ * selection over beams and vocabulary, and the states' reordering.  Every argument block is read before the call returns; all
+ * pointers in it are DEVICE and borrowed until the work enqueued on `stream` is done.  Kernels run on the current device, nothing is
+ * allocated or synchronised, and the calls may be captured into a graph.  Blocks are zeroed by the caller first: fields that are not named
+ * are 0.  Strides count elements.  Sums, softmax statistics and scores are held in float32 or more; each output is rounded once. */
+enum tbs_dtype { TBS_F32 = 0, TBS_BF16 = 1, TBS_F16 = 2 };
+enum tbs_act { TBS_ACT_NONE = 0, TBS_ACT_RELU = 1, TBS_ACT_TANH = 2, TBS_ACT_GELU = 3 /* 0.5 y (1 + erf(y / sqrt 2)) */,
+               TBS_ACT_SILU = 4 };
+
+/* out[i, j] = act(sum_k x[i, k] w[j, k] + bias[j]) + residual[i, j] for i < m, j < n.  x, w: dtype; bias float32 or NULL; residual
+ * (may be NULL) and out: out_dtype, which is dtype or TBS_F32.  out may be residual itself (same stride); other overlaps are not
+ * allowed.  m = 0 is no work.  Any sizes and strides; rows on 16-byte boundaries and k in whole 16-byte pieces are faster.
+ * The same call gives the same bits. */
+typedef struct tbs_linear_args {
+    const void *x;         /* [m, k], row stride ld_x */
+    const void *w;         /* [n, k], row stride ld_w */
+    const float *bias;     /* [n] */
+    const void *residual;  /* [m, n], row stride ld_residual */
+    void *out;             /* [m, n], row stride ld_out */
+    int64_t ld_x, ld_w, ld_residual, ld_out;
+    int32_t m, n, k;
+    int32_t dtype, out_dtype, act;
+} tbs_linear_args;
+int tbs_linear(const tbs_linear_args *args, void *stream);
+
+/* Attention of one new token per row over a paged cache.  Row r attends to n = lens[r] + 1 tokens (lens[r] of them in the cache, then
+ * the new one) or, without k_new and v_new, to the n = lens[r] in the cache; token t of the row is token t % page of page
+ * tables[r, t / page].  Query head h reads key head h / (heads / kv_heads).  For every query head
+ *     out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t - max),  and 0 where n = 0.
+ * The new token is written to its place in the cache as well: no other row's table may name that page (tbs_beam_reorder sees to it).
+ * lens[r] < 0: the row takes no part; its output is 0 and nothing is written for it.  A table entry outside [0, pages) is a page
+ * whose tokens do not exist: not attended to, not written (a new token is attended to all the same).  Tokens beyond table_width * page
+ * do not exist either.  What the cache holds behind a row's last token is not looked at.
+ * dim is a multiple of 8 up to 256, heads a multiple of kv_heads.  max_len: about how many tokens the longest row attends to (0: as
+ * many as its table holds); it decides how the work is split, never the result's correctness.  beams: rows beams * i .. beams * i +
+ * beams - 1 are hypotheses of one utterance, whose tables may name the same pages (1: rows share nothing); rows is a multiple of it.  It
+ * is a hint too: pages that several rows of a group have in common are then read once.
+ * workspace: tbs_attend_workspace(args) bytes on a 16-byte boundary (0: none), free again when the work is done. */
+typedef struct tbs_attend_args {
+    const void *q;               /* [rows, heads, dim]; elements of a head side by side everywhere */
+    const void *k_new, *v_new;   /* [rows, kv_heads, dim], or both NULL */
+    void *k_cache, *v_cache;     /* [pages, page, kv_heads, dim] */
+    const int32_t *tables;       /* [rows, table_width], row stride ld_tables */
+    const int32_t *lens;         /* [rows] */
+    void *out;                   /* [rows, heads, dim] */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t q_row, q_head, k_new_row, k_new_head, v_new_row, v_new_head, out_row, out_head;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    int64_t ld_tables;
+    int32_t rows, heads, kv_heads, dim, page, pages, table_width, max_len, beams, dtype;
+    float scale;                 /* 0: 1 / sqrt(dim) */
+} tbs_attend_args;
+int tbs_attend_paged(const tbs_attend_args *args, void *stream);
+/* Bytes of workspace that tbs_attend_paged wants for these sizes (pointers and strides are not looked at); negative: an error code. */
+int64_t tbs_attend_workspace(const tbs_attend_args *args);
+
+/* The `beams` best continuations of every group of `beams` hypotheses (rows beams * i .. of the batch) over a vocabulary without a blank:
+ * candidate (row r, token v) has the score scores[r] + logits[r, v] - log sum_v' exp logits[r, v'] (float64 from the logits on).
+ * A finished row (finished[r] != 0) has one candidate, itself: its score, the token eos; its logits are not looked at.  A row's candidates
+ * rank by logit, then token; rows against each other by score, then row.  A score that is NaN or -inf is no candidate: so is
+ * every token of a row with a logit that is NaN or +inf or with none above -inf, and every row whose score is -inf (the rows that do not
+ * exist yet at the first step).  Where a group has fewer than `beams` candidates its last places are: score -inf, token -1, parent
+ * -1, finished.  A place is also finished where its token is eos or its parent was.  parents are places in the group, 0 .. beams - 1.
+ * workspace: tbs_beam_select_workspace(args) bytes on a 16-byte boundary.  The same call gives the same bits. */
+#define TBS_MAX_VOCAB 524288
+typedef struct tbs_beam_select_args {
+    const void *logits;       /* [rows, vocab] in dtype, row stride ld_logits */
+    const double *scores;     /* [rows] */
+    const uint8_t *finished;  /* [rows] or NULL: none is */
+    double *out_scores;       /* [rows], every group best first */
+    int32_t *out_tokens, *out_parents;
+    uint8_t *out_finished;
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t ld_logits;
+    int32_t rows, beams, vocab, eos, dtype;   /* beams 1..TBS_MAX_BEAM, vocab 1..TBS_MAX_VOCAB; eos: any number, -1 for none */
+} tbs_beam_select_args;
+int tbs_beam_select(const tbs_beam_select_args *args, void *stream);
+int64_t tbs_beam_select_workspace(const tbs_beam_select_args *args);
+
+/* The states of tbs_beam_select's hypotheses: page tables and lengths follow the parents, in every cache that the tables index.
+ * Row r had lens[r] tokens before this step and has `appended` more now (lens[r] < 0: it took no part, ~lens[r] tokens).  Its first
+ * tokens / page pages are whole and never written again, so that hypotheses may share them; its table's entries from there on are its own.
+ * Place c with parent p: the first child of p keeps p's table; every other one has p's whole pages, then the own pages
+ * of a row without children (in order: the k-th such place those of the k-th such row), and the tokens of p's page that is not full are
+ * copied to the first of them.  So nothing is allocated or freed: a group starts with tables whose rows share nothing (or whole pages
+ * at their heads only) and holds the tokens of every hypothesis for good.  What that needs: a row with several children is as long, in
+ * whole pages, as any row of its group without children (all hypotheses of a group that still grow are equally long).  A place
+ * that this does not hold for is dropped (length -1) and counted in *status.
+ * Parents outside 0 .. beams - 1 are places without a hypothesis: length -1 and some row's table.  Otherwise the new length is that of the
+ * parent with its appended tokens; with finished[c] its complement ~length: it takes no part in the steps to come. */
+#define TBS_MAX_CACHES 128
+typedef struct tbs_beam_reorder_args {
+    const int32_t *parents;    /* [rows] places in the group */
+    const int32_t *tables;     /* [rows, table_width], row stride ld_tables */
+    const int32_t *lens;       /* [rows] */
+    const uint8_t *finished;   /* [rows], of the new hypotheses, or NULL: none is */
+    int32_t *out_tables;       /* [rows, table_width], row stride ld_out_tables; not the tables that are read */
+    int32_t *out_lens;         /* [rows], not the lengths that are read */
+    int32_t *status;           /* one number that dropped places are added to, or NULL */
+    void *const *caches;       /* HOST array of n_caches DEVICE pointers, each a cache [pages, page, kv_heads, dim] of these strides */
+    int64_t cache_page, cache_token, cache_head;
+    int64_t ld_tables, ld_out_tables;
+    int32_t n_caches, rows, beams, table_width, pages, page, kv_heads, dim, dtype, appended;   /* n_caches up to TBS_MAX_CACHES */
+} tbs_beam_reorder_args;
+int tbs_beam_reorder(const tbs_beam_reorder_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

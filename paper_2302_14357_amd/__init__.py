@@ -16,3 +16,4 @@ from .tbs import (  # noqa: F401
     KERNEL,
     EXPORTED_SYMBOLS,
 )
+from .ops import attend_paged, beam_reorder, beam_select, linear  # noqa: F401

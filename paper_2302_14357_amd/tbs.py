@@ -16,6 +16,7 @@ EXPORTED_SYMBOLS = [
     "tbs_debug_write", "tbs_debug_rebuild", "tbs_debug_hyps", "tbs_profile_select", "tbs_profile_read",
     "tbs_strerror", "tbs_last_hip_error", "tbs_gemm_bf16", "tbs_stream_begin", "tbs_push_segment",
     "tbs_profile_overhead", "tbs_debug_hyps_noalloc", "tbs_path", "tbs_one_launch",
+    "tbs_linear", "tbs_attend_paged", "tbs_attend_workspace", "tbs_beam_select", "tbs_beam_select_workspace", "tbs_beam_reorder",
 ]
 
 TBS_MAX_LAYERS = 4
@@ -96,6 +97,11 @@ def load_library():
     L.tbs_strerror.restype = C.c_char_p
     L.tbs_last_hip_error.argtypes = [vp]
     L.tbs_gemm_bf16.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    for name in ("tbs_linear", "tbs_attend_paged", "tbs_beam_select", "tbs_beam_reorder"):
+        getattr(L, name).argtypes = [vp, vp]
+    for name in ("tbs_attend_workspace", "tbs_beam_select_workspace"):
+        getattr(L, name).argtypes = [vp]
+        getattr(L, name).restype = C.c_int64
     _lib = L
     return L
 
