@@ -7,7 +7,7 @@ import pytest
 
 def _ops():
     from paper_2302_14357_amd import ops
-    return ops._library(), ops
+    return ops.load_library(), ops
 
 
 P = 1 << 20   # an aligned address that nothing may look at
