@@ -98,6 +98,43 @@ def test_linear_strides_and_alignment(m, n, k, pad, shift, dtype):
     _linear_case(m, n, k, dtype, "relu", True, True, pad=pad, shift=shift)
 
 
+def _linear_by(kernel, x, w, b, act, r, out):
+    import ctypes
+    from paper_2302_14357_amd import ops
+    L = ops.load_library()
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    a = ops._Linear(x=x.data_ptr(), w=w.data_ptr(), bias=b.data_ptr(), residual=r.data_ptr(), out=out.data_ptr(), ld_x=x.stride(0), ld_w=w.stride(0),
+                    ld_residual=r.stride(0), ld_out=out.stride(0), m=x.shape[0], n=w.shape[0], k=x.shape[1], dtype=code[x.dtype], out_dtype=code[out.dtype], act=ops._ACTS[act])
+    return L.linear_by(ctypes.byref(a), ctypes.c_int(kernel), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kernel", [1, 11, 12, 21, 22, 42, 121, 142, 164, 184])
+def test_linear_every_kernel(kernel, dtype):
+    """One, two, several and more K tiles than a kernel has stages, pieces behind K, one past and one short of whole tiles, one row, and the float32 result."""
+    for m, n, k in [(1, 4, 8), (63, 66, 64), (65, 257, 72), (129, 250, 128), (193, 520, 200), (257, 254, 328), (300, 300, 1032), (30, 515, 640)]:
+        for act, odt in (("gelu", dtype), ("none", torch.float32)):
+            g = _gen(m + n + k)
+            x, w, b, r = _randn(g, m, k, dtype=dtype), _randn(g, n, k, dtype=dtype, scale=1 / math.sqrt(k)), _randn(g, n), _randn(g, m, n, dtype=odt)
+            room = torch.full((m + 1, n), 77.0, dtype=odt, device="cuda")
+            assert _linear_by(kernel, x.cuda(), w.cuda(), b.cuda(), act, r.cuda(), room[:m]) == 0
+            torch.cuda.synchronize()
+            assert bool((room[m:] == 77.0).all())
+            y = x.double() @ w.double().t() + b.double()
+            loss = 1.13 * (k + 1) * 2.0**-24 * (x.double().abs() @ w.double().abs().t() + b.double().abs()) + 4e-7 * (1 + y.abs())
+            y = ACTS[act](y) + r.double()
+            _close(room[:m], y, loss + 2.0**-24 * y.abs() + _half_step(y, odt) * (1 + 2.0**-10))
+
+
+@pytest.mark.parametrize("kernel", [121, 142, 164, 184])
+def test_linear_tiles_want_alignment(kernel):
+    x, w, b = torch.zeros(70, 72, dtype=torch.bfloat16, device="cuda"), torch.zeros(80, 72, dtype=torch.bfloat16, device="cuda"), torch.zeros(80, device="cuda")
+    out = torch.zeros(70, 80, dtype=torch.bfloat16, device="cuda")
+    assert _linear_by(kernel, x[:, :71], w[:, :71], b, "none", out, out) == -1
+    assert _linear_by(kernel, x[:, 1:65], w[:, 1:65], b, "none", out, out) == -1
+    assert _linear_by(99, x, w, b, "none", out, out) == -1
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_in_place_residual_leading_dimensions_and_no_rows(dtype):
     from paper_2302_14357_amd import linear
