@@ -13,8 +13,12 @@
 // A lane keeps maximum, sum and output of one query: nothing but the maximum crosses lanes.
 #include "op_device.h"
 
+//
+// Hypotheses of one utterance (beams) name the same pages for most of their length.  A workgroup then takes a key head and a piece of the
+// length for all of them: the pages at the piece's head that their tables have in common are read once, with all hypotheses' queries as
+// columns, and behind those each hypothesis' own tokens, which count for its columns alone.
 #define ATT_WAVES 4
-#define ATT_TABLE 1024   // page table entries in LDS at a time
+#define ATT_TABLE 1024   // page table entries in LDS at a time, of all hypotheses of a workgroup
 
 struct AttendP {
     const char *q, *k_new, *v_new;
@@ -23,7 +27,7 @@ struct AttendP {
     char *out;
     float *part_o, *part_ml;   // [rows, heads, splits, dim], [rows, heads, splits, 2]; only with more than one split
     int64_t q_row, q_head, kn_row, kn_head, vn_row, vn_head, o_row, o_head, kp, kt, kh, vp, vt, vh, ld_tables;   // bytes (ld_tables: elements)
-    int rows, heads, kv_heads, group, dim, page, pages, width, splits, split_len, qblocks;
+    int rows, heads, kv_heads, group, dim, page, pages, width, splits, split_len, qblocks, beams;
     unsigned page_mul, page_shift;
     float scale2;   // scale * log2(e)
 };
@@ -62,73 +66,143 @@ struct AttTile {
     unsigned ok;   // bit j: V's token j exists
 };
 
-// DP: dim rounded up to 32, 64, 128 or 256 (PAD: it was not that already)
-template <class T, int DP, bool PAD>
+// DP: dim rounded up to 32, 64, 128 or 256 (PAD: it was not that already); QB: blocks of sixteen queries a wave takes together
+template <class T, int DP, int QB, bool PAD>
 __global__ void __launch_bounds__(64 * ATT_WAVES, 2)
 k_attend(AttendP p) {
     typedef AttTile<T, DP> Tile;
     constexpr int E = OpPiece<T>::E, NB = Tile::NB, TK = Tile::TK, NV = Tile::NV, KS = Tile::KS, W = Tile::W, WW = Tile::WW;
-    __shared__ int s_table[ATT_TABLE + 1];
+    constexpr bool LATE = DP > 128;   // (registers for keys and values at the same time are missing: values are asked for when the scores are made)
+    __shared__ int s_table[ATT_TABLE + TBS_MAX_BEAM];
     __shared__ float s_o[ATT_WAVES / 2][W * 4][64];
-    __shared__ float s_ml[ATT_WAVES][2][16];
+    __shared__ float s_ml[ATT_WAVES][2][QB * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, kg = lane >> 4;
-    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = blockIdx.y, row = blockIdx.z;
-    int pos;
-    const int n = att_tokens(p, row, &pos);
+    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = blockIdx.y, N = p.beams, r0 = (int)blockIdx.z * N;
+    // hypothesis `lane` of the group: its tokens, and those of them that are in the cache
+    int n_l = 0, pos_l = -1;
+    if (lane < N) n_l = att_tokens(p, r0 + lane, &pos_l);
+    int n = n_l, cached = lane < N && n_l > 0 ? (pos_l >= 0 ? pos_l : n_l) : INT32_MAX;
+#pragma unroll
+    for (int i = 1; i < 32; i <<= 1) {
+        n = max(n, __shfl_xor(n, i));
+        cached = min(cached, __shfl_xor(cached, i));
+    }
+    n = __builtin_amdgcn_readfirstlane(n);   // of the longest
+    cached = __builtin_amdgcn_readfirstlane(cached);   // of the shortest that takes part
+    const unsigned live = (unsigned)__ballot(n_l > 0);
     const int k0 = split * p.split_len;
-    if (k0 >= n && split > 0) return;   // (of a row without tokens the first workgroup writes the zeros)
-    const int k1 = split == p.splits - 1 ? n : min(n, k0 + p.split_len);   // (the last goes on to the row's end, whatever max_len said)
-    const int qh = qblk * 16 + c;       // query head within the group
-    const bool has_q = qh < p.group;
-    const int head = kvh * p.group + min(qh, p.group - 1);
+    if (k0 >= n && split > 0) return;   // (of a group without tokens the first workgroup writes the zeros)
+    const int k1 = split == p.splits - 1 ? n : min(n, k0 + p.split_len);   // (the last goes on to the end, whatever max_len said)
     const char *kb = p.k_cache + kvh * p.kh, *vb = p.v_cache + kvh * p.vh;
-    const char *kn = p.k_new ? p.k_new + row * p.kn_row + kvh * p.kn_head : nullptr, *vn = kn ? p.v_new + row * p.vn_row + kvh * p.vn_head : nullptr;
     const bool quad = (p.page & 3) == 0;   // four tokens from a multiple of four on lie in one page
 
-    uint4 q[KS];
-    {
-        const T *src = (const T *)(p.q + row * p.q_row + head * p.q_head);
+    int col_row[QB], col_head[QB];   // whose query a lane's column is
+    bool col_live[QB];
+    uint4 q[QB][KS];
+    floatx4 o[QB][W];
+    float m[QB], l[QB];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = has_q && (!PAD || (s * 4 + kg) * E < p.dim) ? op_load16(src + (s * 4 + kg) * E) : make_uint4(0, 0, 0, 0);
+    for (int b = 0; b < QB; ++b) {
+        const int col = (qblk * QB + b) * 16 + c;
+        col_row[b] = col / p.group;
+        col_head[b] = kvh * p.group + col - col_row[b] * p.group;
+        const bool there = col_row[b] < N;
+        col_live[b] = there && (live >> col_row[b] & 1);
+        const T *src = (const T *)(p.q + (r0 + min(col_row[b], N - 1)) * p.q_row + col_head[b] * p.q_head);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[b][s] = there && (!PAD || (s * 4 + kg) * E < p.dim) ? op_load16(src + (s * 4 + kg) * E) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < W; ++i) o[b][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        m[b] = -INFINITY;
+        l[b] = 0.f;
     }
-    floatx4 o[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
 
-    for (int c0 = k0; c0 < k1; c0 += ATT_TABLE * p.page) {
-        const int first = att_page(p, c0), c1 = min((int64_t)k1, (int64_t)c0 + (int64_t)ATT_TABLE * p.page);
+    const int per_row = ATT_TABLE / N, chunk = per_row * p.page;   // table entries of a hypothesis at a time, their tokens
+    for (int c0 = k0; c0 < k1; c0 += chunk) {
+        const int first = att_page(p, c0), c1 = min(k1, c0 + chunk), pages = att_page(p, c1 - 1) - first + 1;
         if (c0 > k0) __syncthreads();
-        for (int i = threadIdx.x; i <= att_page(p, c1 - 1) - first; i += 64 * ATT_WAVES) s_table[i] = p.tables[row * p.ld_tables + first + i];
+        for (int b = wave; b < N; b += ATT_WAVES) {
+            const int mine = __shfl(n_l, b), have = mine > 0 ? min(pages, att_page(p, mine - 1) - first + 1) : 0;
+            for (int i = lane; i < pages; i += 64) s_table[b * (per_row + 1) + i] = i < have ? p.tables[(r0 + b) * p.ld_tables + first + i] : -1;
+        }
         __syncthreads();
+        // tokens up to `common` are everybody's: pages of the same numbers, whole, in the cache of all
+        int common = c0;
+        const int lead = __ffs(live) - 1;
+        if (N > 1) {
+            int same = 0;
+            for (int i0 = 0; i0 < pages; i0 += 64) {
+                const int i = i0 + lane;
+                bool differ = i >= pages;
+                for (unsigned rest = live & (live - 1); rest; rest &= rest - 1)
+                    differ |= i < pages && s_table[lead * (per_row + 1) + i] != s_table[(__ffs(rest) - 1) * (per_row + 1) + i];
+                const unsigned long long d = __ballot(differ);
+                same += d ? __ffsll((long long)d) - 1 : 64;
+                if (d) break;
+            }
+            common = max(c0, min((int)min((int64_t)c1, (int64_t)(first + same) * p.page), att_page(p, min(cached, c1)) * p.page));
+        }
+        // tiles: those of the common tokens, then each hypothesis' own
+        const int shared = (common - c0 + TK - 1) / TK, end_l = min(n_l, c1), own = end_l > common ? (end_l - common + TK - 1) / TK : 0;
+        int start = own;
+#pragma unroll
+        for (int i = 1; i < 32; i <<= 1) {
+            const int x = __shfl_up(start, i);
+            if (lane >= i) start += x;
+        }
+        const int tiles = shared + __builtin_amdgcn_readfirstlane(__shfl(start, 31));
+        start += shared - own;
         // a token's page in the pool (negative: it does not exist) and its place there
-        auto page_of = [&](int t, int &off) {
-            const int i = att_page(p, t), id = s_table[i - first];
+        auto page_of = [&](int t, int at, int &off) {
+            const int i = att_page(p, t), id = s_table[at + i - first];
             off = t - i * p.page;
             return (unsigned)id < (unsigned)p.pages ? id : -1;
         };
-        auto load = [&](Tile &x, int t0) {
+        struct Where {
+            int t0, end, row, at, pos;   // row: whose it is (-1: everybody's); at: its table in LDS
+            const char *kn, *vn;
+        };
+        auto place = [&](int tile) {
+            Where w;
+            int b = lead;
+            if (tile < shared) {
+                w.row = -1, w.pos = -1, w.t0 = c0 + tile * TK, w.end = common;
+            } else {
+                b = 31 - __clz((unsigned)__ballot(lane < N && own > 0 && start <= tile));
+                w.row = b;
+                w.pos = __builtin_amdgcn_readlane(pos_l, b);
+                w.t0 = common + (tile - __builtin_amdgcn_readlane(start, b)) * TK;
+                w.end = __builtin_amdgcn_readlane(end_l, b);
+            }
+            w.at = b * (per_row + 1);
+            w.kn = p.k_new + (r0 + b) * p.kn_row + kvh * p.kn_head;
+            w.vn = p.v_new + (r0 + b) * p.vn_row + kvh * p.vn_head;
+            return w;
+        };
+        auto load_k = [&](Tile &x, const Where &w) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const int t = min(t0 + b * 16 + c, c1 - 1);
+                const int t = min(w.t0 + b * 16 + c, w.end - 1);
                 int off;
-                const int id = page_of(t, off);
-                const char *at = t == pos ? kn : id < 0 ? kb : kb + id * p.kp + off * p.kt;
+                const int id = page_of(t, w.at, off);
+                const char *at = t == w.pos ? w.kn : id < 0 ? kb : kb + id * p.kp + off * p.kt;
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
                     x.k[b][s] = !PAD || (s * 4 + kg) * E < p.dim ? op_load16((const T *)at + (s * 4 + kg) * E) : make_uint4(0, 0, 0, 0);
             }
+        };
+        auto load_v = [&](Tile &x, const Where &w) {
             x.ok = 0;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 int off = 0, id = 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int want = t0 + b * 16 + kg * 4 + r, t = min(want, c1 - 1);
-                    if (r == 0 || !quad) id = page_of(t, off);
-                    const char *at = t == pos ? vn : id < 0 ? vb : vb + id * p.vp + (quad ? off + (t - min(want - r, c1 - 1)) : off) * p.vt;
-                    if (want < c1 && (id >= 0 || t == pos)) x.ok |= 1u << (b * 4 + r);
+                    const int want = w.t0 + b * 16 + kg * 4 + r, t = min(want, w.end - 1);
+                    if (r == 0 || !quad) id = page_of(t, w.at, off);
+                    const char *at = t == w.pos ? w.vn : id < 0 ? vb : vb + id * p.vp + (quad ? off + (t - min(want - r, w.end - 1)) : off) * p.vt;
+                    if (want < w.end && (id >= 0 || t == w.pos)) x.ok |= 1u << (b * 4 + r);
                     unsigned *v = x.v[b * 4 + r];
                     constexpr int G = W < 8 ? W : 8;   // elements that are there together or not at all: dim is a multiple of 8
 #pragma unroll
@@ -142,7 +216,17 @@ k_attend(AttendP p) {
                 }
             }
         };
-        auto compute = [&](Tile &x) {
+        auto compute = [&](Tile &x, const Where &w) {
+            floatx4 s[QB][NB];
+#pragma unroll
+            for (int b = 0; b < QB; ++b)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    s[b][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < KS; ++j) s[b][i] = op_mma<T>(x.k[i][j], q[b][j], s[b][i]);
+                }
+            if (LATE) load_v(x, w);
             const bool whole = __all(x.ok == (1u << NV) - 1);
             if (!whole) {   // what stands in places without a token may be anything
 #pragma unroll
@@ -150,104 +234,112 @@ k_attend(AttendP p) {
 #pragma unroll
                     for (int i = 0; i < WW; ++i) x.v[j][i] = x.ok >> j & 1 ? x.v[j][i] : 0;
             }
-            float t[NV];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                floatx4 s = {0.f, 0.f, 0.f, 0.f};
+            for (int b = 0; b < QB; ++b) {
+                // (a hypothesis' own tokens: blocks without a query of its own have nothing to do)
+                if (QB > 1 && w.row >= 0 && ((w.row + 1) * p.group <= (qblk * QB + b) * 16 || w.row * p.group >= (qblk * QB + b + 1) * 16)) continue;
+                const bool mine = w.row < 0 ? col_live[b] : col_row[b] == w.row;
+                float t[NV];
 #pragma unroll
-                for (int i = 0; i < KS; ++i) s = op_mma<T>(x.k[b][i], q[i], s);
+                for (int j = 0; j < NV; ++j) t[j] = mine && (whole || (x.ok >> j & 1)) ? s[b][j / 4][j % 4] * p.scale2 : -INFINITY;
+                float top = t[0];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) t[b * 4 + r] = whole || (x.ok >> (b * 4 + r) & 1) ? s[r] * p.scale2 : -INFINITY;
-            }
-            float top = t[0];
+                for (int j = 1; j < NV; ++j) top = fmaxf(top, t[j]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (__any(top > m[b])) {
+                    const float m1 = fmaxf(m[b], top), a = m1 == m[b] ? 1.f : __builtin_amdgcn_exp2f(m[b] - m1);
+                    m[b] = m1;
+                    l[b] *= a;
 #pragma unroll
-            for (int j = 1; j < NV; ++j) top = fmaxf(top, t[j]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any(top > m)) {
-                const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-                m = m1;
-                l *= a;
-#pragma unroll
-                for (int i = 0; i < W; ++i) o[i] *= a;
-            }
-            // (fp16: weights up to 2^12 instead of 1, so that small ones keep their digits)
-            const float base = m == -INFINITY ? 0.f : m - (__is_same(T, _Float16) ? 12.f : 0.f);
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                t[j] = __builtin_amdgcn_exp2f(t[j] - base);
-                l += t[j];
-            }
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int i = 0; i < W; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][i]), t[r], o[i], 0, 0, 0);
-            } else {
-                // A weight goes into the matrix instruction as two numbers of 16 bits, its rounding and what that left out: a weight's error
-                // is then 2^-17 (fp16: 2^-22) instead of 2^-9, and the output's own rounding is all that shows.  (The second half of the
-                // products costs no time: memory bounds the kernel.)
-                T hi[8], lo[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    hi[j] = (T)t[j];
-                    lo[j] = (T)(t[j] - (float)hi[j]);
+                    for (int i = 0; i < W; ++i) o[b][i] *= a;
                 }
-                uint4 ph, pl;
-                __builtin_memcpy(&ph, hi, 16);
-                __builtin_memcpy(&pl, lo, 16);
+                // (fp16: weights up to 2^12 instead of 1, so that small ones keep their digits)
+                const float base = m[b] == -INFINITY ? 0.f : m[b] - (__is_same(T, _Float16) ? 12.f : 0.f);
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const unsigned sel = i & 1 ? 0x07060302u : 0x05040100u;
-                    const uint4 a = make_uint4(__builtin_amdgcn_perm(x.v[1][i / 2], x.v[0][i / 2], sel), __builtin_amdgcn_perm(x.v[3][i / 2], x.v[2][i / 2], sel),
-                                               __builtin_amdgcn_perm(x.v[5][i / 2], x.v[4][i / 2], sel), __builtin_amdgcn_perm(x.v[7][i / 2], x.v[6][i / 2], sel));
-                    o[i] = op_mma<T>(a, ph, o[i]);
-                    o[i] = op_mma<T>(a, pl, o[i]);
+                for (int j = 0; j < NV; ++j) {
+                    t[j] = __builtin_amdgcn_exp2f(t[j] - base);
+                    l[b] += t[j];
+                }
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int i = 0; i < W; ++i) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][i]), t[r], o[b][i], 0, 0, 0);
+                } else {
+                    // A weight goes into the matrix instruction as two numbers of 16 bits, its rounding and what that left out: a weight's
+                    // error is then 2^-17 (fp16: 2^-22) instead of 2^-9, and the output's own rounding is all that shows.  (The second half
+                    // of the products costs no time: memory bounds the kernel.)
+                    T hi[8], lo[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        hi[j] = (T)t[j];
+                        lo[j] = (T)(t[j] - (float)hi[j]);
+                    }
+                    uint4 ph, pl;
+                    __builtin_memcpy(&ph, hi, 16);
+                    __builtin_memcpy(&pl, lo, 16);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const unsigned sel = i & 1 ? 0x07060302u : 0x05040100u;
+                        const uint4 a = make_uint4(__builtin_amdgcn_perm(x.v[1][i / 2], x.v[0][i / 2], sel), __builtin_amdgcn_perm(x.v[3][i / 2], x.v[2][i / 2], sel),
+                                                   __builtin_amdgcn_perm(x.v[5][i / 2], x.v[4][i / 2], sel), __builtin_amdgcn_perm(x.v[7][i / 2], x.v[6][i / 2], sel));
+                        o[b][i] = op_mma<T>(a, ph, o[b][i]);
+                        o[b][i] = op_mma<T>(a, pl, o[b][i]);
+                    }
                 }
             }
         };
-        for (int t0 = c0 + wave * TK; t0 < c1; t0 += ATT_WAVES * TK) {
+        for (int tile = wave; tile < tiles; tile += ATT_WAVES) {
+            const Where w = place(tile);
             Tile x;
-            load(x, t0);
-            compute(x);
+            load_k(x, w);
+            if (!LATE) load_v(x, w);
+            compute(x, w);
         }
     }
     // the waves' shares: 3 and 2 to 1 and 0, 1 to 0; every lane has the same place in all of them
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (lane < 16) {
-        s_ml[wave][0][c] = m;
-        s_ml[wave][1][c] = l;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+        if (lane < 16) {
+            s_ml[wave][0][b * 16 + c] = m[b];
+            s_ml[wave][1][b * 16 + c] = l[b];
+        }
     }
     __syncthreads();
-    float top = m;
 #pragma unroll
-    for (int i = 0; i < ATT_WAVES; ++i) top = fmaxf(top, s_ml[i][0][c]);
-    auto share = [&](float x) { return x == top ? 1.f : __builtin_amdgcn_exp2f(x - top); };   // (-inf of -inf: nothing there, 1 x 0)
-    const float a = share(m);
-    l = 0.f;
+    for (int b = 0; b < QB; ++b) {
+        float top = m[b];
 #pragma unroll
-    for (int i = 0; i < ATT_WAVES; ++i) l += s_ml[i][1][c] * share(s_ml[i][0][c]);
+        for (int i = 0; i < ATT_WAVES; ++i) top = fmaxf(top, s_ml[i][0][b * 16 + c]);
+        auto share = [&](float x) { return x == top ? 1.f : __builtin_amdgcn_exp2f(x - top); };   // (-inf of -inf: nothing there, 1 x 0)
+        const float a = share(m[b]);
+        float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < W; ++i) o[i] *= a;
+        for (int i = 0; i < ATT_WAVES; ++i) sum += s_ml[i][1][b * 16 + c] * share(s_ml[i][0][b * 16 + c]);
 #pragma unroll
-    for (int h = ATT_WAVES / 2; h > 0; h >>= 1) {
-        if (wave >= h && wave < 2 * h)
+        for (int i = 0; i < W; ++i) o[b][i] *= a;
 #pragma unroll
-            for (int i = 0; i < W; ++i)
+        for (int h = ATT_WAVES / 2; h > 0; h >>= 1) {
+            if (wave >= h && wave < 2 * h)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s_o[wave - h][i * 4 + r][lane] = o[i][r];
-        __syncthreads();
-        if (wave < h)
+                for (int i = 0; i < W; ++i)
 #pragma unroll
-            for (int i = 0; i < W; ++i)
+                    for (int r = 0; r < 4; ++r) s_o[wave - h][i * 4 + r][lane] = o[b][i][r];
+            __syncthreads();
+            if (wave < h)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[i][r] += s_o[wave][i * 4 + r][lane];
-        __syncthreads();
-    }
-    if (wave == 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;   // (no weight at all: 0)
-        if (has_q) {
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[b][i][r] += s_o[wave][i * 4 + r][lane];
+            __syncthreads();
+        }
+        if (wave == 0 && col_row[b] < N) {
+            const int64_t row = r0 + col_row[b];
+            const int head = col_head[b];
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int d = (kg * 4 + r) * W;
@@ -256,81 +348,110 @@ k_attend(AttendP p) {
                 for (int g = 0; g < W / G; ++g) {
                     if (PAD && d + g * G >= p.dim) continue;
                     if (p.splits > 1) {
-                        float *dst = p.part_o + (((int64_t)row * p.heads + head) * p.splits + split) * p.dim + d + g * G;
+                        float *dst = p.part_o + ((row * p.heads + head) * p.splits + split) * p.dim + d + g * G;
+                        float y[G];
 #pragma unroll
-                        for (int i = 0; i < G; ++i) dst[i] = o[g * G + i][r];
+                        for (int i = 0; i < G; ++i) y[i] = o[b][g * G + i][r];
+                        __builtin_memcpy(dst, y, sizeof y);
                     } else {
                         T y[G];
 #pragma unroll
-                        for (int i = 0; i < G; ++i) y[i] = (T)(l == 0.f ? 0.f : o[g * G + i][r] * inv);
+                        for (int i = 0; i < G; ++i) y[i] = (T)(sum == 0.f ? 0.f : o[b][g * G + i][r] * inv);
                         __builtin_memcpy((T *)(p.out + row * p.o_row + head * p.o_head) + d + g * G, y, sizeof y);
                     }
                 }
             }
             if (p.splits > 1 && kg == 0) {
-                float *ml = p.part_ml + (((int64_t)row * p.heads + head) * p.splits + split) * 2;
+                float *ml = p.part_ml + ((row * p.heads + head) * p.splits + split) * 2;
                 ml[0] = top;
-                ml[1] = l;
+                ml[1] = sum;
             }
         }
-    } else if (wave == 1 && qblk == 0 && pos >= k0 && pos < k1) {
-        // the new token's place in the cache (this launch reads the token from k_new and v_new, whoever attends to it)
-        const int i = att_page(p, pos), id = p.tables[row * p.ld_tables + i], off = pos - i * p.page;
-        if ((unsigned)id < (unsigned)p.pages)
-            for (int d = lane; d < p.dim; d += 64) {
-                ((T *)(p.k_cache + id * p.kp + off * p.kt + kvh * p.kh))[d] = ((const T *)kn)[d];
-                ((T *)(p.v_cache + id * p.vp + off * p.vt + kvh * p.vh))[d] = ((const T *)vn)[d];
-            }
     }
+    if (qblk == 0)   // the new tokens' places in the cache (this launch reads them from k_new and v_new, whoever attends to them)
+        for (int b = wave; b < N; b += ATT_WAVES) {
+            const int pos = __shfl(pos_l, b);
+            if (pos < k0 || pos >= k1) continue;
+            const int i = att_page(p, pos), id = p.tables[(r0 + b) * p.ld_tables + i], off = pos - i * p.page;
+            if ((unsigned)id >= (unsigned)p.pages) continue;
+            const T *kn = (const T *)(p.k_new + (r0 + b) * p.kn_row + kvh * p.kn_head), *vn = (const T *)(p.v_new + (r0 + b) * p.vn_row + kvh * p.vn_head);
+            for (int d = lane; d < p.dim; d += 64) {
+                ((T *)(p.k_cache + id * p.kp + off * p.kt + kvh * p.kh))[d] = kn[d];
+                ((T *)(p.v_cache + id * p.vp + off * p.vt + kvh * p.vh))[d] = vn[d];
+            }
+        }
 }
 
-// The splits' shares of one row and head: a workgroup of four waves, a share of the splits each.
+// The splits' shares of one row and head.  Four dimensions a thread: dim / 4 threads (rounded up to 2^x) to a split, the workgroup's
+// threads over as many splits as fit, four of each asked for at a time.
 template <class T>
 __global__ void __launch_bounds__(256)
-k_attend_join(AttendP p) {
-    __shared__ float s_o[4][256], s_l[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.y, head = blockIdx.x;
+k_attend_join(AttendP p, int threads) {
+    __shared__ float s_o[256][4], s_l[256];
+    const int lane = threadIdx.x & 63, row = blockIdx.y, head = blockIdx.x, d = (int)threadIdx.x % threads * 4, from = (int)threadIdx.x / threads, step = 256 / threads;
     int pos;
     const int n = att_tokens(p, row, &pos), used = n == 0 ? 1 : min(p.splits, (int)(((int64_t)n + p.split_len - 1) / p.split_len));
     const float *ml = p.part_ml + ((int64_t)row * p.heads + head) * p.splits * 2;
-    const float *po = p.part_o + ((int64_t)row * p.heads + head) * p.splits * p.dim;
+    const float *po = p.part_o + ((int64_t)row * p.heads + head) * p.splits * p.dim + min(d, p.dim - 4);
     float top = -INFINITY;
     for (int s = lane; s < used; s += 64) top = fmaxf(top, ml[2 * s]);
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
     float o[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-    for (int s = wave; s < used; s += 4) {
-        const float m = ml[2 * s], a = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-        l += a * ml[2 * s + 1];
+    for (int s0 = from; s0 < used; s0 += 4 * step) {
+        float x[4][4], w[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i * 64 + lane < p.dim) o[i] += a * po[(int64_t)s * p.dim + i * 64 + lane];
+        for (int i = 0; i < 4; ++i) {
+            const int s = min(s0 + i * step, used - 1);
+            w[i] = ml[2 * s];
+            y[i] = ml[2 * s + 1];
+            __builtin_memcpy(x[i], po + (int64_t)s * p.dim, 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (s0 + i * step >= used) continue;
+            const float a = w[i] == top ? 1.f : __builtin_amdgcn_exp2f(w[i] - top);
+            l += a * y[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] += a * x[i][j];
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_o[wave][i * 64 + lane] = o[i];
-    if (lane == 0) s_l[wave] = l;
+    for (int j = 0; j < 4; ++j) s_o[threadIdx.x][j] = o[j];
+    s_l[threadIdx.x] = l;
     __syncthreads();
-    const int d = threadIdx.x;
-    l = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-    if (d < p.dim)
-        ((T *)(p.out + row * p.o_row + head * p.o_head))[d] = (T)(l == 0.f ? 0.f : (s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d]) / l);
+    if (from > 0 || d >= p.dim) return;
+    for (int i = 1; i < step; ++i) {
+        l += s_l[i * threads];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += s_o[i * threads + threadIdx.x][j];
+    }
+    T y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = (T)(l == 0.f ? 0.f : o[j] / l);
+    __builtin_memcpy((T *)(p.out + row * p.o_row + head * p.o_head) + d, y, sizeof y);
 }
 
-// How the work is split: workgroups of a row and key head (and sixteen query heads), and over the tokens where those are fewer than the
-// chip holds at once.
+// How the work is split: workgroups of a key head, a row or a group of hypotheses and 16 or 32 queries, and over the tokens where those are
+// fewer than the chip holds at once.
 struct AttendPlan {
-    int qblocks, splits, split_len;
+    int beams, qb, qblocks, splits, split_len;
 };
 
 static AttendPlan attend_plan(const tbs_attend_args &a) {
     const int group = a.heads / a.kv_heads, tile = a.dtype == TBS_F32 ? 16 : 32;
-    AttendPlan pl;
-    pl.qblocks = (group + 15) / 16;
     const int64_t cap = (int64_t)a.table_width * a.page;
     const int64_t longest = a.max_len > 0 && a.max_len < cap ? a.max_len : cap;
-    const int64_t units = (int64_t)a.rows * a.kv_heads * pl.qblocks;
+    AttendPlan pl;
+    // Hypotheses together, where the groups fill the chip: a CU each, with pieces of 512 tokens.  (A group of few tokens that stands alone is sooner
+    // done row by row, from the caches.)
+    pl.beams = a.beams <= TBS_MAX_BEAM && (int64_t)a.rows / a.beams * a.kv_heads * (longest / 512 + 1) >= 256 ? a.beams : 1;
+    const int columns = pl.beams * group;
+    pl.qb = columns > 16 && a.dim <= 128 ? 2 : 1;
+    pl.qblocks = (columns + 16 * pl.qb - 1) / (16 * pl.qb);
+    const int64_t units = (int64_t)a.rows / pl.beams * a.kv_heads * pl.qblocks;
     const int64_t step = ATT_WAVES * tile;   // a tile for every wave
-    int64_t splits = 1024 / units, most = (longest + 2 * step - 1) / (2 * step);
+    int64_t splits = (pl.beams > 1 ? 2048 : 1024) / units, most = (longest + 2 * step - 1) / (2 * step);
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     int64_t len = (longest + splits - 1) / splits;
@@ -356,22 +477,24 @@ extern "C" int64_t tbs_attend_workspace(const tbs_attend_args *args) {
     return pl.splits > 1 ? (int64_t)args->rows * args->heads * pl.splits * (args->dim + 2) * 4 : 0;
 }
 
-template <class T, int DP>
+template <class T, int DP, int QB>
 static void attend_launch(const AttendP &p, hipStream_t st) {
-    const dim3 grid(p.kv_heads * p.qblocks, p.splits, p.rows), block(64 * ATT_WAVES);
-    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, false>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_attend<T, DP, true>), grid, block, 0, st, p);
+    const dim3 grid(p.kv_heads * p.qblocks, p.splits, p.rows / p.beams), block(64 * ATT_WAVES);
+    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_attend<T, DP, QB, true>), grid, block, 0, st, p);
 }
 
 template <class T>
-static hipError_t attend_run(const AttendP &p, hipStream_t st) {
-    if (p.dim <= 32) attend_launch<T, 32>(p, st);
-    else if (p.dim <= 64) attend_launch<T, 64>(p, st);
-    else if (p.dim <= 128) attend_launch<T, 128>(p, st);
-    else attend_launch<T, 256>(p, st);
+static hipError_t attend_run(const AttendP &p, int qb, hipStream_t st) {
+    if (p.dim <= 32) qb == 1 ? attend_launch<T, 32, 1>(p, st) : attend_launch<T, 32, 2>(p, st);
+    else if (p.dim <= 64) qb == 1 ? attend_launch<T, 64, 1>(p, st) : attend_launch<T, 64, 2>(p, st);
+    else if (p.dim <= 128) qb == 1 ? attend_launch<T, 128, 1>(p, st) : attend_launch<T, 128, 2>(p, st);
+    else attend_launch<T, 256, 1>(p, st);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
-        hipLaunchKernelGGL((k_attend_join<T>), dim3(p.heads, p.rows), dim3(256), 0, st, p);
+        int threads = 2;
+        while (threads * 4 < p.dim) threads *= 2;
+        hipLaunchKernelGGL((k_attend_join<T>), dim3(p.heads, p.rows), dim3(256), 0, st, p, threads);
         e = hipGetLastError();
     }
     return e;
@@ -410,12 +533,12 @@ extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) {
     p.kp = a.k_page * es, p.kt = a.k_token * es, p.kh = a.k_head * es, p.vp = a.v_page * es, p.vt = a.v_token * es, p.vh = a.v_head * es;
     p.ld_tables = a.ld_tables;
     p.rows = a.rows, p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = a.heads / a.kv_heads, p.dim = a.dim;
-    p.page = a.page, p.pages = a.pages, p.width = a.table_width, p.splits = pl.splits, p.split_len = pl.split_len, p.qblocks = pl.qblocks;
+    p.page = a.page, p.pages = a.pages, p.width = a.table_width, p.splits = pl.splits, p.split_len = pl.split_len, p.qblocks = pl.qblocks, p.beams = pl.beams;
     const unsigned lg = 31 - __builtin_clz((unsigned)a.page);
     p.page_shift = lg;
     p.page_mul = (a.page & (a.page - 1)) ? (unsigned)((((uint64_t)1 << (32 + lg)) / (unsigned)a.page) + 1) : 0;
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.dim)) * 1.44269504f;
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = a.dtype == TBS_F32 ? attend_run<float>(p, st) : a.dtype == TBS_BF16 ? attend_run<__bf16>(p, st) : attend_run<_Float16>(p, st);
+    const hipError_t e = a.dtype == TBS_F32 ? attend_run<float>(p, pl.qb, st) : a.dtype == TBS_BF16 ? attend_run<__bf16>(p, pl.qb, st) : attend_run<_Float16>(p, pl.qb, st);
     return e == hipSuccess ? TBS_OK : TBS_EHIP;
 }
