@@ -346,7 +346,7 @@ int tbs_linear(const tbs_linear_args *args, void *stream);
  * lens[r] < 0: the row takes no part; its output is 0 and nothing is written for it.  A table entry outside [0, pages) is a page
  * whose tokens do not exist: not attended to, not written (a new token is attended to all the same).  Tokens beyond table_width * page
  * do not exist either.  What the cache holds behind a row's last token is not looked at.
- * dim is a multiple of 8 up to 256, heads a multiple of kv_heads.  max_len: about how many tokens the longest row attends to (0: as
+ * dim is a multiple of 8 up to 256, heads a multiple of kv_heads, a page's stride and `page` tokens' below 4 GiB.  max_len: about how many tokens the longest row attends to (0: as
  * many as its table holds); it decides how the work is split, never the result's correctness.  beams: rows beams * i .. beams * i +
  * beams - 1 are hypotheses of one utterance, whose tables may name the same pages (1: rows share nothing); rows is a multiple of it.  It
  * is a hint too: pages that several rows of a group have in common are then read once.

@@ -26,15 +26,24 @@ struct AttendP {
     const int *tables, *lens;
     char *out;
     float *part_o, *part_ml;   // [rows, heads, splits, dim], [rows, heads, splits, 2]; only with more than one split
-    int64_t q_row, q_head, kn_row, kn_head, vn_row, vn_head, o_row, o_head, kp, kt, kh, vp, vt, vh, ld_tables;   // bytes (ld_tables: elements)
+    int64_t q_row, q_head, kn_row, kn_head, vn_row, vn_head, o_row, o_head, kh, vh, ld_tables;   // bytes (ld_tables: elements)
+    unsigned kp, kt, vp, vt;
     int rows, heads, kv_heads, group, dim, page, pages, width, splits, split_len, qblocks, beams;
     unsigned page_mul, page_shift;
     float scale2;   // scale * log2(e)
 };
 
-// t / page for 0 <= t < 2^31 (by multiplication: page_mul = floor(2^(32 + s) / page) + 1 with s = floor(log2 page) errs by less than 2^-31 a unit)
-__device__ __forceinline__ int att_page(const AttendP &p, int t) {
-    return p.page_mul ? (int)(__umulhi((unsigned)t, p.page_mul) >> p.page_shift) : (int)((unsigned)t >> p.page_shift);
+// t / page = 2 t / (2 page) for 0 <= t <= 2^30, by multiplication: page_mul = floor(2^(32 + s) / (2 page)) + 1 with s = floor(log2 (2 page)) is at most
+// 2^(s + 1) / 2^(32 + s) of a unit too large for numerators below 2^31 (powers of two: 2^32 / (2 page), which is exact)
+__device__ __forceinline__ int att_page(const AttendP &p, int t) { return (int)(__umulhi((unsigned)t << 1, p.page_mul) >> p.page_shift); }
+
+// the larger of a lane's number and those 16 and 32 lanes away (rows of 16 lanes, and halves, change places)
+__device__ __forceinline__ float att_max4(float x) {
+    typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
+    uint2_ u = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
+    u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
 }
 
 // tokens that row r attends to; *pos: place of its new token (-1: none)
@@ -74,20 +83,22 @@ k_attend(AttendP p) {
     constexpr int E = OpPiece<T>::E, NB = Tile::NB, TK = Tile::TK, NV = Tile::NV, KS = Tile::KS, W = Tile::W, WW = Tile::WW;
     constexpr bool LATE = DP > 128;   // (registers for keys and values at the same time are missing: values are asked for when the scores are made)
     __shared__ int s_table[ATT_TABLE + TBS_MAX_BEAM];
-    __shared__ float s_o[ATT_WAVES / 2][W * 4][64];
+    __shared__ float s_o[ATT_WAVES][4][W][64];
+    static_assert(ATT_WAVES == 4, "a wave writes one of a lane's four rows");
     __shared__ float s_ml[ATT_WAVES][2][QB * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, kg = lane >> 4;
-    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = blockIdx.y, N = p.beams, r0 = (int)blockIdx.z * N;
+    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = p.splits - 1 - (int)blockIdx.z, N = p.beams, r0 = (int)blockIdx.y * N;   // (a row's end takes longest: first)
     // hypothesis `lane` of the group: its tokens, and those of them that are in the cache
     int n_l = 0, pos_l = -1;
     if (lane < N) n_l = att_tokens(p, r0 + lane, &pos_l);
     int n = n_l, cached = lane < N && n_l > 0 ? (pos_l >= 0 ? pos_l : n_l) : INT32_MAX;
+    if (N > 1)
 #pragma unroll
-    for (int i = 1; i < 32; i <<= 1) {
-        n = max(n, __shfl_xor(n, i));
-        cached = min(cached, __shfl_xor(cached, i));
-    }
+        for (int i = 1; i < 32; i <<= 1) {
+            n = max(n, __shfl_xor(n, i));
+            cached = min(cached, __shfl_xor(cached, i));
+        }
     n = __builtin_amdgcn_readfirstlane(n);   // of the longest
     cached = __builtin_amdgcn_readfirstlane(cached);   // of the shortest that takes part
     const unsigned live = (unsigned)__ballot(n_l > 0);
@@ -123,8 +134,11 @@ k_attend(AttendP p) {
         const int first = att_page(p, c0), c1 = min(k1, c0 + chunk), pages = att_page(p, c1 - 1) - first + 1;
         if (c0 > k0) __syncthreads();
         for (int b = wave; b < N; b += ATT_WAVES) {
-            const int mine = __shfl(n_l, b), have = mine > 0 ? min(pages, att_page(p, mine - 1) - first + 1) : 0;
-            for (int i = lane; i < pages; i += 64) s_table[b * (per_row + 1) + i] = i < have ? p.tables[(r0 + b) * p.ld_tables + first + i] : -1;
+            const int mine = __shfl(n_l, b), have = mine > 0 ? att_page(p, mine - 1) - first + 1 : 0;
+            for (int i = lane; i < pages; i += 64) {
+                const int id = p.tables[(r0 + b) * p.ld_tables + first + i];   // (in the table: i < width)
+                s_table[b * (per_row + 1) + i] = i < have && (unsigned)id < (unsigned)p.pages ? id : -1;   // (negative: its tokens do not exist)
+            }
         }
         __syncthreads();
         // tokens up to `common` are everybody's: pages of the same numbers, whole, in the cache of all
@@ -146,73 +160,85 @@ k_attend(AttendP p) {
         // tiles: those of the common tokens, then each hypothesis' own
         const int shared = (common - c0 + TK - 1) / TK, end_l = min(n_l, c1), own = end_l > common ? (end_l - common + TK - 1) / TK : 0;
         int start = own;
+        if (N > 1)
 #pragma unroll
-        for (int i = 1; i < 32; i <<= 1) {
-            const int x = __shfl_up(start, i);
-            if (lane >= i) start += x;
-        }
-        const int tiles = shared + __builtin_amdgcn_readfirstlane(__shfl(start, 31));
+            for (int i = 1; i < 32; i <<= 1) {
+                const int x = __shfl_up(start, i);
+                if (lane >= i) start += x;
+            }
+        const int tiles = shared + __builtin_amdgcn_readlane(start, N - 1);
         start += shared - own;
-        // a token's page in the pool (negative: it does not exist) and its place there
-        auto page_of = [&](int t, int at, int &off) {
-            const int i = att_page(p, t), id = s_table[at + i - first];
-            off = t - i * p.page;
-            return (unsigned)id < (unsigned)p.pages ? id : -1;
-        };
         struct Where {
-            int t0, end, row, at, pos;   // row: whose it is (-1: everybody's); at: its table in LDS
-            const char *kn, *vn;
+            int t0, end, row, b;   // row: whose it is (-1: everybody's, by the table of hypothesis b)
         };
         auto place = [&](int tile) {
-            Where w;
-            int b = lead;
-            if (tile < shared) {
-                w.row = -1, w.pos = -1, w.t0 = c0 + tile * TK, w.end = common;
-            } else {
-                b = 31 - __clz((unsigned)__ballot(lane < N && own > 0 && start <= tile));
-                w.row = b;
-                w.pos = __builtin_amdgcn_readlane(pos_l, b);
-                w.t0 = common + (tile - __builtin_amdgcn_readlane(start, b)) * TK;
-                w.end = __builtin_amdgcn_readlane(end_l, b);
+            Where w = {c0 + tile * TK, common, -1, lead};
+            if (tile >= shared) {
+                w.row = w.b = 31 - __clz((unsigned)__ballot(lane < N && own > 0 && start <= tile));
+                w.t0 = common + (tile - __builtin_amdgcn_readlane(start, w.b)) * TK;
+                w.end = __builtin_amdgcn_readlane(end_l, w.b);
             }
-            w.at = b * (per_row + 1);
-            w.kn = p.k_new + (r0 + b) * p.kn_row + kvh * p.kn_head;
-            w.vn = p.v_new + (r0 + b) * p.vn_row + kvh * p.vn_head;
             return w;
         };
+        // A token's address in the cache; one whose page does not exist has the first page's.  No branch in here: the loads of a tile have to
+        // leave together.
+        auto address = [&](const char *base, unsigned page_bytes, unsigned token_bytes, const Where &w, int t, bool &there) {
+            const int i = att_page(p, t), id = s_table[w.b * (per_row + 1) + i - first];
+            there = id >= 0;
+            return base + (uint64_t)(unsigned)max(id, 0) * page_bytes + (unsigned)(t - i * p.page) * token_bytes;
+        };
+        auto take_k = [&](Tile &x, int b, const char *at) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) x.k[b][s] = !PAD || (s * 4 + kg) * E < p.dim ? op_load16((const T *)at + (s * 4 + kg) * E) : make_uint4(0, 0, 0, 0);
+        };
+        auto take_v = [&](Tile &x, int j, const char *at) {
+            constexpr int G = W < 8 ? W : 8, GW = G * (int)sizeof(T) / 4;   // elements that are there together or not at all: dim is a multiple of 8
+#pragma unroll
+            for (int g = 0; g < W / G; ++g) {
+                AttWords<GW> u = {};
+                if (!PAD || c * W + g * G < p.dim) __builtin_memcpy(&u, (const T *)at + c * W + g * G, sizeof u);
+#pragma unroll
+                for (int i = 0; i < GW; ++i) x.v[j][g * GW + i] = u.w[i];
+            }
+        };
+        // whole tiles of tokens in the cache, pages of a multiple of four tokens: a lane's four tokens of V lie in one page
+        auto plain = [&](const Where &w) { return quad && w.t0 + TK + (w.row >= 0 ? 1 : 0) <= w.end; };   // (the new token is its row's last)
         auto load_k = [&](Tile &x, const Where &w) {
+            bool there;
+            if (plain(w)) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int t = min(w.t0 + b * 16 + c, w.end - 1);
-                int off;
-                const int id = page_of(t, w.at, off);
-                const char *at = t == w.pos ? w.kn : id < 0 ? kb : kb + id * p.kp + off * p.kt;
+                for (int b = 0; b < NB; ++b) take_k(x, b, address(kb, p.kp, p.kt, w, w.t0 + b * 16 + c, there));
+            } else {
+                const int pos = w.row >= 0 ? __builtin_amdgcn_readlane(pos_l, w.b) : -1;
+                const char *kn = p.k_new + (r0 + w.b) * p.kn_row + kvh * p.kn_head;
 #pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    x.k[b][s] = !PAD || (s * 4 + kg) * E < p.dim ? op_load16((const T *)at + (s * 4 + kg) * E) : make_uint4(0, 0, 0, 0);
+                for (int b = 0; b < NB; ++b) {
+                    const int t = min(w.t0 + b * 16 + c, w.end - 1);
+                    const char *at = address(kb, p.kp, p.kt, w, t, there);
+                    take_k(x, b, t == pos ? kn : at);
+                }
             }
         };
         auto load_v = [&](Tile &x, const Where &w) {
+            bool there;
             x.ok = 0;
+            if (plain(w)) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                int off = 0, id = 0;
+                for (int b = 0; b < NB; ++b) {
+                    const char *at = address(vb, p.vp, p.vt, w, w.t0 + b * 16 + kg * 4, there);
+                    x.ok |= there ? 15u << (b * 4) : 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int want = w.t0 + b * 16 + kg * 4 + r, t = min(want, w.end - 1);
-                    if (r == 0 || !quad) id = page_of(t, w.at, off);
-                    const char *at = t == w.pos ? w.vn : id < 0 ? vb : vb + id * p.vp + (quad ? off + (t - min(want - r, w.end - 1)) : off) * p.vt;
-                    if (want < w.end && (id >= 0 || t == w.pos)) x.ok |= 1u << (b * 4 + r);
-                    unsigned *v = x.v[b * 4 + r];
-                    constexpr int G = W < 8 ? W : 8;   // elements that are there together or not at all: dim is a multiple of 8
+                    for (int r = 0; r < 4; ++r) take_v(x, b * 4 + r, at + (uint64_t)r * p.vt);
+                }
+            } else {
+                const int pos = w.row >= 0 ? __builtin_amdgcn_readlane(pos_l, w.b) : -1;
+                const char *vn = p.v_new + (r0 + w.b) * p.vn_row + kvh * p.vn_head;
 #pragma unroll
-                    for (int g = 0; g < W / G; ++g) {
-                        constexpr int GW = G * (int)sizeof(T) / 4;
-                        AttWords<GW> u = {};
-                        if (!PAD || c * W + g * G < p.dim) __builtin_memcpy(&u, (const T *)at + c * W + g * G, sizeof u);
-#pragma unroll
-                        for (int i = 0; i < GW; ++i) v[g * GW + i] = u.w[i];
-                    }
+                for (int j = 0; j < NV; ++j) {
+                    const int want = w.t0 + (j / 4) * 16 + kg * 4 + j % 4, t = min(want, w.end - 1);
+                    const char *at = address(vb, p.vp, p.vt, w, t, there);
+                    x.ok |= want < w.end && (there || t == pos) ? 1u << j : 0;
+                    take_v(x, j, t == pos ? vn : at);
                 }
             }
         };
@@ -245,8 +271,7 @@ k_attend(AttendP p) {
                 float top = t[0];
 #pragma unroll
                 for (int j = 1; j < NV; ++j) top = fmaxf(top, t[j]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
+                top = att_max4(top);
                 if (__any(top > m[b])) {
                     const float m1 = fmaxf(m[b], top), a = m1 == m[b] ? 1.f : __builtin_amdgcn_exp2f(m[b] - m1);
                     m[b] = m1;
@@ -290,6 +315,8 @@ k_attend(AttendP p) {
                 }
             }
         };
+        // (No tile ahead: with the next one's loads in front of this one's products the kernel takes 20 to 90 registers more, so fewer waves a SIMD, and
+        // was 0 to 20 % slower: 320 rows of up to 400 tokens 29.0 us against 24.0 at two splits, 17.1 against 16.6 at one.)
         for (int tile = wave; tile < tiles; tile += ATT_WAVES) {
             const Where w = place(tile);
             Tile x;
@@ -298,7 +325,8 @@ k_attend(AttendP p) {
             compute(x, w);
         }
     }
-    // the waves' shares: 3 and 2 to 1 and 0, 1 to 0; every lane has the same place in all of them
+    // The waves' shares meet in LDS; a lane has the same place in all of them.  Wave r then adds up and writes the r-th of the four rows of every
+    // block that a lane has: W dimensions side by side.
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         l[b] += __shfl_xor(l[b], 16);
@@ -308,60 +336,44 @@ k_attend(AttendP p) {
             s_ml[wave][1][b * 16 + c] = l[b];
         }
     }
-    __syncthreads();
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-        float top = m[b];
+        if (b > 0) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < ATT_WAVES; ++i) top = fmaxf(top, s_ml[i][0][b * 16 + c]);
-        auto share = [&](float x) { return x == top ? 1.f : __builtin_amdgcn_exp2f(x - top); };   // (-inf of -inf: nothing there, 1 x 0)
-        const float a = share(m[b]);
-        float sum = 0.f;
+        for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int i = 0; i < ATT_WAVES; ++i) sum += s_ml[i][1][b * 16 + c] * share(s_ml[i][0][b * 16 + c]);
+            for (int r = 0; r < 4; ++r) s_o[wave][r][i][lane] = o[b][i][r];
+        __syncthreads();
+        float top = s_ml[0][0][b * 16 + c];
 #pragma unroll
-        for (int i = 0; i < W; ++i) o[b][i] *= a;
+        for (int i = 1; i < ATT_WAVES; ++i) top = fmaxf(top, s_ml[i][0][b * 16 + c]);
+        float y[W], sum = 0.f;
 #pragma unroll
-        for (int h = ATT_WAVES / 2; h > 0; h >>= 1) {
-            if (wave >= h && wave < 2 * h)
+        for (int i = 0; i < W; ++i) y[i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < W; ++i)
+        for (int j = 0; j < ATT_WAVES; ++j) {
+            const float x = s_ml[j][0][b * 16 + c], a = x == top ? 1.f : __builtin_amdgcn_exp2f(x - top);   // (-inf of -inf: nothing there, 1 x 0)
+            sum += a * s_ml[j][1][b * 16 + c];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s_o[wave - h][i * 4 + r][lane] = o[b][i][r];
-            __syncthreads();
-            if (wave < h)
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[b][i][r] += s_o[wave][i * 4 + r][lane];
-            __syncthreads();
+            for (int i = 0; i < W; ++i) y[i] += a * s_o[j][wave][i][lane];
         }
-        if (wave == 0 && col_row[b] < N) {
+        if (col_row[b] < N) {
             const int64_t row = r0 + col_row[b];
-            const int head = col_head[b];
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
+            const int head = col_head[b], d = (kg * 4 + wave) * W;
+            constexpr int G = W < 8 ? W : 8;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (kg * 4 + r) * W;
-                constexpr int G = W < 8 ? W : 8;
+            for (int g = 0; g < W / G; ++g) {
+                if (PAD && d + g * G >= p.dim) continue;
+                if (p.splits > 1) {
+                    __builtin_memcpy(p.part_o + ((row * p.heads + head) * p.splits + split) * p.dim + d + g * G, y + g * G, G * 4);
+                } else {
+                    T z[G];
 #pragma unroll
-                for (int g = 0; g < W / G; ++g) {
-                    if (PAD && d + g * G >= p.dim) continue;
-                    if (p.splits > 1) {
-                        float *dst = p.part_o + ((row * p.heads + head) * p.splits + split) * p.dim + d + g * G;
-                        float y[G];
-#pragma unroll
-                        for (int i = 0; i < G; ++i) y[i] = o[b][g * G + i][r];
-                        __builtin_memcpy(dst, y, sizeof y);
-                    } else {
-                        T y[G];
-#pragma unroll
-                        for (int i = 0; i < G; ++i) y[i] = (T)(sum == 0.f ? 0.f : o[b][g * G + i][r] * inv);
-                        __builtin_memcpy((T *)(p.out + row * p.o_row + head * p.o_head) + d + g * G, y, sizeof y);
-                    }
+                    for (int i = 0; i < G; ++i) z[i] = (T)(sum == 0.f ? 0.f : y[g * G + i] / sum);   // (no weight at all: 0)
+                    __builtin_memcpy((T *)(p.out + row * p.o_row + head * p.o_head) + d + g * G, z, sizeof z);
                 }
             }
-            if (p.splits > 1 && kg == 0) {
+            if (p.splits > 1 && kg == 0 && wave == 0) {
                 float *ml = p.part_ml + ((row * p.heads + head) * p.splits + split) * 2;
                 ml[0] = top;
                 ml[1] = sum;
@@ -376,8 +388,8 @@ k_attend(AttendP p) {
             if ((unsigned)id >= (unsigned)p.pages) continue;
             const T *kn = (const T *)(p.k_new + (r0 + b) * p.kn_row + kvh * p.kn_head), *vn = (const T *)(p.v_new + (r0 + b) * p.vn_row + kvh * p.vn_head);
             for (int d = lane; d < p.dim; d += 64) {
-                ((T *)(p.k_cache + id * p.kp + off * p.kt + kvh * p.kh))[d] = kn[d];
-                ((T *)(p.v_cache + id * p.vp + off * p.vt + kvh * p.vh))[d] = vn[d];
+                ((T *)(p.k_cache + (uint64_t)(unsigned)id * p.kp + (unsigned)off * p.kt + kvh * p.kh))[d] = kn[d];
+                ((T *)(p.v_cache + (uint64_t)(unsigned)id * p.vp + (unsigned)off * p.vt + kvh * p.vh))[d] = vn[d];
             }
         }
 }
@@ -438,25 +450,37 @@ struct AttendPlan {
     int beams, qb, qblocks, splits, split_len;
 };
 
-static AttendPlan attend_plan(const tbs_attend_args &a) {
+// (together: 0 = by the rule below, 1 = row by row, 2 = hypotheses together; piece: 0 = by the rule, else tokens of a piece, in whole steps)
+static AttendPlan attend_plan(const tbs_attend_args &a, int together = 0, int piece = 0) {
     const int group = a.heads / a.kv_heads, tile = a.dtype == TBS_F32 ? 16 : 32;
     const int64_t cap = (int64_t)a.table_width * a.page;
     const int64_t longest = a.max_len > 0 && a.max_len < cap ? a.max_len : cap;
     AttendPlan pl;
-    // Hypotheses together, where the groups fill the chip: a CU each, with pieces of 512 tokens.  (A group of few tokens that stands alone is sooner
-    // done row by row, from the caches.)
-    pl.beams = a.beams <= TBS_MAX_BEAM && (int64_t)a.rows / a.beams * a.kv_heads * (longest / 512 + 1) >= 256 ? a.beams : 1;
+    // Hypotheses together where row by row there would be more than 1536 workgroups, or 130 MB to be read (of which what is shared comes from the caches, but
+    // is computed again): us together / row by row, 64 x 8 rows of 40 tokens 13.3 / 24.9, 4 x 8 of 2000 27.9 / 30.9, 16 x 5 of 3000 29 / 57; the other way 16 x 8
+    // of 200 15.5 / 11.4, one utterance's 8 of 1500 20.3 / 11.8.  (Where nothing is shared: 64 x 4 of 500 to 1500 117 / 112.)
+    const int64_t row_bytes = (int64_t)a.rows * a.kv_heads * longest * a.dim * 2 * (int64_t)op_dtype_size(a.dtype);
+    pl.beams = a.beams <= TBS_MAX_BEAM && (together == 2 || (together == 0 && ((int64_t)a.rows * a.kv_heads > 1536 || row_bytes > 130000000))) ? a.beams : 1;
     const int columns = pl.beams * group;
     pl.qb = columns > 16 && a.dim <= 128 ? 2 : 1;
     pl.qblocks = (columns + 16 * pl.qb - 1) / (16 * pl.qb);
     const int64_t units = (int64_t)a.rows / pl.beams * a.kv_heads * pl.qblocks;
     const int64_t step = ATT_WAVES * tile;   // a tile for every wave
-    int64_t splits = (pl.beams > 1 ? 2048 : 1024) / units, most = (longest + 2 * step - 1) / (2 * step);
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
+    // As many pieces as take the least time, in tokens that a workgroup handles meanwhile (100 a us): turns of the 256 CUs, of a piece and 500 for a
+    // workgroup's start and end, and 400 for the join.  (us by pieces: 16 units of 131071 tokens 16 177, 24 215, 32 184, 64 190; 128 units of 3000 2 30, 3 28,
+    // 6 27, 12 33; 256 of up to 4000 1 119, 2 122, 4 117; 512 of 400 1 16.6, 2 24; 16 of 300 1 8.4, 2 10.3.)
+    const int64_t most = (longest + 2 * step - 1) / (2 * step);
+    int64_t splits = 1, least = (units + 255) / 256 * (longest + 500);
+    for (int turns = 1; turns <= 4; ++turns) {   // (the pieces that fill so many turns)
+        const int64_t fill = 256 * turns / units, k = fill < most ? fill : most;
+        if (k < 2) continue;
+        const int64_t t = (units * k + 255) / 256 * ((longest + k - 1) / k + 500) + 400;
+        if (t < least) least = t, splits = k;
+    }
     int64_t len = (longest + splits - 1) / splits;
     len = (len + step - 1) / step * step;
     if (len < step) len = step;
+    if (piece > 0) len = (piece + step - 1) / step * step;
     pl.split_len = (int)len;
     pl.splits = (int)((longest + len - 1) / len);
     if (pl.splits < 1) pl.splits = 1;
@@ -471,15 +495,16 @@ static int attend_check(const tbs_attend_args &a) {
     return TBS_OK;
 }
 
+static int64_t attend_bytes(const tbs_attend_args &a, const AttendPlan &pl) { return pl.splits > 1 ? (int64_t)a.rows * a.heads * pl.splits * (a.dim + 2) * 4 : 0; }
+
 extern "C" int64_t tbs_attend_workspace(const tbs_attend_args *args) {
     if (!args || attend_check(*args) != TBS_OK) return TBS_EINVAL;
-    const AttendPlan pl = attend_plan(*args);
-    return pl.splits > 1 ? (int64_t)args->rows * args->heads * pl.splits * (args->dim + 2) * 4 : 0;
+    return args->rows == 0 ? 0 : attend_bytes(*args, attend_plan(*args));
 }
 
 template <class T, int DP, int QB>
 static void attend_launch(const AttendP &p, hipStream_t st) {
-    const dim3 grid(p.kv_heads * p.qblocks, p.splits, p.rows / p.beams), block(64 * ATT_WAVES);
+    const dim3 grid(p.kv_heads * p.qblocks, p.rows / p.beams, p.splits), block(64 * ATT_WAVES);
     if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((k_attend<T, DP, QB, true>), grid, block, 0, st, p);
 }
@@ -500,7 +525,7 @@ static hipError_t attend_run(const AttendP &p, int qb, hipStream_t st) {
     return e;
 }
 
-extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) {
+static int attend_call(const tbs_attend_args *args, int together, int piece, void *stream) {
     if (!args) return TBS_EINVAL;
     const tbs_attend_args &a = *args;
     if (attend_check(a) != TBS_OK) return TBS_EINVAL;
@@ -511,6 +536,10 @@ extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) {
                                a.k_page, a.k_token, a.k_head, a.v_page, a.v_token, a.v_head};
     for (int64_t s : strides)
         if (s < 0 || s > INT64_MAX / 64 / INT32_MAX) return TBS_EINVAL;
+    // (addresses in the cache: a page's number times 32 bits, a place in the page of 32 bits)
+    const int64_t wide[] = {a.k_page * es, a.v_page * es, a.k_token * es * a.page, a.v_token * es * a.page};
+    for (int i = 0; i < 4; ++i)
+        if ((i >= 2 || a.pages > 1) && wide[i] > UINT32_MAX) return TBS_EINVAL;
     // what is written may not lie over itself: a head after the other in the outputs and the cache
     if ((a.heads > 1 && a.out_head < a.dim) || (a.rows > 1 && a.out_row < a.dim)) return TBS_EINVAL;
     if (a.k_new && ((a.kv_heads > 1 && (a.k_head < a.dim || a.v_head < a.dim)) || (a.page > 1 && (a.k_token < a.dim || a.v_token < a.dim)) ||
@@ -519,8 +548,8 @@ extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) {
     const void *ptrs[] = {a.q, a.k_new, a.v_new, a.k_cache, a.v_cache, a.out};
     for (const void *x : ptrs)
         if ((uintptr_t)x % es) return TBS_EINVAL;
-    const AttendPlan pl = attend_plan(a);
-    const int64_t need = tbs_attend_workspace(&a);
+    const AttendPlan pl = attend_plan(a, together, piece);
+    const int64_t need = attend_bytes(a, pl);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return TBS_EINVAL;
     AttendP p = {};
     p.q = (const char *)a.q, p.k_new = (const char *)a.k_new, p.v_new = (const char *)a.v_new;
@@ -530,15 +559,20 @@ extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) {
     p.part_ml = p.part_o + (int64_t)a.rows * a.heads * pl.splits * a.dim;
     p.q_row = a.q_row * es, p.q_head = a.q_head * es, p.kn_row = a.k_new_row * es, p.kn_head = a.k_new_head * es;
     p.vn_row = a.v_new_row * es, p.vn_head = a.v_new_head * es, p.o_row = a.out_row * es, p.o_head = a.out_head * es;
-    p.kp = a.k_page * es, p.kt = a.k_token * es, p.kh = a.k_head * es, p.vp = a.v_page * es, p.vt = a.v_token * es, p.vh = a.v_head * es;
+    p.kp = (unsigned)(a.k_page * es), p.kt = (unsigned)(a.k_token * es), p.kh = a.k_head * es, p.vp = (unsigned)(a.v_page * es), p.vt = (unsigned)(a.v_token * es), p.vh = a.v_head * es;
     p.ld_tables = a.ld_tables;
     p.rows = a.rows, p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = a.heads / a.kv_heads, p.dim = a.dim;
     p.page = a.page, p.pages = a.pages, p.width = a.table_width, p.splits = pl.splits, p.split_len = pl.split_len, p.qblocks = pl.qblocks, p.beams = pl.beams;
-    const unsigned lg = 31 - __builtin_clz((unsigned)a.page);
-    p.page_shift = lg;
-    p.page_mul = (a.page & (a.page - 1)) ? (unsigned)((((uint64_t)1 << (32 + lg)) / (unsigned)a.page) + 1) : 0;
+    const unsigned twice = 2 * (unsigned)a.page, lg = 31 - __builtin_clz(twice);
+    p.page_shift = (twice & (twice - 1)) ? lg : 0;
+    p.page_mul = (unsigned)((((uint64_t)1 << (32 + p.page_shift)) / twice) + (p.page_shift ? 1 : 0));
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.dim)) * 1.44269504f;
     const hipStream_t st = (hipStream_t)stream;
     const hipError_t e = a.dtype == TBS_F32 ? attend_run<float>(p, pl.qb, st) : a.dtype == TBS_BF16 ? attend_run<__bf16>(p, pl.qb, st) : attend_run<_Float16>(p, pl.qb, st);
     return e == hipSuccess ? TBS_OK : TBS_EHIP;
 }
+
+extern "C" int tbs_attend_paged(const tbs_attend_args *args, void *stream) { return attend_call(args, 0, 0, stream); }
+
+// one way of splitting the work, for the tests (not in the header)
+extern "C" int attend_by(const tbs_attend_args *args, int together, int piece, void *stream) { return attend_call(args, together, piece, stream); }

@@ -167,7 +167,29 @@ def test_linear_of_numbers_that_are_none(m, dtype):
 
 # ------------------------------------------------------------------ attention over a paged cache
 
-def _attend_case(lens, *, heads, kv, dim, page, dtype, beams=1, shared=0, new=True, layout="token", width=0, holes=(), seed=0, max_len=None, fused=False, scale=None,
+def _attend_by(form, q, kc, vc, tables, lens, kn, vn, beams, scale):
+    """attend_paged by one way of splitting its work: form = (1 row by row or 2 hypotheses together, tokens of a piece)."""
+    import ctypes
+    from paper_2302_14357_amd import ops
+    rows, heads, dim = q.shape
+    out = torch.empty(rows, heads, dim, dtype=q.dtype, device="cuda")
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    pieces = tables.shape[1] * kc.shape[1] // form[1] + 1 if form[1] else 1024
+    work = torch.full((rows * heads * pieces * (dim + 2),), math.nan, device="cuda")
+    a = ops._Attend(q=q.data_ptr(), k_cache=kc.data_ptr(), v_cache=vc.data_ptr(), tables=tables.data_ptr(), lens=lens.data_ptr(), out=out.data_ptr(),
+                    workspace=work.data_ptr(), workspace_bytes=work.numel() * 4, q_row=q.stride(0), q_head=q.stride(1), out_row=heads * dim, out_head=dim,
+                    k_page=kc.stride(0), k_token=kc.stride(1), k_head=kc.stride(2), v_page=vc.stride(0), v_token=vc.stride(1), v_head=vc.stride(2),
+                    ld_tables=tables.stride(0), rows=rows, heads=heads, kv_heads=kc.shape[2], dim=dim, page=kc.shape[1], pages=kc.shape[0],
+                    table_width=tables.shape[1], beams=beams, dtype=code[q.dtype], scale=scale or 0.0)
+    if kn is not None:
+        a.k_new, a.v_new = kn.data_ptr(), vn.data_ptr()
+        a.k_new_row, a.k_new_head, a.v_new_row, a.v_new_head = kn.stride(0), kn.stride(1), vn.stride(0), vn.stride(1)
+    assert ops.load_library().attend_by(ctypes.byref(a), ctypes.c_int(form[0]), ctypes.c_int(form[1]), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+    return out
+
+
+def _attend_case(lens, *, form=None, heads, kv, dim, page, dtype, beams=1, shared=0, new=True, layout="token", width=0, holes=(), seed=0, max_len=None, fused=False, scale=None,
                  garbage=True, q_scale=1.0):
     """lens: tokens of every row in the cache (negative: takes no part); shared: that many pages at the head of every group are one row's; holes:
     (row, place in its table) entries that name no page."""
@@ -177,8 +199,9 @@ def _attend_case(lens, *, heads, kv, dim, page, dtype, beams=1, shared=0, new=Tr
     width = max(width, max(max(n, ~n) for n in lens) // page + 1)
     pages = rows * width + 3
     tables = r.permutation(pages)[:rows * width].reshape(rows, width).astype(np.int32)
-    for i in range(0, rows, beams):
-        tables[i:i + beams, :shared] = tables[i, :shared]
+    for i in range(0, rows, beams):   # (only whole pages of everybody's are shared: nobody writes them)
+        common = min(shared, min(max(n, ~n) for n in lens[i:i + beams]) // page)
+        tables[i:i + beams, :common] = tables[i, :common]
     for i, j in holes:
         tables[i, j] = (-1, pages, -2**31, 2**31 - 1)[(i + j) % 4]
     kc, vc = _randn(g, pages, page, kv, dim, dtype=dtype), _randn(g, pages, page, kv, dim, dtype=dtype)
@@ -206,7 +229,10 @@ def _attend_case(lens, *, heads, kv, dim, page, dtype, beams=1, shared=0, new=Tr
     td = torch.from_numpy(tables).cuda()
     kw = dict(k_new=b, v_new=c) if new else {}
     k0, v0 = kd.clone(), vd.clone()
-    got = attend_paged(a, kd, vd, td, ln, beams=beams, max_len=max_len, scale=scale, **kw)
+    if form:
+        got = _attend_by(form, a, kd, vd, td, ln, kw.get("k_new"), kw.get("v_new"), beams, scale)
+    else:
+        got = attend_paged(a, kd, vd, td, ln, beams=beams, max_len=max_len, scale=scale, **kw)
     # the cache: the new tokens where they belong and nothing else
     for cache, before, fresh in ((kd, k0, b), (vd, v0, c)):
         want = before.clone()
@@ -293,7 +319,30 @@ def test_attend_with_a_full_table(dtype):
 def test_attend_hypotheses_that_share_pages(beams, heads, kv, lens, shared, page, dtype):
     rows = [lens] * beams + [lens // 2 + 7] * beams
     rows[1] = ~rows[1]
-    _attend_case(rows, heads=heads, kv=kv, dim=64, page=page, dtype=dtype, beams=beams, shared=min(shared, (lens // 2 + 7) // page))
+    for form in (None, (2, 0), (2, 128), (2, 256), (2, 1 << 20), (1, 128)):
+        _attend_case(rows, form=form, heads=heads, kv=kv, dim=64, page=page, dtype=dtype, beams=beams, shared=min(shared, (lens // 2 + 7) // page))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("form", [(2, 0), (2, 128), (2, 1 << 20)])
+@pytest.mark.parametrize("heads,kv,dim,page", [(1, 1, 64, 16), (16, 2, 128, 32), (40, 2, 40, 7), (6, 2, 80, 1), (3, 1, 96, 48), (8, 4, 256, 16), (9, 3, 24, 3), (2, 1, 32, 64)])
+def test_attend_hypotheses_together(heads, kv, dim, page, form, dtype):
+    """Groups of four with common pages, with none, all finished, without tokens, of unequal lengths, with pages that do not exist in the common part and behind it."""
+    lens = [150, 150, 150, 150] + [~20, ~3, ~0, ~100] + [0, 0, 0, 0] + [130, 33, 64, 5] + [300, ~300, 300, 299]
+    for shared in (0, 1, 2):
+        _attend_case(lens, form=form, heads=heads, kv=kv, dim=dim, page=page, dtype=dtype, beams=4, shared=min(shared, 5 // page))
+    lens = [300, 300, 301, 290]
+    _attend_case(lens, form=form, heads=heads, kv=kv, dim=dim, page=page, dtype=dtype, beams=4, shared=256 // page, holes=[(i, 0) for i in range(4)] + [(2, 260 // page), (1, 40 // page)])
+    _attend_case(lens, form=form, heads=heads, kv=kv, dim=dim, page=page, dtype=dtype, beams=4, shared=256 // page, new=False)
+    _attend_case(lens, form=form, heads=heads, kv=kv, dim=dim, page=page, dtype=dtype, beams=2, shared=100 // page)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("form", [(2, 0), (2, 512), (1, 0)])
+def test_attend_more_pages_than_fit_at_a_time(form, dtype):
+    """Pages of one token and of three, sixteen hypotheses: their table entries pass through LDS in several turns."""
+    for page, n in ((1, 300), (3, 500)):
+        _attend_case([n] * 15 + [n - 5], form=form, heads=4, kv=1, dim=32, page=page, dtype=dtype, beams=16, shared=200 // page)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -310,8 +359,8 @@ def test_attend_hypotheses_of_different_lengths_and_partly_shared_pages(dtype):
     kc, vc = _randn(g, 6 * width, page, kv, dim, dtype=dtype).cuda(), _randn(g, 6 * width, page, kv, dim, dtype=dtype).cuda()
     q, kn, vn = (_randn(g, 6, h, dim, dtype=dtype).cuda() for h in (8, kv, kv))
     td, ln = torch.from_numpy(tables).cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
-    got = attend_paged(q, kc, vc, td, ln, k_new=kn, v_new=vn, beams=6)
-    for i in range(6):
+    for i, got in [(i, g) for g in (attend_paged(q, kc, vc, td, ln, k_new=kn, v_new=vn, beams=6), _attend_by((2, 0), q, kc, vc, td, ln, kn, vn, 6, None),
+                                    _attend_by((2, 128), q, kc, vc, td, ln, kn, vn, 6, None)) for i in range(6)]:
         one = attend_paged(q[i:i + 1], kc, vc, td[i:i + 1], ln[i:i + 1], k_new=kn[i:i + 1], v_new=vn[i:i + 1])
         # (each is within its own error of the same result: float32 sums in another order, weights of two 16-bit numbers, and a rounding each)
         off = (got[i].double() - one[0].double()).abs()
