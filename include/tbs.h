@@ -377,7 +377,7 @@ int64_t tbs_attend_workspace(const tbs_attend_args *args);
  * every token of a row with a logit that is NaN or +inf or with none above -inf, and every row whose score is -inf (the rows that do not
  * exist yet at the first step).  Where a group has fewer than `beams` candidates its last places are: score -inf, token -1, parent
  * -1, finished.  A place is also finished where its token is eos or its parent was.  parents are places in the group, 0 .. beams - 1.
- * workspace: tbs_beam_select_workspace(args) bytes on a 16-byte boundary.  The same call gives the same bits. */
+ * workspace: tbs_beam_select_workspace(args) bytes on a 16-byte boundary (0: none).  The same call gives the same bits. */
 #define TBS_MAX_VOCAB 524288
 typedef struct tbs_beam_select_args {
     const void *logits;       /* [rows, vocab] in dtype, row stride ld_logits */

@@ -1,7 +1,7 @@
 // The best continuations of groups of hypotheses over a vocabulary (no transducer blank): scores + log softmax(logits), the best
 // `beams` of beams x vocabulary.
 //
-// Two launches.  k_vocab_part reads the logits once, a workgroup a slice of at most 8192 of a row, in registers: its maximum, sum of
+// One launch for small vocabularies (k_vocab_small), else two.  k_vocab_part reads the logits once, a workgroup a slice of at most 8192 of a row, in registers: its maximum, sum of
 // exponentials and best candidates.  k_vocab_join has a workgroup a group: the slices' sums give each row's normaliser, their lists its best
 // logits, and the rows' lists the group's best scores.
 #include "op_device.h"
@@ -10,6 +10,7 @@ typedef unsigned long long vk_u64;
 
 #define VOC_SLICE 8192
 #define VOC_ELEMS (VOC_SLICE / 256)
+#define VOC_SMALL (64 * VOC_ELEMS)
 #define VOC_SPLITS (TBS_MAX_VOCAB / VOC_SLICE)   // at most a wave's lanes
 
 struct VocabP {
@@ -57,6 +58,31 @@ __device__ __forceinline__ vk_u64 voc_shfl_xor(vk_u64 v, int i) {
     return (vk_u64)__shfl_xor((unsigned)(v >> 32), i) << 32 | (unsigned)__shfl_xor((unsigned)v, i);
 }
 
+// The other operand of a reduction over the wave that any order of lanes serves, step 0 to 5: lanes 1 and 2 away, mirrored in 8 and in 16, and
+// rows of 16 and halves exchanged; all without LDS.
+typedef unsigned voc_uint2 __attribute__((ext_vector_type(2)));
+template <int STEP>
+__device__ __forceinline__ unsigned voc_other(unsigned x) {
+    if constexpr (STEP < 4) {
+        constexpr int CTRL[4] = {0xB1, 0x4E, 0x141, 0x140};   // quad_perm 1 0 3 2, quad_perm 2 3 0 1, row_half_mirror, row_mirror
+        return __builtin_amdgcn_update_dpp(0u, x, CTRL[STEP], 0xF, 0xF, true);
+    } else {
+        const voc_uint2 u = STEP == 4 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        const bool upper = (threadIdx.x & (STEP == 4 ? 16 : 32)) != 0;   // (u[0]: the lower row or half in both, u[1]: the upper)
+        return upper ? u[0] : u[1];
+    }
+}
+template <int STEP = 0>
+__device__ __forceinline__ float voc_max(float x) {
+    if constexpr (STEP == 6) return x;
+    else return voc_max<STEP + 1>(fmaxf(x, __uint_as_float(voc_other<STEP>(__float_as_uint(x)))));
+}
+template <int STEP = 0>
+__device__ __forceinline__ double voc_add(double x) {
+    if constexpr (STEP == 6) return x;
+    else return voc_add<STEP + 1>(x + __hiloint2double((int)voc_other<STEP>((unsigned)__double2hiint(x)), (int)voc_other<STEP>((unsigned)__double2loint(x))));
+}
+
 // what lanes of a wave wrote to LDS is there for its others
 __device__ __forceinline__ void voc_wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -64,46 +90,51 @@ __device__ __forceinline__ void voc_wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-template <class T>
-__global__ void __launch_bounds__(256)
-k_vocab_part(VocabP p) {
-    constexpr int E = OpPiece<T>::E, PASS = 256 * E, PASSES = VOC_SLICE / PASS;
-    __shared__ vk_u64 s_cand[4][64], s_best[4][TBS_MAX_BEAM];
-    __shared__ double s_sum[4];
-    __shared__ float s_top[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.y, split = blockIdx.x;
-    if (p.finished && p.finished[row]) return;   // (nobody reads its lists)
-    const int v0 = split * p.slice, count = min(p.slice, p.vocab - v0), N = p.beams;
-    const T *l = (const T *)p.logits + row * p.ld + v0;
-    float v[VOC_ELEMS];
+// A wave's N best of `used` numbers a lane, those from `from` on, one after the other: for many equal ones.
+template <int ELEMS, class Token>
+__device__ __forceinline__ void voc_wave_slow(float (&v)[ELEMS], float from, int used, int N, vk_u64 *best, Token token) {
+    for (int i = 0; i < N; ++i) {
+        vk_u64 k = 0;
+        const vk_u64 before = i > 0 ? best[i - 1] : ~0ull;
+        int zero = 0;
+        asm volatile("" : "+v"(zero));   // (made anew each time: 32 keys kept over the loop would cost every call its registers)
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-        const int at = i * PASS + tid * E;
-        if (i * PASS < count && at + E <= count) {
-            const uint4 u = op_load16(l + at);
-            T e[E];
-            __builtin_memcpy(e, &u, 16);
+        for (int j = 0; j < ELEMS; ++j) {
+            asm volatile("" : "+v"(v[j]));
+            const vk_u64 kj = (vk_u64)voc_key(v[j]) << 32 | (unsigned)~token(j, zero);
+            if (j < used && v[j] >= from && kj > k && kj < before) k = kj;
+        }
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[i * E + j] = op_float(e[j]) + 0.f;   // (+ 0: -0 and 0 are equal logits)
-        } else {
+        for (int x = 1; x < 64; x <<= 1) k = max(k, voc_shfl_xor(k, x));
+        if ((threadIdx.x & 63) == 0) best[i] = k;
+        voc_wave_sync();
+    }
+}
+
+// The numbers of a wave from `from` on, as keys, into cand (64 at most are written); how many they are.
+template <int ELEMS, class Token>
+__device__ __forceinline__ int voc_collect(const float (&v)[ELEMS], float from, int used, vk_u64 *cand, Token token) {
+    int found = 0;
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[i * E + j] = i * PASS < count && at + j < count ? op_float(l[at + j]) + 0.f : -INFINITY;
+    for (int j = 0; j < ELEMS; ++j) {
+        if (j >= used) continue;
+        const vk_u64 m = __ballot(v[j] >= from);
+        if (m) {
+            const int at = found + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
+            if (v[j] >= from && at < 64) cand[at] = (vk_u64)voc_key(v[j]) << 32 | (unsigned)~token(j, 0);
+            found += __popcll(m);
         }
     }
-    float mine = -INFINITY;
-    bool bad = false;   // NaN or +inf
-#pragma unroll
-    for (int j = 0; j < VOC_ELEMS; ++j) {
-        mine = fmaxf(mine, v[j]);
-        bad |= !(v[j] < INFINITY);
-    }
-    float top = mine;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-    if (__any(bad)) top = NAN;
-    if (lane == 0) s_top[wave] = top;
-    // The wave's N best.  At least N lanes have a maximum of `least` or more, so the N best are among the elements from there on: the
-    // N-th largest lane maximum, cut to its first 16 bits (what a bf16 has), found bit by bit.
+    return found;
+}
+
+// A wave's N best of `used` numbers a lane, best first, into best[0 .. N) in LDS: keys of (number, the lower token first), 0 where there are fewer
+// above -inf.  At least N lanes have a maximum of `least` or more, so the N best are among the numbers from there on: the N-th
+// largest lane maximum, cut to its first 16 bits (what a bf16 has), found bit by bit.  They are collected, at most 64 of them, and a lane
+// each finds its rank by counting; more of them (many equal logits) are taken one after the other.
+template <int ELEMS, class Token>
+__device__ __forceinline__ void voc_wave_best(float (&v)[ELEMS], float mine, int used, int N, vk_u64 *cand, vk_u64 *best, Token token) {
+    const int lane = threadIdx.x & 63;
     unsigned least = 0;
     const unsigned key = voc_key(mine);
 #pragma unroll
@@ -112,158 +143,280 @@ k_vocab_part(VocabP p) {
         if (__popcll(__ballot(key >= t)) >= N) least = t;
     }
     const float from = voc_unkey(max(least, voc_key(-INFINITY) + 1));   // (-inf is no candidate)
-    int found = 0;
+    const int found = voc_collect(v, from, used, cand, token);
+    if (lane < N) best[lane] = 0;
+    voc_wave_sync();
+    if (found <= 64) {
+        const vk_u64 k = lane < found ? cand[lane] : 0;
+        int rank = 0;
+        for (int i = 0; i < found; ++i) rank += cand[i] > k;
+        if (lane < found && rank < N) best[rank] = k;
+        voc_wave_sync();
+    } else {
+        voc_wave_slow(v, from, used, N, best, token);
+    }
+}
+
+// `count` logits, pieces of 16 bytes dealt out to `threads` threads one after the other; -inf behind the last
+template <class T>
+__device__ __forceinline__ void voc_load(const T *l, int count, int threads, float (&v)[VOC_ELEMS]) {
+    constexpr int E = OpPiece<T>::E;
+#pragma unroll
+    for (int i = 0; i < VOC_ELEMS / E; ++i) {
+        const int at = (i * threads + (int)threadIdx.x % threads) * E;
+        if (i * threads * E < count && at + E <= count) {
+            const uint4 u = op_load16(l + at);
+            T e[E];
+            __builtin_memcpy(e, &u, 16);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[i * E + j] = op_float(e[j]) + 0.f;   // (+ 0: -0 and 0 are equal logits)
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[i * E + j] = i * threads * E < count && at + j < count ? op_float(l[at + j]) + 0.f : -INFINITY;
+        }
+    }
+}
+
+// a lane's maximum, and the wave's: NaN where one of its logits is NaN or +inf
+__device__ __forceinline__ float voc_top(const float (&v)[VOC_ELEMS], float &mine) {
+    mine = -INFINITY;
+    int largest = INT32_MIN;   // as whole numbers +inf and positive NaN come behind all others, without a sign negative NaN do
+    unsigned last = 0;
 #pragma unroll
     for (int j = 0; j < VOC_ELEMS; ++j) {
-        const vk_u64 m = __ballot(v[j] >= from);
-        if (m) {
-            const int at = found + __popcll(m & ((1ull << lane) - 1));
-            if (v[j] >= from && at < 64) s_cand[wave][at] = (vk_u64)voc_key(v[j]) << 32 | (unsigned)~(v0 + (j / E) * PASS + tid * E + j % E);
-            found += __popcll(m);
-        }
+        mine = fmaxf(mine, v[j]);
+        largest = max(largest, __float_as_int(v[j]));
+        last = max(last, __float_as_uint(v[j]));
     }
+    const float top = voc_max(mine);
+    return __any(largest >= 0x7F800000 || last > 0xFF800000u) ? NAN : top;
+}
+
+// the wave's sum of e^(v - top), `used` numbers a lane (top: not -inf)
+template <int E>
+__device__ __forceinline__ double voc_sum(const float (&v)[VOC_ELEMS], float top, int used) {
+    double sum = 0.;
+#pragma unroll
+    for (int i = 0; i < VOC_ELEMS / E; ++i)
+        if (i * E < used)
+#pragma unroll
+            for (int j = 0; j < E; ++j) sum += voc_exp(fmax((double)v[i * E + j] - (double)top, -690.));   // (e^-690 for nothing at all: 1e-300)
+    return voc_add(sum);
+}
+
+// A slice's best: as voc_wave_best, with the line drawn by all 256 lane maxima, so that the four waves together collect little more than N.
+// Eight waves a SIMD: a slice's loads wait behind other slices' arithmetic.
+template <class T>
+__global__ void __launch_bounds__(256, 8)
+k_vocab_part(VocabP p) {
+    constexpr int E = OpPiece<T>::E, PASS = 256 * E;
+    __shared__ vk_u64 s_cand[4][64], s_best[4][TBS_MAX_BEAM];
+    __shared__ double s_sum[4];
+    __shared__ float s_top[4];
+    __shared__ int s_found[4];
+    __shared__ __attribute__((aligned(8))) uint16_t s_key[256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.y, split = blockIdx.x;
+    if (p.finished && p.finished[row]) return;   // (nobody reads its lists)
+    const int v0 = split * p.slice, count = min(p.slice, p.vocab - v0), N = p.beams, used = (count + PASS - 1) / PASS * E;
+    auto token = [&](int j, int zero) { return v0 + tid * E + zero + (j / E) * PASS + j % E; };
+    float v[VOC_ELEMS], mine;
+    voc_load((const T *)p.logits + row * p.ld + v0, count, 256, v);
+    float top = voc_top(v, mine);
+    if (lane == 0) s_top[wave] = top;
+    s_key[tid] = (uint16_t)(voc_key(mine) >> 16);
     if (lane < N) s_best[wave][lane] = 0;
-    voc_wave_sync();
-    if (found <= 64) {   // each lane one of them: its rank is the number of larger ones
-        const vk_u64 k = lane < found ? s_cand[wave][lane] : 0;
-        int rank = 0;
-        for (int i = 0; i < found; ++i) rank += s_cand[wave][i] > k;
-        if (lane < found && rank < N) s_best[wave][rank] = k;
-    } else {   // many equal logits: one after the other
-        for (int i = 0; i < N; ++i) {
-            vk_u64 k = 0;
-#pragma unroll
-            for (int j = 0; j < VOC_ELEMS; ++j) {
-                const vk_u64 kj = (vk_u64)voc_key(v[j]) << 32 | (unsigned)~(v0 + (j / E) * PASS + tid * E + j % E);
-                if (v[j] >= from && kj > k && (i == 0 || kj < s_best[wave][i - 1])) k = kj;
-            }
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) k = max(k, voc_shfl_xor(k, x));
-            if (lane == 0) s_best[wave][i] = k;
-            voc_wave_sync();
-        }
-    }
     __syncthreads();
+    unsigned k4[4], least = 0;
+    {
+        const uint2 u = *reinterpret_cast<const uint2 *>(s_key + 4 * lane);
+        k4[0] = u.x & 0xFFFF, k4[1] = u.x >> 16, k4[2] = u.y & 0xFFFF, k4[3] = u.y >> 16;
+    }
+#pragma unroll
+    for (int b = 15; b >= 0; --b) {
+        const unsigned t = least | 1u << b;
+        if (__popcll(__ballot(k4[0] >= t)) + __popcll(__ballot(k4[1] >= t)) + __popcll(__ballot(k4[2] >= t)) + __popcll(__ballot(k4[3] >= t)) >= N) least = t;
+    }
+    const float from = voc_unkey(max(least << 16, voc_key(-INFINITY) + 1));   // (-inf is no candidate)
+    const int found = voc_collect(v, from, used, s_cand[wave], token);
+    if (lane == 0) s_found[wave] = found;
     top = s_top[0];
 #pragma unroll
     for (int i = 1; i < 4; ++i) top = top != top || s_top[i] != s_top[i] ? NAN : fmaxf(top, s_top[i]);
-    double sum = 0.;
-    if (top > -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i)
-            if (i * PASS < count)
-#pragma unroll
-                for (int j = 0; j < E; ++j) sum += voc_exp(fmax((double)v[i * E + j] - (double)top, -690.));   // (e^-690 for nothing at all: 1e-300)
-    }
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+    const double sum = top > -INFINITY ? voc_sum<E>(v, top, used) : 0.;
     if (lane == 0) s_sum[wave] = sum;
-    // the four waves' lists: a key's rank is its place in its own and the larger ones in the others
-    if (lane < N) {
-        const vk_u64 k = s_best[wave][lane];
-        int rank = lane;
+    __syncthreads();
+    const int n[4] = {s_found[0], s_found[1], s_found[2], s_found[3]}, all = n[0] + n[1] + n[2] + n[3];
+    const int64_t list = ((int64_t)row * p.splits + split) * N;
+    auto put = [&](int rank, vk_u64 k) {
+        p.val[list + rank] = k ? voc_unkey((unsigned)(k >> 32)) : -INFINITY;
+        p.tok[list + rank] = (int)~(unsigned)k;
+    };
+    if (all <= 64) {   // (the same for every wave) one of them has a lane each
+        if (wave == 0) {
+            const int w = lane < n[0] ? 0 : lane < n[0] + n[1] ? 1 : lane < n[0] + n[1] + n[2] ? 2 : 3;
+            const vk_u64 k = lane < all ? s_cand[w][lane - (w > 0 ? n[0] : 0) - (w > 1 ? n[1] : 0) - (w > 2 ? n[2] : 0)] : 0;
+            int rank = 0;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) {
-            const vk_u64 *b = s_best[(wave + w) & 3];
-            int lo = 0, hi = N;   // keys before lo are larger, from hi on they are not
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (b[mid] > k || (b[mid] == k && ((wave + w) & 3) < wave)) lo = mid + 1;   // (equal: 0, no candidate)
-                else hi = mid;
-            }
-            rank += lo;
+            for (int i = 0; i < 4; ++i)
+                for (int j = 0; j < n[i]; ++j) rank += s_cand[i][j] > k;
+            if (lane < all && rank < N) put(rank, k);
+            if (lane < N && lane >= all) put(lane, 0);
         }
-        if (rank < N) {
-            const int64_t at = ((int64_t)row * p.splits + split) * N + rank;
-            p.val[at] = k ? voc_unkey((unsigned)(k >> 32)) : -INFINITY;
-            p.tok[at] = (int)~(unsigned)k;
+    } else {
+        voc_wave_slow(v, from, used, N, s_best[wave], token);
+        __syncthreads();
+        // the four waves' lists: a key's rank is its place in its own and the larger ones in the others
+        if (lane < N) {
+            const vk_u64 k = s_best[wave][lane];
+            int rank = lane;
+#pragma unroll
+            for (int w = 1; w < 4; ++w) {
+                const vk_u64 *b = s_best[(wave + w) & 3];
+                int lo = 0, hi = N;   // keys before lo are larger, from hi on they are not
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (b[mid] > k || (b[mid] == k && ((wave + w) & 3) < wave)) lo = mid + 1;   // (equal: 0, no candidate)
+                    else hi = mid;
+                }
+                rank += lo;
+            }
+            if (rank < N) put(rank, k);
         }
     }
-    __syncthreads();
     if (tid == 0) {
         p.sum[row * p.splits + split] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
         p.top[row * p.splits + split] = top;
     }
 }
 
-// the larger of two candidates: by score, the lower row at a tie
-struct VocBest {
-    double score;
-    int row;
-};
-__device__ __forceinline__ VocBest voc_best(VocBest a, VocBest b) { return b.score > a.score || (b.score == a.score && b.row < a.row) ? b : a; }
+// A row's list from its N best keys: scores, tokens (a lane each).  The row has none where its maximum is NaN or -inf.
+__device__ __forceinline__ void voc_row(int lane, int N, const vk_u64 *best, double score, float top, double sum, double *scores, int *tokens) {
+    if (lane >= N) return;
+    const vk_u64 k = best[lane];
+    const double lse = (double)top + log(sum), x = score + ((double)voc_unkey((unsigned)(k >> 32)) - lse);
+    const bool there = k != 0 && top > -INFINITY && x > -INFINITY;
+    scores[lane] = there ? x : -INFINITY;
+    tokens[lane] = there ? (int)~(unsigned)k : -1;
+}
 
+__device__ __forceinline__ void voc_row_finished(int lane, int N, double score, int eos, double *scores, int *tokens) {
+    if (lane >= N) return;
+    scores[lane] = lane == 0 && score > -INFINITY ? score : -INFINITY;
+    tokens[lane] = eos;
+}
+
+// The group's N best of its rows' lists.  An entry's rank is its place in its own list and the better ones in the others, a binary search in each
+// of them (they are sorted; the lower row first at a tie), a thread an entry and another row: the searches' steps wait for LDS, so as many as can
+// run beside each other.
+template <int STRIDE>
+__device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const double (*scores)[STRIDE], const int (*tokens)[STRIDE], int *ranks) {
+    const int N = p.beams, entries = N * N;
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) ranks[i] = i % N;
+    __syncthreads();   // (the lists are complete, too)
+    for (int i = threadIdx.x; i < entries * N; i += blockDim.x) {
+        const int r = i / entries, e = i - r * entries, row = e / N;
+        if (r == row) continue;
+        const double x = scores[row][e - row * N];
+        int lo = 0, hi = N;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const double y = scores[r][mid];
+            if (y > x || (y == x && r < row)) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo > 0) atomicAdd(&ranks[e], lo);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
+        const int rank = ranks[i], row = i / N;
+        if (rank >= N) continue;
+        const double x = scores[row][i - row * N];
+        const bool none = !(x > -INFINITY);
+        const int token = none ? -1 : tokens[row][i - row * N];
+        p.out_scores[r0 + rank] = x;
+        p.out_tokens[r0 + rank] = token;
+        p.out_parents[r0 + rank] = none ? -1 : row;
+        p.out_finished[r0 + rank] = none || token == p.eos || (p.finished && p.finished[r0 + row]);
+    }
+}
+
+// Rows' lists from their slices' (a wave a row), and the group's.
 __global__ void __launch_bounds__(1024)
 k_vocab_join(VocabP p) {
     __shared__ double s_score[TBS_MAX_BEAM][TBS_MAX_BEAM];
     __shared__ int s_token[TBS_MAX_BEAM][TBS_MAX_BEAM];
+    __shared__ vk_u64 s_cand[16][64], s_best[16][TBS_MAX_BEAM];
+    __shared__ int s_rank[TBS_MAX_BEAM * TBS_MAX_BEAM];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, N = p.beams;
     const int64_t r0 = (int64_t)blockIdx.x * N;
     for (int i = wave; i < N; i += waves) {
         const int64_t row = r0 + i;
         const double score = p.scores[row];
         if (p.finished && p.finished[row]) {
-            if (lane < N) {
-                s_score[i][lane] = lane == 0 && score > -INFINITY ? score : -INFINITY;
-                s_token[i][lane] = p.eos;
-            }
+            voc_row_finished(lane, N, score, p.eos, s_score[i], s_token[i]);
             continue;
         }
         const bool in = lane < p.splits;
         const float top = in ? p.top[row * p.splits + lane] : -INFINITY;
-        float best = top;
+        const double part = in ? p.sum[row * p.splits + lane] : 0.;
+        float best = voc_max(top);
+        const double sum = voc_add(top > -INFINITY ? part * exp((double)top - (double)best) : 0.);
+        if (__any(top != top)) best = NAN;
+        // 512 entries of the lists at a time, and the best of those before
+        const int all = p.splits * N;
+        for (int from = 0; from < all; from += 512) {
+            float v[9], mine = -INFINITY;
+            int tok[9];
+            const vk_u64 k = from > 0 && lane < N ? s_best[wave][lane] : 0;
+            v[8] = k ? voc_unkey((unsigned)(k >> 32)) : -INFINITY;
+            tok[8] = (int)~(unsigned)k;
+            const float *val = p.val + row * all + from;
+            const int *token = p.tok + row * all + from;
 #pragma unroll
-        for (int x = 1; x < 64; x <<= 1) best = fmaxf(best, __shfl_xor(best, x));
-        double sum = in && top > -INFINITY ? p.sum[row * p.splits + lane] * exp((double)top - (double)best) : 0.;
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
-        const bool none = __any(top != top) || best == -INFINITY;
-        const double lse = (double)best + log(sum);
-        // the slices' lists, a lane each: whoever has the largest logit (the lower slice at a tie: its tokens come first) goes on to its next
-        int at = 0;
-        const int64_t base = (row * p.splits + lane) * N;
-        float v = in ? p.val[base] : -INFINITY;
-        for (int k = 0; k < N; ++k) {
-            float m = v;
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-            const int from = __ffsll((long long)__ballot(v == m)) - 1;
-            if (lane == from) {
-                const double s = score + ((double)v - lse);
-                s_score[i][k] = none || !(s > -INFINITY) ? -INFINITY : s;
-                if (v > -INFINITY) {   // (so it is one of its list)
-                    s_token[i][k] = p.tok[base + at];
-                    ++at;
-                    v = at < N ? p.val[base + at] : -INFINITY;
-                }
+            for (int j = 0; j < 8; ++j) {
+                const int at = j * 64 + lane;
+                v[j] = from + at < all ? val[at] : -INFINITY;
+                tok[j] = from + at < all ? token[at] : 0;
             }
-        }
-    }
-    __syncthreads();
-    if (wave > 0) return;
-    int at = 0;
-    VocBest b = {lane < N ? s_score[lane][0] : -INFINITY, lane};
-    for (int k = 0; k < N; ++k) {
-        VocBest m = b;
 #pragma unroll
-        for (int x = 1; x < 64; x <<= 1) m = voc_best(m, VocBest{__shfl_xor(m.score, x), __shfl_xor(m.row, x)});
-        if (lane == m.row) {
-            const bool none = !(m.score > -INFINITY);
-            const int token = none ? -1 : s_token[lane][at];
-            p.out_scores[r0 + k] = m.score;
-            p.out_tokens[r0 + k] = token;
-            p.out_parents[r0 + k] = none ? -1 : lane;
-            p.out_finished[r0 + k] = none || token == p.eos || (p.finished && p.finished[r0 + lane]);
-            if (!none) {
-                ++at;
-                b.score = at < N ? s_score[lane][at] : -INFINITY;
-            }
+            for (int j = 0; j < 9; ++j) mine = fmaxf(mine, v[j]);
+            voc_wave_best(v, mine, 9, N, s_cand[wave], s_best[wave], [&](int j, int) { return tok[j]; });
         }
+        voc_row(lane, N, s_best[wave], score, best, sum, s_score[i], s_token[i]);
+        voc_wave_sync();
     }
+    voc_group(p, r0, s_score, s_token, s_rank);
+}
+
+// Vocabularies of up to 2048 and groups of up to 16: one launch, a workgroup a group, a wave a row.
+template <class T>
+__global__ void __launch_bounds__(1024)
+k_vocab_small(VocabP p) {
+    constexpr int E = OpPiece<T>::E, PASS = 64 * E;
+    __shared__ double s_score[16][16];
+    __shared__ int s_token[16][16];
+    __shared__ vk_u64 s_cand[16][64], s_best[16][16];
+    __shared__ int s_rank[16 * 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = p.beams;
+    const int64_t r0 = (int64_t)blockIdx.x * N, row = r0 + wave;
+    const double score = p.scores[row];
+    if (p.finished && p.finished[row]) {
+        voc_row_finished(lane, N, score, p.eos, s_score[wave], s_token[wave]);
+    } else {
+        const int used = (p.vocab + PASS - 1) / PASS * E;
+        float v[VOC_ELEMS], mine;
+        voc_load((const T *)p.logits + row * p.ld, p.vocab, 64, v);
+        const float top = voc_top(v, mine);
+        voc_wave_best(v, mine, used, N, s_cand[wave], s_best[wave], [&](int j, int zero) { return lane * E + zero + (j / E) * PASS + j % E; });
+        const double sum = top > -INFINITY ? voc_sum<E>(v, top, used) : 0.;
+        voc_row(lane, N, s_best[wave], score, top, sum, s_score[wave], s_token[wave]);
+    }
+    voc_group(p, r0, s_score, s_token, s_rank);
 }
 
 struct VocabPlan {
     int splits, slice;
+    bool small;
 };
 
 static VocabPlan vocab_plan(const tbs_beam_select_args &a) {
@@ -274,6 +427,7 @@ static VocabPlan vocab_plan(const tbs_beam_select_args &a) {
     if (splits < more) splits = more;
     const int pass = 256 * (int)(16 / op_dtype_size(a.dtype));
     VocabPlan pl;
+    pl.small = a.vocab <= VOC_SMALL && a.beams <= 16;
     pl.slice = (int)((a.vocab + splits - 1) / splits + pass - 1) / pass * pass;
     pl.splits = (a.vocab + pl.slice - 1) / pl.slice;
     return pl;
@@ -294,7 +448,9 @@ static int64_t vocab_bytes(const tbs_beam_select_args &a, const VocabPlan &pl) {
 
 extern "C" int64_t tbs_beam_select_workspace(const tbs_beam_select_args *args) {
     if (!args || vocab_check(*args) != TBS_OK) return TBS_EINVAL;
-    return args->rows == 0 ? 0 : vocab_bytes(*args, vocab_plan(*args));
+    if (args->rows == 0) return 0;
+    const VocabPlan pl = vocab_plan(*args);
+    return pl.small ? 0 : vocab_bytes(*args, pl);
 }
 
 extern "C" int tbs_beam_select(const tbs_beam_select_args *args, void *stream) {
@@ -306,7 +462,7 @@ extern "C" int tbs_beam_select(const tbs_beam_select_args *args, void *stream) {
         (uintptr_t)a.logits % op_dtype_size(a.dtype))
         return TBS_EINVAL;
     const VocabPlan pl = vocab_plan(a);
-    if (!a.workspace || a.workspace_bytes < vocab_bytes(a, pl) || (uintptr_t)a.workspace % 16) return TBS_EINVAL;
+    if (!pl.small && (!a.workspace || a.workspace_bytes < vocab_bytes(a, pl) || (uintptr_t)a.workspace % 16)) return TBS_EINVAL;
     VocabP p = {};
     p.logits = a.logits, p.scores = a.scores, p.finished = a.finished;
     p.out_scores = a.out_scores, p.out_tokens = a.out_tokens, p.out_parents = a.out_parents, p.out_finished = a.out_finished;
@@ -318,6 +474,13 @@ extern "C" int tbs_beam_select(const tbs_beam_select_args *args, void *stream) {
     p.ld = a.ld_logits;
     p.rows = a.rows, p.beams = a.beams, p.vocab = a.vocab, p.eos = a.eos, p.splits = pl.splits, p.slice = pl.slice;
     const hipStream_t st = (hipStream_t)stream;
+    if (pl.small) {
+        const dim3 groups(a.rows / a.beams), block(64 * a.beams);
+        if (a.dtype == TBS_F32) hipLaunchKernelGGL((k_vocab_small<float>), groups, block, 0, st, p);
+        else if (a.dtype == TBS_BF16) hipLaunchKernelGGL((k_vocab_small<__bf16>), groups, block, 0, st, p);
+        else hipLaunchKernelGGL((k_vocab_small<_Float16>), groups, block, 0, st, p);
+        return hipGetLastError() == hipSuccess ? TBS_OK : TBS_EHIP;
+    }
     const dim3 grid(pl.splits, a.rows);
     if (a.dtype == TBS_F32) hipLaunchKernelGGL((k_vocab_part<float>), grid, dim3(256), 0, st, p);
     else if (a.dtype == TBS_BF16) hipLaunchKernelGGL((k_vocab_part<__bf16>), grid, dim3(256), 0, st, p);

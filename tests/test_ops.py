@@ -438,7 +438,7 @@ def _select_check(logits, scores, finished, beams, eos, stride=None, shift=0):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("groups,beams,vocab", [(1, 1, 1), (1, 1, 2), (3, 2, 3), (1, 5, 3), (2, 7, 2), (2, 5, 32), (4, 1, 1000), (3, 5, 1024), (2, 10, 1025), (1, 32, 31), (2, 32, 4096),
-                                                (2, 16, 8191), (2, 5, 8192), (2, 5, 8193), (1, 4, 50257), (40, 8, 9000), (1, 3, 262144), (130, 5, 700), (1, 32, 524288)])
+                                                (2, 16, 8191), (2, 16, 2048), (1, 17, 2048), (2, 16, 2049), (1, 1, 2047), (3, 16, 5), (2, 5, 8192), (2, 5, 8193), (1, 4, 50257), (40, 8, 9000), (1, 3, 262144), (130, 5, 700), (1, 32, 524288)])
 def test_select_sizes(groups, beams, vocab, dtype):
     g = _gen(groups + beams + vocab)
     rows = groups * beams
@@ -450,7 +450,7 @@ def test_select_equal_logits_and_scores(dtype):
     """All logits equal, a few values only, equal rows with equal scores: the lower row, then the lower token."""
     g = _gen(4)
     zero = torch.zeros(12, dtype=torch.float64)
-    for vocab in (5, 300, 5000, 20000):
+    for vocab in (5, 300, 2048, 5000, 20000, 100000):
         _select_check(torch.full((12, vocab), 1.5, dtype=dtype), zero, None, 6, 0)
         _select_check(torch.randint(0, 3, (12, vocab), generator=g).to(dtype), zero - torch.arange(12), None, 6, 1)
         one = _randn(g, 1, vocab, dtype=dtype)

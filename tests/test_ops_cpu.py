@@ -76,7 +76,8 @@ def _select(ops, **kw):
 
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(scores=None), dict(out_scores=None), dict(out_tokens=None), dict(out_parents=None),
-                                 dict(out_finished=None), dict(workspace=None), dict(workspace_bytes=64), dict(workspace=P + 4), dict(ld_logits=999),
+                                 dict(out_finished=None), dict(workspace=None, vocab=4000, ld_logits=4000), dict(workspace_bytes=64, vocab=4000, ld_logits=4000),
+                                 dict(workspace=P + 4, vocab=4000, ld_logits=4000), dict(ld_logits=999),
                                  dict(rows=-5), dict(rows=11), dict(rows=65540), dict(beams=0), dict(beams=33, rows=33), dict(vocab=0), dict(vocab=524289, ld_logits=524289),
                                  dict(dtype=3), dict(logits=P + 2)])
 def test_select_refuses(bad):
@@ -88,6 +89,8 @@ def test_select_of_no_rows():
     L, ops = _ops()
     assert L.tbs_beam_select(C.byref(_select(ops, rows=0)), None) == 0
     assert L.tbs_beam_select_workspace(C.byref(_select(ops, rows=0))) == 0
+    assert L.tbs_beam_select_workspace(C.byref(_select(ops))) == 0                      # a vocabulary of 1000 needs none
+    assert L.tbs_beam_select_workspace(C.byref(_select(ops, vocab=4000, ld_logits=4000))) > 0
     assert L.tbs_beam_select(None, None) == -1 and L.tbs_beam_select_workspace(None) == -1
 
 
