@@ -42,8 +42,18 @@ k_pages_reorder(PagesP p) {
     for (int k = __popc(need & ((1u << c) - 1)); k > 0; --k) left &= left - 1;
     const int giver = is_first ? mine : __ffs(left) - 1;
     const int L = mine >= 0 ? __shfl(len, max(mine, 0)) : 0, full = L / p.page;
+    // The giver's own pages begin behind its whole ones.  Where it has more of these than the child keeps of its parent's, those in between are free only if
+    // the giver alone names them.
+    const int given = __shfl(len, giver) / p.page;
     bool drop = false;
-    if (mine >= 0 && !is_first) drop = __shfl(len, giver) / p.page > full;
+    if (mine >= 0 && !is_first && given > full) {   // (the same for the whole workgroup)
+        int shared = 0;
+        for (int i = threadIdx.x; i < (given - full) * N; i += 256) {
+            const int col = full + i / N, other = i % N;
+            shared |= col < p.width && other != giver && p.tables[(int64_t)(r0 + other) * p.ld + col] == p.tables[(int64_t)(r0 + giver) * p.ld + col];
+        }
+        drop = __syncthreads_or(shared);
+    }
     const int *from = p.tables + (int64_t)(r0 + max(mine, 0)) * p.ld, *own = p.tables + (int64_t)(r0 + giver) * p.ld;
     if (writer) {
         const int whole = mine >= 0 && !drop ? full : 0;

@@ -105,6 +105,6 @@ def beam_reorder(parents, tables, lens, caches, *, beams, finished=None, appende
     parents and finished are beam_select's; tables int32 [rows, table width] and lens int32 [rows] the ones this step ran with; caches the key and
     value caches [pages, page, kv_heads, dim] of every layer (a list of tensors alike in shape, strides and type, or one tensor with
     their number in front).  Full pages are shared, not copied.  `appended`: the step wrote a token per row that took part.  `status`
-    (int32, one number) counts hypotheses that had to be dropped, which include/tbs.h says how to rule out.
+    (int32, one number) counts hypotheses that had to be dropped; include/tbs.h says when.
     """
     return (_binding or _load()).beam_reorder(parents, tables, lens, caches, beams, finished, appended, status)

@@ -532,7 +532,7 @@ def _reorder_ref(parents, tables, lens, finished, caches, beams, page, appended=
                 if p < 0:
                     continue
                 whole = now[g + p] // page
-                if now[g + q] // page > whole:
+                if any(tables[g + r, j] == tables[g + q, j] for j in range(whole, min(now[g + q] // page, width)) for r in range(beams) if r != q):
                     drop += 1
                     continue
                 t[g + c, :whole] = tables[g + p, :whole]
@@ -546,12 +546,15 @@ def _reorder_ref(parents, tables, lens, finished, caches, beams, page, appended=
     return t, n, caches, drop
 
 
-def _reorder_check(parents, lens, *, beams, page, width, kv=2, dim=16, dtype=torch.float32, layers=2, finished=None, appended=True, layout="token", seed=0):
+def _reorder_check(parents, lens, *, beams, page, width, kv=2, dim=16, dtype=torch.float32, layers=2, finished=None, appended=True, layout="token", seed=0, same=()):
+    """same: (row, other, n): the first n pages of `row` are those of `other`."""
     from paper_2302_14357_amd import beam_reorder
     g, r = _gen(seed), np.random.default_rng(seed)
     parents, lens = np.asarray(parents, np.int32), np.asarray(lens, np.int32)
     rows = len(parents)
     tables = r.permutation(rows * width).reshape(rows, width).astype(np.int32)
+    for row, other, n in same:
+        tables[row, :n] = tables[other, :n]
     caches = [_randn(g, rows * width, page, kv, dim, dtype=dtype) for _ in range(2 * layers)]
     on = [c.cuda() for c in caches]
     if layout == "head":
@@ -590,8 +593,12 @@ def test_reorder_finished_absent_and_full():
     # the table is full: nothing was appended, nothing is copied
     assert _reorder_check([0, 0, 1], [16, 16, 16], beams=3, page=8, width=2) == 0
     assert _reorder_check([0, 0, 1], [2**31 - 1, 16, ~(2**31 - 1)], beams=3, page=8, width=2) == 0
-    # a row with two children that is shorter than the one without: that place is dropped
-    assert _reorder_check([0, 0, 1], [3, 3, 30], beams=3, page=8, width=5) == 1
+    # a row with two children that is shorter than the one without, whose pages are its own; shares them with another up to there; beyond that: dropped
+    assert _reorder_check([0, 0, 1], [3, 3, 30], beams=3, page=8, width=5) == 0
+    assert _reorder_check([0, 0, 1], [11, 30, 30], beams=3, page=8, width=5, same=[(2, 1, 1)]) == 0
+    assert _reorder_check([0, 0, 1], [11, 30, 30], beams=3, page=8, width=5, same=[(2, 1, 2)]) == 1
+    assert _reorder_check([1, 1, 1, 2], [30, 4, 12, 19], beams=4, page=8, width=5, same=[(3, 0, 1)]) == 2   # (both rows that give pages name the first)
+    assert _reorder_check([0, 0, 0, 0], [0, 39, 39, 39], beams=4, page=8, width=5, same=[(2, 1, 3)]) == 2
 
 
 def test_reorder_many_caches():
