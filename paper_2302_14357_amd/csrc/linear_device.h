@@ -134,6 +134,29 @@ k_linear_any(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int
     }
 }
 
+// The 8 XCDs (workgroup id modulo 8) form a grid of gm x 8 / gm rectangles of tiles, each tm x tn of them, so that an XCD's L2 fetches a part of each operand
+// instead of all of both.
+struct LinearXcd {
+    int gm, tm, tn;
+};
+__device__ __forceinline__ bool linear_tile_of(const LinearXcd &g, int tiles_m, int tiles_n, int &m, int &n) {
+    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3, jn = j / g.tm, gn = 8 / g.gm;
+    m = xcd / gn * g.tm + j - jn * g.tm;
+    n = xcd % gn * g.tn + jn;
+    return jn < g.tn && m < tiles_m && n < tiles_n;
+}
+// (host) the grid for which an XCD reads the fewest rows of both operands
+static LinearXcd linear_xcds(int64_t tiles_m, int64_t tiles_n, int rows_m, int rows_n) {
+    LinearXcd best = {1, 1, 1};
+    int64_t least = INT64_MAX;
+    for (int gm = 1; gm <= 8; gm *= 2) {
+        const int64_t tm = (tiles_m + gm - 1) / gm, tn = (tiles_n + 8 / gm - 1) / (8 / gm);
+        const int64_t rows = (tm * rows_m + tn * rows_n) * ((tm * tn * 8 + 255) / 256);   // (and no more turns of the chip than it takes)
+        if (rows < least) least = rows, best = {gm, (int)tm, (int)tn};
+    }
+    return best;
+}
+
 // Few rows: a workgroup of eight waves makes 16 TM x 16 TN outputs, each wave over its share of K, from registers alone: a wave asks for
 // LINEAR_U steps of four pieces of every row at once (256 bytes of a row side by side; eight waves 2 KB), and its matrix instructions take
 // them as they come.  The shares meet in LDS at the end.  What bounds it is how many bytes of the weights are on their way; any strides,
@@ -142,12 +165,14 @@ k_linear_any(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int
 #define LINEAR_U 4
 template <class T, class TO, int TM, int TN>
 __global__ void __launch_bounds__(64 * LINEAR_WAVES)
-k_linear_few(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k, int tiles_m, LinearEp ep) {
+k_linear_few(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k, LinearXcd grid, LinearEp ep) {
     constexpr int E = OpPiece<T>::E, STEP = 4 * E, CHUNK = LINEAR_U * STEP;
     __shared__ floatx4 s_acc[LINEAR_WAVES][TM * TN][64];
     static_assert(TM * TN <= LINEAR_WAVES, "a wave finishes a block of 16 x 16");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
-    const int m0 = (int)(blockIdx.x % tiles_m) * 16 * TM, n0 = (int)(blockIdx.x / tiles_m) * 16 * TN;
+    int tile_m, tile_n;
+    if (!linear_tile_of(grid, (m + 16 * TM - 1) / (16 * TM), (n + 16 * TN - 1) / (16 * TN), tile_m, tile_n)) return;   // before any barrier
+    const int m0 = tile_m * 16 * TM, n0 = tile_n * 16 * TN;
     const T *px[TM], *pw[TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i) px[i] = x + min(m0 + i * 16 + fr, m - 1) * ld_x + fq * E;
@@ -255,15 +280,13 @@ __device__ __forceinline__ void lt_wave_sync() {
 
 template <class T, class TO, int TM, int TN, int NS>
 __global__ void __launch_bounds__(512, 2)
-k_linear_tile(const char *__restrict__ x, const char *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k_bytes, LinearEp ep) {
+k_linear_tile(const char *__restrict__ x, const char *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k_bytes, LinearXcd grid, LinearEp ep) {
     constexpr int BM = 32 * TM, BN = 64 * TN, RA = BM / 64, RB = BN / 64, STAGE = (BM + BN) * LT_ROW;
     extern __shared__ __attribute__((aligned(16))) char lt_smem[];   // NS stages
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
     const int tiles_m = (m + BM - 1) / BM, tiles_n = (n + BN - 1) / BN;
-    // the 8 XCDs (workgroup id modulo 8) form a 2 x 4 grid over the tiles: each XCD's L2 fetches half of x and a quarter of w
-    const int tmx = (tiles_m + 1) >> 1, tnx = (tiles_n + 3) >> 2, xcd = blockIdx.x & 7, j0 = blockIdx.x >> 3, jn = j0 / tmx;
-    const int tile_m = (xcd >> 2) * tmx + j0 - jn * tmx, tile_n = (xcd & 3) * tnx + jn;
-    if (jn >= tnx || tile_m >= tiles_m || tile_n >= tiles_n) return;   // before any barrier
+    int tile_m, tile_n;
+    if (!linear_tile_of(grid, tiles_m, tiles_n, tile_m, tile_n)) return;   // before any barrier
     const int kt_n = (k_bytes + LT_ROW - 1) / LT_ROW;
     // a pass: 64 rows, eight a wave; position lane % 8 of its row receives piece position ^ (row / 2 % 8)
     const int lrow = wave * 8 + (lane >> 3), lch = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;
@@ -385,17 +408,17 @@ static hipError_t linear_tile_launch(const tbs_linear_args &a, const LinearEp &e
     constexpr int BM = 32 * TM, BN = 64 * TN, SHM = NS * (BM + BN) * LT_ROW;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_linear_tile<T, TO, TM, TN, NS>), hipFuncAttributeMaxDynamicSharedMemorySize, SHM);
     if (e != hipSuccess) return e;
-    const int64_t tmx = (((int64_t)a.m + BM - 1) / BM + 1) / 2, tnx = (((int64_t)a.n + BN - 1) / BN + 3) / 4;
-    hipLaunchKernelGGL((k_linear_tile<T, TO, TM, TN, NS>), dim3((unsigned)(8 * tmx * tnx)), dim3(512), SHM, st, (const char *)a.x, (const char *)a.w, a.ld_x * (int64_t)sizeof(T),
-                       a.ld_w * (int64_t)sizeof(T), a.m, a.n, (int)(a.k * sizeof(T)), ep);
+    const LinearXcd g = linear_xcds(((int64_t)a.m + BM - 1) / BM, ((int64_t)a.n + BN - 1) / BN, BM, BN);
+    hipLaunchKernelGGL((k_linear_tile<T, TO, TM, TN, NS>), dim3((unsigned)(8 * (int64_t)g.tm * g.tn)), dim3(512), SHM, st, (const char *)a.x, (const char *)a.w, a.ld_x * (int64_t)sizeof(T),
+                       a.ld_w * (int64_t)sizeof(T), a.m, a.n, (int)(a.k * sizeof(T)), g, ep);
     return hipGetLastError();
 }
 
 template <class T, class TO, int TM, int TN>
 static hipError_t linear_few_launch(const tbs_linear_args &a, const LinearEp &ep, hipStream_t st) {
-    const int64_t tiles_m = ((int64_t)a.m + 16 * TM - 1) / (16 * TM), tiles_n = ((int64_t)a.n + 16 * TN - 1) / (16 * TN);
-    hipLaunchKernelGGL((k_linear_few<T, TO, TM, TN>), dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * LINEAR_WAVES), 0, st, (const T *)a.x, (const T *)a.w, a.ld_x, a.ld_w, a.m,
-                       a.n, a.k, (int)tiles_m, ep);
+    const LinearXcd g = linear_xcds(((int64_t)a.m + 16 * TM - 1) / (16 * TM), ((int64_t)a.n + 16 * TN - 1) / (16 * TN), 16 * TM, 16 * TN);
+    hipLaunchKernelGGL((k_linear_few<T, TO, TM, TN>), dim3((unsigned)(8 * (int64_t)g.tm * g.tn)), dim3(64 * LINEAR_WAVES), 0, st, (const T *)a.x, (const T *)a.w, a.ld_x, a.ld_w, a.m,
+                       a.n, a.k, g, ep);
     return hipGetLastError();
 }
 
