@@ -157,17 +157,34 @@ static LinearXcd linear_xcds(int64_t tiles_m, int64_t tiles_n, int rows_m, int r
     return best;
 }
 
+#define LINEAR_WAVES 8
+#define LINEAR_U 4
+// The waves' shares of 16 TM x 16 TN outputs meet in LDS, are added up in the waves' order and finished, four columns a thread.
+template <class TO, int TM, int TN>
+__device__ __forceinline__ void linear_shares(const LinearEp &ep, const floatx4 (&acc)[TM][TN], floatx4 *s_acc, int m0, int n0, int m, int n) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) s_acc[(wave * TM * TN + i) * 64 + lane] = acc[i / TN][i % TN];
+    __syncthreads();
+    if (wave >= TM * TN) return;
+    floatx4 t = s_acc[wave * 64 + lane];
+#pragma unroll
+    for (int i = 1; i < LINEAR_WAVES; ++i) t += s_acc[(i * TM * TN + wave) * 64 + lane];
+    const int r = m0 + wave / TN * 16 + fr, c = n0 + wave % TN * 16 + fq * 4;
+    float y[4] = {t[0], t[1], t[2], t[3]}, bias[4];
+    linear_bias(ep, c, n, bias);
+    if (r < m && c < n) linear_finish<TO>(ep, r, c, n, y, bias);
+}
+
 // Few rows: a workgroup of eight waves makes 16 TM x 16 TN outputs, each wave over its share of K, from registers alone: a wave asks for
 // LINEAR_U steps of four pieces of every row at once (256 bytes of a row side by side; eight waves 2 KB), and its matrix instructions take
 // them as they come.  The shares meet in LDS at the end.  What bounds it is how many bytes of the weights are on their way; any strides,
 // alignments and K.
-#define LINEAR_WAVES 8
-#define LINEAR_U 4
 template <class T, class TO, int TM, int TN>
 __global__ void __launch_bounds__(64 * LINEAR_WAVES)
 k_linear_few(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k, LinearXcd grid, LinearEp ep) {
     constexpr int E = OpPiece<T>::E, STEP = 4 * E, CHUNK = LINEAR_U * STEP;
-    __shared__ floatx4 s_acc[LINEAR_WAVES][TM * TN][64];
+    __shared__ floatx4 s_acc[LINEAR_WAVES * TM * TN * 64];
     static_assert(TM * TN <= LINEAR_WAVES, "a wave finishes a block of 16 x 16");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
     int tile_m, tile_n;
@@ -239,19 +256,7 @@ k_linear_few(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = op_mma<T>(b[j], a[i], acc[i][j]);
     }
-    // the waves' shares are added up in their order, four columns a thread
-#pragma unroll
-    for (int i = 0; i < TM * TN; ++i) s_acc[wave][i][lane] = acc[i / TN][i % TN];
-    __syncthreads();
-    if (wave < TM * TN) {
-        floatx4 t = s_acc[0][wave][lane];
-#pragma unroll
-        for (int i = 1; i < LINEAR_WAVES; ++i) t += s_acc[i][wave][lane];
-        const int r = m0 + wave / TN * 16 + fr, c = n0 + wave % TN * 16 + fq * 4;
-        float y[4] = {t[0], t[1], t[2], t[3]}, bias[4];
-        linear_bias(ep, c, n, bias);
-        if (r < m && c < n) linear_finish<TO>(ep, r, c, n, y, bias);
-    }
+    linear_shares<TO, TM, TN>(ep, acc, s_acc, m0, n0, m, n);
 }
 
 // Many rows: one tile of 32 TM x 64 TN outputs a workgroup of eight waves (2 x 4), a wave 16 TM x 16 TN.  Rows of 128 bytes of K (8 pieces,
@@ -276,6 +281,78 @@ __device__ __forceinline__ void lt_wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Few rows on 16-byte boundaries: as k_linear_few, but through LDS, D steps of PB pieces of every row on their way.  A load's neighbouring lanes take neighbouring
+// pieces of a row (PB x 16 bytes together), as the first-level cache wants them; the matrix instructions' lanes, of which neighbours are
+// different rows, get theirs from LDS, each wave from a ring of its own, without barriers.  Piece c of row r lies at c ^ swz(r): sixteen rows' pieces of one
+// place are then all LDS banks once.
+template <class T, class TO, int TM, int TN, int PB, int D>
+__global__ void __launch_bounds__(64 * LINEAR_WAVES)
+k_linear_stream(const char *__restrict__ x, const char *__restrict__ w, int64_t ld_x, int64_t ld_w, int m, int n, int k_bytes, LinearXcd grid, LinearEp ep) {
+    constexpr int STEP = PB * 16, PER = LINEAR_U * 64 / STEP, CHUNK = PER * STEP, R = TM + TN, L = PB / 4;   // bytes; L loads to 16 rows
+    constexpr int BLOCK = 16 * STEP, RING = D * R * BLOCK;
+    static_assert(TM * TN <= LINEAR_WAVES && TM * TN * 1024 <= RING, "a wave finishes a block of 16 x 16; the shares lie in the rings");
+    extern __shared__ __attribute__((aligned(16))) char lt_smem[];   // a ring of D steps for every wave
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
+    int tile_m, tile_n;
+    if (!linear_tile_of(grid, (m + 16 * TM - 1) / (16 * TM), (n + 16 * TN - 1) / (16 * TN), tile_m, tile_n)) return;   // before any barrier
+    const int m0 = tile_m * 16 * TM, n0 = tile_n * 16 * TN;
+    auto swz = [](int r) { return PB == 8 ? (r >> 1) & 7 : (r >> 2) & 3; };
+    const char *p[R][L];   // weights first
+    int piece[L];
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+        const int row = q * (64 / PB) + lane / PB;
+        piece[q] = ((lane % PB) ^ swz(row)) * 16;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) p[j][q] = w + min(n0 + j * 16 + row, n - 1) * ld_w + piece[q];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) p[TN + i][q] = x + min(m0 + i * 16 + row, m - 1) * ld_x + piece[q];
+    }
+    // this wave's steps: those of chunks wave, wave + 8, ...; the last chunk may have fewer
+    const int chunks = (k_bytes + CHUNK - 1) / CHUNK, mine = chunks > wave ? (chunks - wave + LINEAR_WAVES - 1) / LINEAR_WAVES : 0;
+    const int missing = mine > 0 && (chunks - 1) % LINEAR_WAVES == wave ? (int)(((int64_t)chunks * CHUNK - k_bytes) / STEP) : 0, steps = mine * PER - missing;
+    char *ring = lt_smem + wave * RING;
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)ring;
+    int asked = 0, slot_in = 0;
+    auto ask = [&]() {
+        const int at = ((asked / PER) * LINEAR_WAVES + wave) * CHUNK + asked % PER * STEP;
+#pragma unroll
+        for (int q = 0; q < L; ++q) {
+            const bool behind = at + STEP > k_bytes && at + piece[q] >= k_bytes;   // (pieces behind K, in the last step only)
+#pragma unroll
+            for (int r = 0; r < R; ++r) lt_load(behind ? (const char *)&linear_zeros : p[r][q] + at, lds + (slot_in * R + r) * BLOCK + q * 1024);
+        }
+        slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
+        ++asked;
+    };
+#pragma unroll
+    for (int s = 0; s < D; ++s)
+        if (s < steps) ask();
+    floatx4 acc[TM][TN] = {};
+    int slot = 0;
+    for (int s = 0; s < steps; ++s) {
+        if (s + D <= steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * R * L) : "memory");   // this step's have landed; the younger ones may be on their way
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        uint4 f[L][R];
+#pragma unroll
+        for (int h = 0; h < L; ++h)
+#pragma unroll
+            for (int r = 0; r < R; ++r) f[h][r] = *reinterpret_cast<const uint4 *>(ring + (slot * R + r) * BLOCK + fr * STEP + ((h * 4 + fq) ^ swz(fr)) * 16);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and have been read before their place is asked for again
+        __builtin_amdgcn_sched_barrier(0);
+        if (asked < steps) ask();
+        slot = slot + 1 == D ? 0 : slot + 1;
+#pragma unroll
+        for (int h = 0; h < L; ++h)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = op_mma<T>(f[h][j], f[h][TN + i], acc[i][j]);
+    }
+    __syncthreads();   // (the shares lie where the other waves' rings were)
+    linear_shares<TO, TM, TN>(ep, acc, reinterpret_cast<floatx4 *>(lt_smem), m0, n0, m, n);
 }
 
 template <class T, class TO, int TM, int TN, int NS>
@@ -414,6 +491,17 @@ static hipError_t linear_tile_launch(const tbs_linear_args &a, const LinearEp &e
     return hipGetLastError();
 }
 
+template <class T, class TO, int TM, int TN, int PB, int D>
+static hipError_t linear_stream_launch(const tbs_linear_args &a, const LinearEp &ep, hipStream_t st) {
+    constexpr int SHM = LINEAR_WAVES * D * (TM + TN) * PB * 256;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_linear_stream<T, TO, TM, TN, PB, D>), hipFuncAttributeMaxDynamicSharedMemorySize, SHM);
+    if (e != hipSuccess) return e;
+    const LinearXcd g = linear_xcds(((int64_t)a.m + 16 * TM - 1) / (16 * TM), ((int64_t)a.n + 16 * TN - 1) / (16 * TN), 16 * TM, 16 * TN);
+    hipLaunchKernelGGL((k_linear_stream<T, TO, TM, TN, PB, D>), dim3((unsigned)(8 * (int64_t)g.tm * g.tn)), dim3(64 * LINEAR_WAVES), SHM, st, (const char *)a.x, (const char *)a.w,
+                       a.ld_x * (int64_t)sizeof(T), a.ld_w * (int64_t)sizeof(T), a.m, a.n, (int)(a.k * sizeof(T)), g, ep);
+    return hipGetLastError();
+}
+
 template <class T, class TO, int TM, int TN>
 static hipError_t linear_few_launch(const tbs_linear_args &a, const LinearEp &ep, hipStream_t st) {
     const LinearXcd g = linear_xcds(((int64_t)a.m + 16 * TM - 1) / (16 * TM), ((int64_t)a.n + 16 * TN - 1) / (16 * TN), 16 * TM, 16 * TN);
@@ -424,12 +512,15 @@ static hipError_t linear_few_launch(const tbs_linear_args &a, const LinearEp &ep
 
 // Which kernel?  The one whose estimated time is least, in us; K in units of 2048 bytes (1024 numbers of 16 bits), "turns" of the chip's 256
 // CUs.  Fitted to 30 sizes of 1 to 8192 rows, operands in the caches or from memory (us, estimated / measured):
-//   k_linear_few: 3.3, and what a CU's workgroups read at 47 (16 x 16 outputs), 40 (16 x 32, 32 x 16) or 37 bytes a ns (32 x 32, 64 x 32), all
-//     of them at 5.5 TB/s at most: 5 x 2560 x 640 4.2 / 4.5, 16 x 4096 x 4096 9.5 / 10.3, 64 x 4096 x 4096 17.5 / 18, 5 x 32000 x 1024 15 / 14,
-//     float32 (37, 37, 34, 28 bytes a ns) 320 x 512 x 2048 18.7 / 18.5
-//   k_linear_tile (operands at 3.4 TB/s at most: 5 x 32000 x 1024 23 / 24) 64 x 64, two workgroups a CU: 3 + 5.5 K for up to one a CU, else 8 K a turn of 512: 256 x 4096 x 1024 8.5 / 9.4, 1000 x 4096 x 1024 19 / 22
+//   k_linear_stream: 1.3, and for every turn 2 (2.8 where they are more than two) and what a workgroup reads at so many bytes a ns: 100 (16 x 16 outputs), 90 (16 x 32, 32 x 16, 32 x 32),
+//     60 (64 x 32), all of it at 6.5 TB/s at most: 5 x 2560 x 640 3.7 / 4.5, 16 x 4096 x 4096 8.4 / 7.7, 64 x 4096 x 4096 9.1 / 9.3, 320 x 640 x 2560 6.9 / 6.9,
+//     320 x 1024 x 1024 6.6 / 6.4; float32, whose matrix instructions take their time, 60, 45, 38, 30: 320 x 512 x 2048 17.1 / 17.2
+//   k_linear_few: 3.3, and what a CU's workgroups read at 47 (16 x 16) or 37 bytes a ns (32 x 32; float32 37, 34), all of it at 5.5 TB/s at most: its neighbouring
+//     lanes are different rows, which the first-level cache serves 16 bytes at a time; several workgroups a CU, though, and no alignment: 5 x 32000 x 1024 15 / 14
+//   k_linear_tile (operands at 3.4 TB/s at most) 64 x 64, two workgroups a CU: 3 + 5.5 K for up to one a CU, else 8 K a turn of 512: 256 x 4096 x 1024 8.5 / 9.4,
+//     1000 x 4096 x 1024 19 / 22, 64 x 32000 x 1024 22 / 18
 //   128 x 128, two a CU: 12.5 K for one a CU, 18 K + 4 for two: 1000 x 4096 x 1024 15.5 / 16.5, 8000 x 1024 x 4096 79 / 75
-//   192 x 256: 22 K + 6 a turn: 2560 x 4096 x 1024 30 / 30;  256 x 256: 28 K + 9 a turn: 8000 x 4096 x 1024 76 / 83, 8192 x 4096 x 4096 244 / 237
+//   192 x 256: 22 K + 6 a turn: 2560 x 4096 x 1024 30 / 30;  256 x 256: 28 K + 9 a turn: 8000 x 4096 x 1024 76 / 81, 8192 x 4096 x 4096 244 / 237
 //   float32's matrix instructions take their own time: 64 x 64 11 K and 20 K, 128 x 128 32 K and 70 K, 192 x 256 112 K, 256 x 256 137 K
 //   k_linear_any, where the tiles' alignment is missing: 10 K, or 18.5 K for every 1024 tiles (float32 15 and 48)
 struct LinearChoice {
@@ -449,8 +540,13 @@ static LinearChoice linear_choice(const tbs_linear_args &a, int es, bool tiles) 
         const double groups = up(m, 16 * tm) * up(n, 16 * tn), turns = groups < 1024 ? up(groups, 256) : groups / 256;
         consider(kernel, 3.3 + fmax(turns * 16 * (tm + tn) * a.k * es / (rate * 1000), bytes / 5.5e6));
     };
-    few(11, 1, 1, f32 ? 37 : 47), few(12, 1, 2, f32 ? 37 : 40), few(21, 2, 1, f32 ? 37 : 40), few(22, 2, 2, f32 ? 34 : 37), few(42, 4, 2, f32 ? 28 : 37);
+    few(11, 1, 1, f32 ? 37 : 47), few(22, 2, 2, f32 ? 34 : 37);
     if (tiles) {
+        auto stream = [&](int kernel, int tm, int tn, double rate) {
+            const double turns = up(up(m, 16 * tm) * up(n, 16 * tn), 256);
+            consider(kernel, 1.3 + fmax(turns * (16 * (tm + tn) * a.k * es / (rate * 1000) + (turns > 2 ? 2.8 : 2)), bytes / 6.5e6 + 2));
+        };
+        stream(311, 1, 1, f32 ? 60 : 100), stream(312, 1, 2, f32 ? 45 : 90), stream(321, 2, 1, f32 ? 45 : 90), stream(322, 2, 2, f32 ? 38 : 90), stream(342, 4, 2, f32 ? 30 : 60);
         auto two = [&](int kernel, double bm, double bn, double one_a_cu, double two_a_cu, double end) {   // two workgroups a CU
             const double t = up(m, bm) * up(n, bn), whole = floor(t / 512), rest = t - 512 * whole;
             consider(kernel, 3 + fmax(whole * (two_a_cu * K + end) + (rest == 0 ? 0 : (rest <= 256 ? one_a_cu : two_a_cu) * K + (whole ? end : 0)), bytes / 3.4e6));
@@ -466,7 +562,8 @@ static LinearChoice linear_choice(const tbs_linear_args &a, int es, bool tiles) 
     return best;
 }
 
-// kernel: 0 = the choice for the sizes; otherwise that one (10 TM + TN of k_linear_few, 100 + 10 TM + TN of k_linear_tile, 1 = k_linear_any)
+// kernel: 0 = the choice for the sizes; otherwise that one (10 TM + TN of k_linear_few, 300 + that of k_linear_stream, 100 + that of k_linear_tile,
+// 1 = k_linear_any)
 template <class T, class TO>
 static hipError_t linear_run(const tbs_linear_args &a, int kernel, hipStream_t st) {
     const LinearEp ep = {a.bias, a.residual, a.out, a.ld_residual, a.ld_out, a.act};
@@ -476,10 +573,12 @@ static hipError_t linear_run(const tbs_linear_args &a, int kernel, hipStream_t s
     if (kernel >= 100 && !tiles) return hipErrorInvalidValue;
     switch (kernel) {
         case 11: return linear_few_launch<T, TO, 1, 1>(a, ep, st);
-        case 12: return linear_few_launch<T, TO, 1, 2>(a, ep, st);
-        case 21: return linear_few_launch<T, TO, 2, 1>(a, ep, st);
         case 22: return linear_few_launch<T, TO, 2, 2>(a, ep, st);
-        case 42: return linear_few_launch<T, TO, 4, 2>(a, ep, st);
+        case 311: return linear_stream_launch<T, TO, 1, 1, 8, 4>(a, ep, st);
+        case 312: return linear_stream_launch<T, TO, 1, 2, 8, 2>(a, ep, st);
+        case 321: return linear_stream_launch<T, TO, 2, 1, 8, 2>(a, ep, st);
+        case 322: return linear_stream_launch<T, TO, 2, 2, 8, 2>(a, ep, st);
+        case 342: return linear_stream_launch<T, TO, 4, 2, 4, 3>(a, ep, st);
         case 121: return linear_tile_launch<T, TO, 2, 1, 4>(a, ep, st);
         case 142: return linear_tile_launch<T, TO, 4, 2, 2>(a, ep, st);
         case 164: return linear_tile_launch<T, TO, 6, 4, 2>(a, ep, st);

@@ -109,10 +109,10 @@ def _linear_by(kernel, x, w, b, act, r, out):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("kernel", [1, 11, 12, 21, 22, 42, 121, 142, 164, 184])
+@pytest.mark.parametrize("kernel", [1, 11, 22, 311, 312, 321, 322, 342, 121, 142, 164, 184])
 def test_linear_every_kernel(kernel, dtype):
     """One, two, several and more K tiles than a kernel has stages, pieces behind K, one past and one short of whole tiles, one row, and the float32 result."""
-    for m, n, k in [(1, 4, 8), (63, 66, 64), (65, 257, 72), (129, 250, 128), (193, 520, 200), (257, 254, 328), (300, 300, 1032), (30, 515, 640)]:
+    for m, n, k in [(1, 4, 8), (63, 66, 64), (65, 257, 72), (129, 250, 128), (193, 520, 200), (257, 254, 328), (300, 300, 1032), (30, 515, 640), (40, 70, 4104)]:
         for act, odt in (("gelu", dtype), ("none", torch.float32)):
             g = _gen(m + n + k)
             x, w, b, r = _randn(g, m, k, dtype=dtype), _randn(g, n, k, dtype=dtype, scale=1 / math.sqrt(k)), _randn(g, n), _randn(g, m, n, dtype=odt)
@@ -126,7 +126,7 @@ def test_linear_every_kernel(kernel, dtype):
             _close(room[:m], y, loss + 2.0**-24 * y.abs() + _half_step(y, odt) * (1 + 2.0**-10))
 
 
-@pytest.mark.parametrize("kernel", [121, 142, 164, 184])
+@pytest.mark.parametrize("kernel", [121, 142, 164, 184, 311, 322, 342])
 def test_linear_tiles_want_alignment(kernel):
     x, w, b = torch.zeros(70, 72, dtype=torch.bfloat16, device="cuda"), torch.zeros(80, 72, dtype=torch.bfloat16, device="cuda"), torch.zeros(80, device="cuda")
     out = torch.zeros(70, 80, dtype=torch.bfloat16, device="cuda")
