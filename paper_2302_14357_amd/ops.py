@@ -16,6 +16,7 @@ _P, _I32, _I64 = C.c_void_p, C.c_int32, C.c_int64
 _ACTS = {"none": 0, "relu": 1, "tanh": 2, "gelu": 3, "silu": 4}
 
 
+# The C ABI's argument blocks, for callers of libtbs without the binding module.
 class _Linear(C.Structure):
     _fields_ = ([(n, _P) for n in ("x", "w", "bias", "residual", "out")] + [(n, _I64) for n in ("ld_x", "ld_w", "ld_residual", "ld_out")] +
                 [(n, _I32) for n in ("m", "n", "k", "dtype", "out_dtype", "act")])
