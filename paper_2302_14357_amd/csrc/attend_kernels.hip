@@ -17,7 +17,6 @@
 // Hypotheses of one utterance (beams) name the same pages for most of their length.  A workgroup then takes a key head and a piece of the
 // length for all of them: the pages at the piece's head that their tables have in common are read once, with all hypotheses' queries as
 // columns, and behind those each hypothesis' own tokens, which count for its columns alone.
-#define ATT_WAVES 4
 #define ATT_TABLE 1024   // page table entries in LDS at a time, of all hypotheses of a workgroup
 
 struct AttendP {
@@ -75,17 +74,17 @@ struct AttTile {
     unsigned ok;   // bit j: V's token j exists
 };
 
-// DP: dim rounded up to 32, 64, 128 or 256 (PAD: it was not that already); QB: blocks of sixteen queries a wave takes together
-template <class T, int DP, int QB, bool PAD>
-__global__ void __launch_bounds__(64 * ATT_WAVES, 2)
+// DP: dim rounded up to 32, 64, 128 or 256 (PAD: it was not that already); QB: blocks of sixteen queries a wave takes together;
+// NW: waves, of which four write the outputs
+template <class T, int DP, int QB, bool PAD, int NW>
+__global__ void __launch_bounds__(64 * NW, 2)
 k_attend(AttendP p) {
     typedef AttTile<T, DP> Tile;
     constexpr int E = OpPiece<T>::E, NB = Tile::NB, TK = Tile::TK, NV = Tile::NV, KS = Tile::KS, W = Tile::W, WW = Tile::WW;
     constexpr bool LATE = DP > 128;   // (registers for keys and values at the same time are missing: values are asked for when the scores are made)
     __shared__ int s_table[ATT_TABLE + TBS_MAX_BEAM];
-    __shared__ float s_o[ATT_WAVES][4][W][64];
-    static_assert(ATT_WAVES == 4, "a wave writes one of a lane's four rows");
-    __shared__ float s_ml[ATT_WAVES][2][QB * 16];
+    __shared__ float s_o[NW][4][W][64];
+    __shared__ float s_ml[NW][2][QB * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, kg = lane >> 4;
     const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = p.splits - 1 - (int)blockIdx.z, N = p.beams, r0 = (int)blockIdx.y * N;   // (a row's end takes longest: first)
@@ -133,7 +132,7 @@ k_attend(AttendP p) {
     for (int c0 = k0; c0 < k1; c0 += chunk) {
         const int first = att_page(p, c0), c1 = min(k1, c0 + chunk), pages = att_page(p, c1 - 1) - first + 1;
         if (c0 > k0) __syncthreads();
-        for (int b = wave; b < N; b += ATT_WAVES) {
+        for (int b = wave; b < N; b += NW) {
             const int mine = __shfl(n_l, b), have = mine > 0 ? att_page(p, mine - 1) - first + 1 : 0;
             for (int i = lane; i < pages; i += 64) {
                 const int id = p.tables[(r0 + b) * p.ld_tables + first + i];   // (in the table: i < width)
@@ -317,7 +316,7 @@ k_attend(AttendP p) {
         };
         // (No tile ahead: with the next one's loads in front of this one's products the kernel takes 20 to 90 registers more, so fewer waves a SIMD, and
         // was 0 to 20 % slower: 320 rows of up to 400 tokens 29.0 us against 24.0 at two splits, 17.1 against 16.6 at one.)
-        for (int tile = wave; tile < tiles; tile += ATT_WAVES) {
+        for (int tile = wave; tile < tiles; tile += NW) {
             const Where w = place(tile);
             Tile x;
             load_k(x, w);
@@ -346,18 +345,18 @@ k_attend(AttendP p) {
         __syncthreads();
         float top = s_ml[0][0][b * 16 + c];
 #pragma unroll
-        for (int i = 1; i < ATT_WAVES; ++i) top = fmaxf(top, s_ml[i][0][b * 16 + c]);
+        for (int i = 1; i < NW; ++i) top = fmaxf(top, s_ml[i][0][b * 16 + c]);
         float y[W], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < ATT_WAVES; ++j) {
+        for (int j = 0; j < NW; ++j) {
             const float x = s_ml[j][0][b * 16 + c], a = x == top ? 1.f : __builtin_amdgcn_exp2f(x - top);   // (-inf of -inf: nothing there, 1 x 0)
             sum += a * s_ml[j][1][b * 16 + c];
 #pragma unroll
-            for (int i = 0; i < W; ++i) y[i] += a * s_o[j][wave][i][lane];
+            for (int i = 0; i < W; ++i) y[i] += a * s_o[j][wave & 3][i][lane];
         }
-        if (col_row[b] < N) {
+        if (wave < 4 && col_row[b] < N) {
             const int64_t row = r0 + col_row[b];
             const int head = col_head[b], d = (kg * 4 + wave) * W;
             constexpr int G = W < 8 ? W : 8;
@@ -381,7 +380,7 @@ k_attend(AttendP p) {
         }
     }
     if (qblk == 0)   // the new tokens' places in the cache (this launch reads them from k_new and v_new, whoever attends to them)
-        for (int b = wave; b < N; b += ATT_WAVES) {
+        for (int b = wave; b < N; b += NW) {
             const int pos = __shfl(pos_l, b);
             if (pos < k0 || pos >= k1) continue;
             const int i = att_page(p, pos), id = p.tables[(r0 + b) * p.ld_tables + i], off = pos - i * p.page;
@@ -447,28 +446,25 @@ k_attend_join(AttendP p, int threads) {
 // How the work is split: workgroups of a key head, a row or a group of hypotheses and 16 or 32 queries, and over the tokens where those are
 // fewer than the chip holds at once.
 struct AttendPlan {
-    int beams, qb, qblocks, splits, split_len;
+    int beams, qb, qblocks, waves, splits, split_len;
+    double us;   // estimated
 };
 
-// (together: 0 = by the rule below, 1 = row by row, 2 = hypotheses together; piece: 0 = by the rule, else tokens of a piece, in whole steps)
-static AttendPlan attend_plan(const tbs_attend_args &a, int together = 0, int piece = 0) {
+// beams: how many hypotheses a workgroup takes together; piece: 0 = by the rule, else tokens of a piece, in whole steps
+static AttendPlan attend_form(const tbs_attend_args &a, int beams, int piece) {
     const int group = a.heads / a.kv_heads, tile = a.dtype == TBS_F32 ? 16 : 32;
     const int64_t cap = (int64_t)a.table_width * a.page;
     const int64_t longest = a.max_len > 0 && a.max_len < cap ? a.max_len : cap;
     AttendPlan pl;
-    // Hypotheses together where row by row there would be more than 1536 workgroups, or 130 MB to be read (of which what is shared comes from the caches, but
-    // is computed again): us together / row by row, 64 x 8 rows of 40 tokens 13.3 / 24.9, 4 x 8 of 2000 27.9 / 30.9, 16 x 5 of 3000 29 / 57; the other way 16 x 8
-    // of 200 15.5 / 11.4, one utterance's 8 of 1500 20.3 / 11.8.  (Where nothing is shared: 64 x 4 of 500 to 1500 117 / 112.)
-    const int64_t row_bytes = (int64_t)a.rows * a.kv_heads * longest * a.dim * 2 * (int64_t)op_dtype_size(a.dtype);
-    pl.beams = a.beams <= TBS_MAX_BEAM && (together == 2 || (together == 0 && ((int64_t)a.rows * a.kv_heads > 1536 || row_bytes > 130000000))) ? a.beams : 1;
-    const int columns = pl.beams * group;
+    pl.beams = beams;
+    const int columns = beams * group;
     pl.qb = columns > 16 && a.dim <= 128 ? 2 : 1;
     pl.qblocks = (columns + 16 * pl.qb - 1) / (16 * pl.qb);
-    const int64_t units = (int64_t)a.rows / pl.beams * a.kv_heads * pl.qblocks;
-    const int64_t step = ATT_WAVES * tile;   // a tile for every wave
+    const int64_t units = (int64_t)a.rows / beams * a.kv_heads * pl.qblocks;
+    const int64_t step = 4 * tile;   // a tile for each of four waves
     // As many pieces as take the least time, in tokens that a workgroup handles meanwhile (100 a us): turns of the 256 CUs, of a piece and 500 for a
     // workgroup's start and end, and 400 for the join.  (us by pieces: 16 units of 131071 tokens 16 177, 24 215, 32 184, 64 190; 128 units of 3000 2 30, 3 28,
-    // 6 27, 12 33; 256 of up to 4000 1 119, 2 122, 4 117; 512 of 400 1 16.6, 2 24; 16 of 300 1 8.4, 2 10.3.)
+    // 6 27, 12 33; 256 of up to 4000 1 101, 2 118, 4 127; 512 of 400 1 16.6, 2 24; 16 of 300 1 8.4, 2 10.3.)
     const int64_t most = (longest + 2 * step - 1) / (2 * step);
     int64_t splits = 1, least = (units + 255) / 256 * (longest + 500);
     for (int turns = 1; turns <= 4; ++turns) {   // (the pieces that fill so many turns)
@@ -484,7 +480,26 @@ static AttendPlan attend_plan(const tbs_attend_args &a, int together = 0, int pi
     pl.split_len = (int)len;
     pl.splits = (int)((longest + len - 1) / len);
     if (pl.splits < 1) pl.splits = 1;
+    // Hypotheses together, up to two workgroups a CU: eight waves, to have more loads on their way (us with eight / four: 32 x 8 rows of up to 4000 tokens
+    // 101 / 120, 4 x 8 of 2000 25.2 / 28.4, 64 x 8 of 40 15.3 / 16.0; nothing shared, 64 x 4 of 500 to 1500 121 / 117).  More workgroups four (128 x 8 of 200
+    // 39.4 / 36.1), row by row four (4 rows of 131071 183 / 170, 128 of 4000 379 / 374; one of 300 8.1 / 8.7), and where dim leaves room for the sums of no more.
+    pl.waves = beams > 1 && a.dim <= 128 && units * pl.splits <= 512 ? 8 : 4;
+    const double mb = (double)units * longest * a.dim * 2 * (double)op_dtype_size(a.dtype) * 1e-6, join = pl.splits > 1 ? 5 : 0;
+    pl.us = beams == 1 ? 4.5 + 0.0045 * units + (a.dtype == TBS_F32 ? 0.12 : 0.08) * mb + join
+                       : 7.5 + beams * (columns > 16 ? 0.75 : 0.25) + 0.0015 * beams * units + 0.2 * mb + join;
     return pl;
+}
+
+// (together: 0 = by the rule below, 1 = row by row, 2 = hypotheses together)
+static AttendPlan attend_plan(const tbs_attend_args &a, int together = 0, int piece = 0) {
+    const AttendPlan rows = attend_form(a, 1, piece);
+    if (a.beams == 1 || a.beams > TBS_MAX_BEAM || together == 1) return rows;
+    // Hypotheses together where that is estimated to take less time.  Row by row what they share comes from the caches at 12 TB/s (float32's matrix
+    // instructions: 8), but is computed again; together every hypothesis' own end costs, and memory gives 5 TB/s.  us together / row by row, estimated and
+    // measured: 64 x 8 rows of 40 tokens 17, 26; 15.3, 24.8.  16 x 5 of 400 12.3, 12.6; 11.5, 13.5.  8 x 8 of 500 (four queries to a key head) 22.5, 17.3; 21.5, 16.6,
+    // of 1000 25.8, 27.8; 25.2, 25.5.  2 x 16 of 1000 27, 16; 27.4, 18, of 4000 38, 47; 29, 48.  8 x 32 of 200 35, 22; 32, 19.7, of 800 40, 47; 36.6, 45.8.
+    const AttendPlan groups = attend_form(a, a.beams, piece);
+    return together == 2 || groups.us < rows.us ? groups : rows;
 }
 
 static int attend_check(const tbs_attend_args &a) {
@@ -502,19 +517,25 @@ extern "C" int64_t tbs_attend_workspace(const tbs_attend_args *args) {
     return args->rows == 0 ? 0 : attend_bytes(*args, attend_plan(*args));
 }
 
-template <class T, int DP, int QB>
+template <class T, int DP, int QB, int NW>
 static void attend_launch(const AttendP &p, hipStream_t st) {
-    const dim3 grid(p.kv_heads * p.qblocks, p.rows / p.beams, p.splits), block(64 * ATT_WAVES);
-    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_attend<T, DP, QB, true>), grid, block, 0, st, p);
+    const dim3 grid(p.kv_heads * p.qblocks, p.rows / p.beams, p.splits), block(64 * NW);
+    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false, NW>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_attend<T, DP, QB, true, NW>), grid, block, 0, st, p);
+}
+
+template <class T, int QB, int NW>
+static void attend_dims(const AttendP &p, hipStream_t st) {
+    if (p.dim <= 32) attend_launch<T, 32, QB, NW>(p, st);
+    else if (p.dim <= 64) attend_launch<T, 64, QB, NW>(p, st);
+    else attend_launch<T, 128, QB, NW>(p, st);
 }
 
 template <class T>
-static hipError_t attend_run(const AttendP &p, int qb, hipStream_t st) {
-    if (p.dim <= 32) qb == 1 ? attend_launch<T, 32, 1>(p, st) : attend_launch<T, 32, 2>(p, st);
-    else if (p.dim <= 64) qb == 1 ? attend_launch<T, 64, 1>(p, st) : attend_launch<T, 64, 2>(p, st);
-    else if (p.dim <= 128) qb == 1 ? attend_launch<T, 128, 1>(p, st) : attend_launch<T, 128, 2>(p, st);
-    else attend_launch<T, 256, 1>(p, st);
+static hipError_t attend_run(const AttendP &p, int qb, int waves, hipStream_t st) {
+    if (p.dim > 128) attend_launch<T, 256, 1, 4>(p, st);
+    else if (waves == 8) qb == 1 ? attend_dims<T, 1, 8>(p, st) : attend_dims<T, 2, 8>(p, st);
+    else qb == 1 ? attend_dims<T, 1, 4>(p, st) : attend_dims<T, 2, 4>(p, st);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
         int threads = 2;
@@ -568,7 +589,7 @@ static int attend_call(const tbs_attend_args *args, int together, int piece, voi
     p.page_mul = (unsigned)((((uint64_t)1 << (32 + p.page_shift)) / twice) + (p.page_shift ? 1 : 0));
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.dim)) * 1.44269504f;
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = a.dtype == TBS_F32 ? attend_run<float>(p, pl.qb, st) : a.dtype == TBS_BF16 ? attend_run<__bf16>(p, pl.qb, st) : attend_run<_Float16>(p, pl.qb, st);
+    const hipError_t e = a.dtype == TBS_F32 ? attend_run<float>(p, pl.qb, pl.waves, st) : a.dtype == TBS_BF16 ? attend_run<__bf16>(p, pl.qb, pl.waves, st) : attend_run<_Float16>(p, pl.qb, pl.waves, st);
     return e == hipSuccess ? TBS_OK : TBS_EHIP;
 }
 

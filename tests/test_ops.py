@@ -338,6 +338,16 @@ def test_attend_hypotheses_together(heads, kv, dim, page, form, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,dim,beams,groups", [(4, 64, 2, 140), (16, 128, 5, 130), (4, 24, 3, 129)])
+def test_attend_many_groups(heads, dim, beams, groups, dtype):
+    """More groups and key heads than two workgroups a CU: few waves take a group."""
+    lens = np.random.default_rng(groups).integers(0, 70, groups * beams)
+    lens[::7] = ~lens[::7]
+    for form in ((2, 0), (1, 0), None):
+        _attend_case([int(x) for x in lens], form=form, heads=heads, kv=4, dim=dim, page=4, dtype=dtype, beams=beams, shared=6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("form", [(2, 0), (2, 512), (1, 0)])
 def test_attend_more_pages_than_fit_at_a_time(form, dtype):
     """Pages of one token and of three, sixteen hypotheses: their table entries pass through LDS in several turns."""
