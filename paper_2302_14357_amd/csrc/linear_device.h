@@ -577,7 +577,7 @@ static hipError_t linear_run(const tbs_linear_args &a, int kernel, hipStream_t s
         case 311: return linear_stream_launch<T, TO, 1, 1, 8, 4>(a, ep, st);
         case 312: return linear_stream_launch<T, TO, 1, 2, 8, 2>(a, ep, st);
         case 321: return linear_stream_launch<T, TO, 2, 1, 8, 2>(a, ep, st);
-        case 322: return linear_stream_launch<T, TO, 2, 2, 8, 2>(a, ep, st);
+        case 322: return sizeof(T) == 4 ? linear_stream_launch<T, TO, 2, 2, 4, 4>(a, ep, st) : linear_stream_launch<T, TO, 2, 2, 8, 2>(a, ep, st);
         case 342: return linear_stream_launch<T, TO, 4, 2, 4, 3>(a, ep, st);
         case 121: return linear_tile_launch<T, TO, 2, 1, 4>(a, ep, st);
         case 142: return linear_tile_launch<T, TO, 4, 2, 2>(a, ep, st);

@@ -128,10 +128,37 @@ __device__ __forceinline__ int voc_collect(const float (&v)[ELEMS], float from, 
     return found;
 }
 
+// how many of a list's `count` keys are better than k (eight reads of LDS on their way; a list has room for 64)
+__device__ __forceinline__ int voc_rank(const vk_u64 *list, int count, vk_u64 k) {
+    int rank = 0;
+    for (int i = 0; i < count; i += 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rank += i + j < count && list[i + j] > k;
+    return rank;
+}
+
+// the N-th largest of a wave's numbers, `used` a lane, if it is `from` or more
+template <int ELEMS>
+__device__ __forceinline__ float voc_nth(const float (&v)[ELEMS], float from, int used, int N) {
+    unsigned least = 0;
+#pragma unroll 1
+    for (int b = 31; b >= 0; --b) {
+        const unsigned t = least | 1u << b;
+        const float x = voc_unkey(t);   // (no number at all: nothing is as large)
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < ELEMS; ++j)
+            if (j < used) count += __popcll(__ballot(v[j] >= x));
+        if (count >= N) least = t;
+    }
+    return fmaxf(from, voc_unkey(least));
+}
+
 // A wave's N best of `used` numbers a lane, best first, into best[0 .. N) in LDS: keys of (number, the lower token first), 0 where there are fewer
 // above -inf.  At least N lanes have a maximum of `least` or more, so the N best are among the numbers from there on: the N-th
 // largest lane maximum, cut to its first 16 bits (what a bf16 has), found bit by bit.  They are collected, at most 64 of them, and a lane
-// each finds its rank by counting; more of them (many equal logits) are taken one after the other.
+// each finds its rank by counting.  More than 64 are collected from the N-th largest number on, and taken one after the other if they are more than that still (many equal
+// logits).
 template <int ELEMS, class Token>
 __device__ __forceinline__ void voc_wave_best(float (&v)[ELEMS], float mine, int used, int N, vk_u64 *cand, vk_u64 *best, Token token) {
     const int lane = threadIdx.x & 63;
@@ -142,14 +169,17 @@ __device__ __forceinline__ void voc_wave_best(float (&v)[ELEMS], float mine, int
         const unsigned t = least | 1u << b;
         if (__popcll(__ballot(key >= t)) >= N) least = t;
     }
-    const float from = voc_unkey(max(least, voc_key(-INFINITY) + 1));   // (-inf is no candidate)
-    const int found = voc_collect(v, from, used, cand, token);
+    float from = voc_unkey(max(least, voc_key(-INFINITY) + 1));   // (-inf is no candidate)
+    int found = voc_collect(v, from, used, cand, token);
+    if (found > 64) {
+        from = voc_nth(v, from, used, N);
+        found = voc_collect(v, from, used, cand, token);
+    }
     if (lane < N) best[lane] = 0;
     voc_wave_sync();
     if (found <= 64) {
         const vk_u64 k = lane < found ? cand[lane] : 0;
-        int rank = 0;
-        for (int i = 0; i < found; ++i) rank += cand[i] > k;
+        const int rank = voc_rank(cand, found, k);
         if (lane < found && rank < N) best[rank] = k;
         voc_wave_sync();
     } else {
@@ -160,20 +190,34 @@ __device__ __forceinline__ void voc_wave_best(float (&v)[ELEMS], float mine, int
 // `count` logits, pieces of 16 bytes dealt out to `threads` threads one after the other; -inf behind the last
 template <class T>
 __device__ __forceinline__ void voc_load(const T *l, int count, int threads, float (&v)[VOC_ELEMS]) {
-    constexpr int E = OpPiece<T>::E;
+    constexpr int E = OpPiece<T>::E, P = VOC_ELEMS / E;
+    const int mine = (int)threadIdx.x % threads * E;
+    if (count == threads * VOC_ELEMS) {   // the loads leave together
+        uint4 u[P];
 #pragma unroll
-    for (int i = 0; i < VOC_ELEMS / E; ++i) {
-        const int at = (i * threads + (int)threadIdx.x % threads) * E;
-        if (i * threads * E < count && at + E <= count) {
-            const uint4 u = op_load16(l + at);
+        for (int i = 0; i < P; ++i) u[i] = op_load16(l + mine + i * threads * E);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
             T e[E];
-            __builtin_memcpy(e, &u, 16);
+            __builtin_memcpy(e, &u[i], 16);
 #pragma unroll
             for (int j = 0; j < E; ++j) v[i * E + j] = op_float(e[j]) + 0.f;   // (+ 0: -0 and 0 are equal logits)
-        } else {
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[i * E + j] = i * threads * E < count && at + j < count ? op_float(l[at + j]) + 0.f : -INFINITY;
         }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int at = i * threads * E + mine;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (at + E <= count) u = op_load16(l + at);
+        T e[E];
+        __builtin_memcpy(e, &u, 16);
+        if (at < count && at + E > count)
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (at + j < count) e[j] = l[at + j];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[i * E + j] = at + j < count ? op_float(e[j]) + 0.f : -INFINITY;
     }
 }
 
@@ -205,7 +249,9 @@ __device__ __forceinline__ double voc_sum(const float (&v)[VOC_ELEMS], float top
 }
 
 // A slice's best: as voc_wave_best, with the line drawn by all 256 lane maxima, so that the four waves together collect little more than N.
-// Eight waves a SIMD: a slice's loads wait behind other slices' arithmetic.
+// Eight waves a SIMD: a slice's loads wait behind other slices' arithmetic.  (512 rows of 131000 in float32, groups of 16: 78 us, 3.4 TB/s; the float64
+// exponentials, sixteen instructions a logit, keep the vector units busy most of that.  Slices of 4096 100 us; waves that go on through 32768 each with a list
+// of its own 106.)
 template <class T>
 __global__ void __launch_bounds__(256, 8)
 k_vocab_part(VocabP p) {
@@ -305,18 +351,45 @@ __device__ __forceinline__ void voc_row_finished(int lane, int N, double score, 
     tokens[lane] = eos;
 }
 
-// The group's N best of its rows' lists.  An entry's rank is its place in its own list and the better ones in the others, a binary search in each
-// of them (they are sorted; the lower row first at a tie), a thread an entry and another row: the searches' steps wait for LDS, so as many as can
-// run beside each other.
+// The group's N best of its rows' lists.  The entry at place e of a list (sorted, from 0) to which the entries at place e of h others are better (the lower
+// row first at a tie) has h (e + 1) + e better ones at least: only N + N / 2 + N / 3 + ... entries are looked at further, 119 of 1024 for 32.  An entry's rank is its place
+// in its own list and the better ones in the others, a binary search in each of them, a thread an entry and another row: the searches' steps wait
+// for LDS, so as many as can run beside each other.
+struct VocGroup {
+    int count, entry[128], rank[128];
+};
 template <int STRIDE>
-__device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const double (*scores)[STRIDE], const int (*tokens)[STRIDE], int *ranks) {
-    const int N = p.beams, entries = N * N;
-    for (int i = threadIdx.x; i < entries; i += blockDim.x) ranks[i] = i % N;
-    __syncthreads();   // (the lists are complete, too)
-    for (int i = threadIdx.x; i < entries * N; i += blockDim.x) {
-        const int r = i / entries, e = i - r * entries, row = e / N;
+__device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const double (*scores)[STRIDE], const int (*tokens)[STRIDE], VocGroup &g) {
+    const int N = p.beams, tid = threadIdx.x, entries = N * N;
+    const bool all = entries <= 128;   // (looking at all of them took 1 us less of five rows of 32001, 0.7 of ten of 50000; at some, 50 us less of 32 of 131000)
+    if (tid == 0) g.count = all ? entries : 0;
+    if (!all) __syncthreads();   // (the lists are complete, too)
+    for (int i = tid; i < entries; i += blockDim.x) {
+        const int row = i / N, e = i - row * N;
+        if (all) {
+            g.entry[i] = row << 8 | e;
+            g.rank[i] = e;
+            continue;
+        }
+        const double x = scores[row][e];
+        int h = 0;
+#pragma unroll 8
+        for (int r = 0; r < N; ++r) {
+            const double y = scores[r][e];
+            h += y > x || (y == x && r < row);
+        }
+        if (h * (e + 1) + e < N) {
+            const int at = atomicAdd(&g.count, 1);   // (in any order)
+            g.entry[at] = row << 8 | e;
+            g.rank[at] = e;
+        }
+    }
+    __syncthreads();
+    const int count = g.count;
+    for (int i = tid; i < count * N; i += blockDim.x) {
+        const int at = i / N, r = i - at * N, row = g.entry[at] >> 8;
         if (r == row) continue;
-        const double x = scores[row][e - row * N];
+        const double x = scores[row][g.entry[at] & 255];
         int lo = 0, hi = N;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
@@ -324,15 +397,15 @@ __device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const dou
             if (y > x || (y == x && r < row)) lo = mid + 1;
             else hi = mid;
         }
-        if (lo > 0) atomicAdd(&ranks[e], lo);
+        if (lo > 0) atomicAdd(&g.rank[at], lo);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
-        const int rank = ranks[i], row = i / N;
+    for (int i = tid; i < count; i += blockDim.x) {
+        const int rank = g.rank[i], row = g.entry[i] >> 8, e = g.entry[i] & 255;
         if (rank >= N) continue;
-        const double x = scores[row][i - row * N];
+        const double x = scores[row][e];
         const bool none = !(x > -INFINITY);
-        const int token = none ? -1 : tokens[row][i - row * N];
+        const int token = none ? -1 : tokens[row][e];
         p.out_scores[r0 + rank] = x;
         p.out_tokens[r0 + rank] = token;
         p.out_parents[r0 + rank] = none ? -1 : row;
@@ -340,13 +413,14 @@ __device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const dou
     }
 }
 
-// Rows' lists from their slices' (a wave a row), and the group's.
+// Rows' lists from their slices' (a wave a row), and the group's.  (Steps that wait for each other: 5 us for 64 groups of five rows of 32001, 10 for 32 of sixteen rows
+// of 131000.)
 __global__ void __launch_bounds__(1024)
 k_vocab_join(VocabP p) {
     __shared__ double s_score[TBS_MAX_BEAM][TBS_MAX_BEAM];
     __shared__ int s_token[TBS_MAX_BEAM][TBS_MAX_BEAM];
     __shared__ vk_u64 s_cand[16][64], s_best[16][TBS_MAX_BEAM];
-    __shared__ int s_rank[TBS_MAX_BEAM * TBS_MAX_BEAM];
+    __shared__ VocGroup s_group;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, N = p.beams;
     const int64_t r0 = (int64_t)blockIdx.x * N;
     for (int i = wave; i < N; i += waves) {
@@ -364,19 +438,27 @@ k_vocab_join(VocabP p) {
         if (__any(top != top)) best = NAN;
         // 512 entries of the lists at a time, and the best of those before
         const int all = p.splits * N;
+        const float one_n = 1.f / N;
         for (int from = 0; from < all; from += 512) {
             float v[9], mine = -INFINITY;
             int tok[9];
-            const vk_u64 k = from > 0 && lane < N ? s_best[wave][lane] : 0;
+            const vk_u64 k = from > 0 && lane % 2 == 0 && lane / 2 < N ? s_best[wave][lane / 2] : 0;   // (theirs, too)
             v[8] = k ? voc_unkey((unsigned)(k >> 32)) : -INFINITY;
             tok[8] = (int)~(unsigned)k;
-            const float *val = p.val + row * all + from;
-            const int *token = p.tok + row * all + from;
+            const float *val = p.val + row * all;
+            const int *token = p.tok + row * all;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int at = j * 64 + lane;
-                v[j] = from + at < all ? val[at] : -INFINITY;
-                tok[j] = from + at < all ? token[at] : 0;
+                // (lists side by side, each turned by another number of places, so that their best ones are different lanes': every lane's maximum then
+                // says something about where the line is)
+                v[j] = -INFINITY;
+                tok[j] = 0;
+                if (from + j * 64 >= all) continue;
+                const int at = from + j * 64 + lane, list = (int)((at + 0.5f) * one_n), turn = (list * N * N) >> 9;
+                int place = at - list * N + turn - (int)((turn + 0.5f) * one_n) * N;
+                place = list * N + (place >= N ? place - N : place);
+                v[j] = at < all ? val[place] : -INFINITY;
+                tok[j] = at < all ? token[place] : 0;
             }
 #pragma unroll
             for (int j = 0; j < 9; ++j) mine = fmaxf(mine, v[j]);
@@ -385,7 +467,7 @@ k_vocab_join(VocabP p) {
         voc_row(lane, N, s_best[wave], score, best, sum, s_score[i], s_token[i]);
         voc_wave_sync();
     }
-    voc_group(p, r0, s_score, s_token, s_rank);
+    voc_group(p, r0, s_score, s_token, s_group);
 }
 
 // Vocabularies of up to 2048 and groups of up to 16: one launch, a workgroup a group, a wave a row.
@@ -396,7 +478,7 @@ k_vocab_small(VocabP p) {
     __shared__ double s_score[16][16];
     __shared__ int s_token[16][16];
     __shared__ vk_u64 s_cand[16][64], s_best[16][16];
-    __shared__ int s_rank[16 * 16];
+    __shared__ VocGroup s_group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = p.beams;
     const int64_t r0 = (int64_t)blockIdx.x * N, row = r0 + wave;
     const double score = p.scores[row];
@@ -411,7 +493,7 @@ k_vocab_small(VocabP p) {
         const double sum = top > -INFINITY ? voc_sum<E>(v, top, used) : 0.;
         voc_row(lane, N, s_best[wave], score, top, sum, s_score[wave], s_token[wave]);
     }
-    voc_group(p, r0, s_score, s_token, s_rank);
+    voc_group(p, r0, s_score, s_token, s_group);
 }
 
 struct VocabPlan {
@@ -420,7 +502,8 @@ struct VocabPlan {
 };
 
 static VocabPlan vocab_plan(const tbs_beam_select_args &a) {
-    // slices of 8192, smaller ones (2048 at least) while these are fewer than two workgroups a CU
+    // One launch where a wave has a row's logits in registers (five rows of 1024: 7 us a call, by two launches 14.6).  Else slices of 8192, smaller ones (2048 at
+    // least) while these are fewer than two workgroups a CU
     int64_t splits = (a.vocab + VOC_SLICE - 1) / VOC_SLICE, more = 512 / a.rows;
     if (more > (a.vocab + 2047) / 2048) more = (a.vocab + 2047) / 2048;
     if (more > VOC_SPLITS) more = VOC_SPLITS;
