@@ -514,7 +514,7 @@ static hipError_t linear_few_launch(const tbs_linear_args &a, const LinearEp &ep
 // CUs.  Fitted to 30 sizes of 1 to 8192 rows, operands in the caches or from memory (us, estimated / measured):
 //   k_linear_stream: 1.3, and for every turn 2 (2.8 where they are more than two) and what a workgroup reads at so many bytes a ns: 100 (16 x 16 outputs), 90 (16 x 32, 32 x 16, 32 x 32),
 //     60 (64 x 32), all of it at 6.5 TB/s at most: 5 x 2560 x 640 3.7 / 4.5, 16 x 4096 x 4096 8.4 / 7.7, 64 x 4096 x 4096 9.1 / 9.3, 320 x 640 x 2560 6.9 / 6.9,
-//     320 x 1024 x 1024 6.6 / 6.4; float32, whose matrix instructions take their time, 60, 45, 38, 30: 320 x 512 x 2048 17.1 / 17.2
+//     320 x 1024 x 1024 6.6 / 6.4; float32, whose matrix instructions take their time, 60, 45, 40, 30: 320 x 512 x 2048 16.4 / 16.5
 //   k_linear_few: 3.3, and what a CU's workgroups read at 47 (16 x 16) or 37 bytes a ns (32 x 32; float32 37, 34), all of it at 5.5 TB/s at most: its neighbouring
 //     lanes are different rows, which the first-level cache serves 16 bytes at a time; several workgroups a CU, though, and no alignment: 5 x 32000 x 1024 15 / 14
 //   k_linear_tile (operands at 3.4 TB/s at most) 64 x 64, two workgroups a CU: 3 + 5.5 K for up to one a CU, else 8 K a turn of 512: 256 x 4096 x 1024 8.5 / 9.4,
@@ -546,7 +546,7 @@ static LinearChoice linear_choice(const tbs_linear_args &a, int es, bool tiles) 
             const double turns = up(up(m, 16 * tm) * up(n, 16 * tn), 256);
             consider(kernel, 1.3 + fmax(turns * (16 * (tm + tn) * a.k * es / (rate * 1000) + (turns > 2 ? 2.8 : 2)), bytes / 6.5e6 + 2));
         };
-        stream(311, 1, 1, f32 ? 60 : 100), stream(312, 1, 2, f32 ? 45 : 90), stream(321, 2, 1, f32 ? 45 : 90), stream(322, 2, 2, f32 ? 38 : 90), stream(342, 4, 2, f32 ? 30 : 60);
+        stream(311, 1, 1, f32 ? 60 : 100), stream(312, 1, 2, f32 ? 45 : 90), stream(321, 2, 1, f32 ? 45 : 90), stream(322, 2, 2, f32 ? 40 : 90), stream(342, 4, 2, f32 ? 30 : 60);
         auto two = [&](int kernel, double bm, double bn, double one_a_cu, double two_a_cu, double end) {   // two workgroups a CU
             const double t = up(m, bm) * up(n, bn), whole = floor(t / 512), rest = t - 512 * whole;
             consider(kernel, 3 + fmax(whole * (two_a_cu * K + end) + (rest == 0 ? 0 : (rest <= 256 ? one_a_cu : two_a_cu) * K + (whole ? end : 0)), bytes / 3.4e6));
@@ -577,7 +577,9 @@ static hipError_t linear_run(const tbs_linear_args &a, int kernel, hipStream_t s
         case 311: return linear_stream_launch<T, TO, 1, 1, 8, 4>(a, ep, st);
         case 312: return linear_stream_launch<T, TO, 1, 2, 8, 2>(a, ep, st);
         case 321: return linear_stream_launch<T, TO, 2, 1, 8, 2>(a, ep, st);
-        case 322: return sizeof(T) == 4 ? linear_stream_launch<T, TO, 2, 2, 4, 4>(a, ep, st) : linear_stream_launch<T, TO, 2, 2, 8, 2>(a, ep, st);
+        case 322:   // (us by steps of 64 / 128 bytes: float32 320 x 512 x 2048 16.5 / 17.3, 64 x 2048 x 2048 15.8 / 16.7; bf16 64 x 4096 x 4096 12.6 / 9.3)
+            if constexpr (sizeof(T) == 4) return linear_stream_launch<T, TO, 2, 2, 4, 4>(a, ep, st);
+            else return linear_stream_launch<T, TO, 2, 2, 8, 2>(a, ep, st);
         case 342: return linear_stream_launch<T, TO, 4, 2, 4, 3>(a, ep, st);
         case 121: return linear_tile_launch<T, TO, 2, 1, 4>(a, ep, st);
         case 142: return linear_tile_launch<T, TO, 4, 2, 2>(a, ep, st);
