@@ -13,12 +13,12 @@ struct LinearEp {
     int act;
 };
 
-// Error function by the rational approximation 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (absolute
-// error 1.5e-7): for outputs of 16 bits, whose rounding is far larger.
-__device__ __forceinline__ float linear_erf16(float x) {
-    const float a = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return copysignf(1.f - p * __expf(-a * a), x);
+// y (1 + erf(y / sqrt 2)) / 2 = max(y, 0) - |y| (1 - erf(|y| / sqrt 2)) / 2, the complement by the rational approximation 7.1.26 of Abramowitz and Stegun,
+// Handbook of Mathematical Functions (absolute error 1.5e-7): for outputs of 16 bits, whose rounding is far larger.  From 20 on nothing is left of it.
+__device__ __forceinline__ float linear_gelu16(float y) {
+    const float a = fminf(fabsf(y), 20.f), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, a, 1.f));
+    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f);
+    return fmaf(-a * p, __builtin_amdgcn_exp2f(a * a * (-0.5f * 1.44269504f)), y <= 0.f ? 0.f : y);   // (NaN stays)
 }
 
 // ... hyperbolic tangent and logistic function for such outputs: hardware exponential and reciprocal (a few units of float32), near 0, where
@@ -32,19 +32,21 @@ template <int ACT, bool F32>
 __device__ __forceinline__ float linear_act(float y) {
     if constexpr (ACT == TBS_ACT_RELU) return y > 0.f || y != y ? y : 0.f;   // (NaN stays)
     else if constexpr (ACT == TBS_ACT_TANH) return F32 ? tanhf(y) : linear_tanh16(y);
-    else if constexpr (ACT == TBS_ACT_GELU) return 0.5f * y * (1.f + (F32 ? erff(y * 0.70710678f) : linear_erf16(y * 0.70710678f)));
+    else if constexpr (ACT == TBS_ACT_GELU) return F32 ? 0.5f * y * (1.f + erff(y * 0.70710678f)) : linear_gelu16(y);
     else if constexpr (ACT == TBS_ACT_SILU) return F32 ? y / (1.f + expf(-y)) : y * __builtin_amdgcn_rcpf(1.f + __expf(-y));
     else return y;
 }
 
+// The residual of N columns c .. of row `row`, where they are all there (asked for ahead of the arithmetic).
+template <class TO, int N>
+__device__ __forceinline__ void linear_residual(const LinearEp &ep, int64_t row, int c, int n, TO (&r)[N]) {
+    if (ep.residual && c + N <= n) __builtin_memcpy(r, (const TO *)ep.residual + row * ep.ld_r + c, sizeof r);
+}
+
 // N columns c .. of row `row`, some of them perhaps behind the last: activation of sum + bias, residual, one rounding.
 template <class TO, int N>
-__device__ __forceinline__ void linear_finish(const LinearEp &ep, int row, int c, int n, float (&y)[N], const float (&bias)[N]) {
+__device__ __forceinline__ void linear_finish(const LinearEp &ep, int64_t row, int c, int n, float (&y)[N], const float (&bias)[N], const TO (&r)[N]) {
     constexpr bool F32 = sizeof(TO) == 4;
-    TO r[N];
-    const TO *pr = (const TO *)ep.residual + row * ep.ld_r + c;
-    const bool whole = c + N <= n;
-    if (ep.residual && whole) __builtin_memcpy(r, pr, sizeof r);   // (asked for ahead of the arithmetic)
     switch (ep.act) {
 #define LINEAR_EACH(A)                                                                   \
     case A:                                                                              \
@@ -60,12 +62,13 @@ __device__ __forceinline__ void linear_finish(const LinearEp &ep, int row, int c
             for (int q = 0; q < N; ++q) y[q] += bias[q];
     }
     TO *o = (TO *)ep.out + row * ep.ld_o + c;
-    if (whole) {
+    if (c + N <= n) {
         TO v[N];
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = (TO)(ep.residual ? y[q] + op_float(r[q]) : y[q]);
         __builtin_memcpy(o, v, sizeof v);
     } else {
+        const TO *pr = (const TO *)ep.residual + row * ep.ld_r + c;
 #pragma unroll
         for (int q = 0; q < N - 1; ++q)
             if (c + q < n) o[q] = (TO)(ep.residual ? y[q] + op_float(pr[q]) : y[q]);
@@ -129,7 +132,11 @@ k_linear_any(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int
         for (int i = 0; i < 2; ++i) {
             const int r = m0 + wm * 32 + i * 16 + fr;
             float y[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (r < m && c < n) linear_finish<TO>(ep, r, c, n, y, bias);
+            if (r < m && c < n) {
+                TO before[4];
+                linear_residual(ep, r, c, n, before);
+                linear_finish<TO>(ep, r, c, n, y, bias, before);
+            }
         }
     }
 }
@@ -173,7 +180,11 @@ __device__ __forceinline__ void linear_shares(const LinearEp &ep, const floatx4 
     const int r = m0 + wave / TN * 16 + fr, c = n0 + wave % TN * 16 + fq * 4;
     float y[4] = {t[0], t[1], t[2], t[3]}, bias[4];
     linear_bias(ep, c, n, bias);
-    if (r < m && c < n) linear_finish<TO>(ep, r, c, n, y, bias);
+    if (r < m && c < n) {
+        TO before[4];
+        linear_residual(ep, r, c, n, before);
+        linear_finish<TO>(ep, r, c, n, y, bias, before);
+    }
 }
 
 // Few rows: a workgroup of eight waves makes 16 TM x 16 TN outputs, each wave over its share of K, from registers alone: a wave asks for
@@ -453,8 +464,18 @@ k_linear_tile(const char *__restrict__ x, const char *__restrict__ w, int64_t ld
     auto swz = [](int r) { return TN == 4 ? r & 15 : TN == 2 ? (r >> 1) & 7 : (r >> 2) & 3; };
     char *mine = lt_smem + wave * 16 * TH * RL;
     const int col = lane % (2 * TN) * 8, c = tile_n * BN + wn * 16 * TN + col;
+    // Passes of 32 / TN rows, G of them in one turn of the loop; the residual of the next turn's rows is asked for before this turn's arithmetic (8000 x 4096 x 1024 with gelu
+    // and residual 98 us; asked for with its own row 109, eight passes a turn 103).
+    constexpr int PASSES = 16 * TH * TN / 32, G = PASSES % 4 == 0 && sizeof(TO) == 2 ? 4 : PASSES % 2 == 0 ? 2 : 1;
+    const int row0 = tile_m * BM + wm * 16 * TM + lane / (2 * TN);
     float bias[8];
     linear_bias(ep, c, n, bias);
+    TO next[G][8];   // the residual of the next turn's rows
+    auto ask = [&](int row) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) linear_residual(ep, min(row + i * (32 / TN), m - 1), c, n, next[i]);
+    };
+    ask(row0);
     __builtin_amdgcn_s_waitcnt(LT_LDS_READ);
     __builtin_amdgcn_s_barrier();   // every wave has read its last fragments
     asm volatile("" ::: "memory");
@@ -468,13 +489,18 @@ k_linear_tile(const char *__restrict__ x, const char *__restrict__ w, int64_t ld
                     *reinterpret_cast<floatx4 *>(mine + r * RL + ((b * 4 + fq) ^ swz(r)) * 16) = acc[i][b];
                 }
         lt_wave_sync();
-#pragma unroll 4
-        for (int r = lane / (2 * TN); r < 16 * TH; r += 32 / TN) {
-            const floatx4 u = *reinterpret_cast<const floatx4 *>(mine + r * RL + ((col / 4) ^ swz(r)) * 16);
-            const floatx4 v = *reinterpret_cast<const floatx4 *>(mine + r * RL + ((col / 4 + 1) ^ swz(r)) * 16);
-            float y[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-            const int row = tile_m * BM + wm * 16 * TM + h * 16 * TH + r;
-            if (row < m && c < n) linear_finish<TO>(ep, row, c, n, y, bias);
+        for (int g = 0; g < PASSES; g += G) {
+            TO before[G][8];
+            __builtin_memcpy(before, next, sizeof next);
+            ask(row0 + h * 16 * TH + (g + G) * (32 / TN));   // (the turn after a half's last is the next half's first)
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int r = lane / (2 * TN) + (g + i) * (32 / TN), row = row0 + h * 16 * TH + (g + i) * (32 / TN);
+                const floatx4 u = *reinterpret_cast<const floatx4 *>(mine + r * RL + ((col / 4) ^ swz(r)) * 16);
+                const floatx4 v = *reinterpret_cast<const floatx4 *>(mine + r * RL + ((col / 4 + 1) ^ swz(r)) * 16);
+                float y[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+                if (row < m && c < n) linear_finish<TO>(ep, row, c, n, y, bias, before[i]);
+            }
         }
         lt_wave_sync();
     }
