@@ -417,8 +417,8 @@ __device__ __forceinline__ void voc_group(const VocabP &p, int64_t r0, const dou
 // of 131000.)
 __global__ void __launch_bounds__(1024)
 k_vocab_join(VocabP p) {
-    __shared__ double s_score[TBS_MAX_BEAM][TBS_MAX_BEAM];
-    __shared__ int s_token[TBS_MAX_BEAM][TBS_MAX_BEAM];
+    __shared__ double s_score[TBS_MAX_BEAM][TBS_MAX_BEAM + 1];   // (places of one number in neighbouring lists: neighbouring LDS banks)
+    __shared__ int s_token[TBS_MAX_BEAM][TBS_MAX_BEAM + 1];
     __shared__ vk_u64 s_cand[16][64], s_best[16][TBS_MAX_BEAM];
     __shared__ VocGroup s_group;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, N = p.beams;
@@ -475,8 +475,8 @@ template <class T>
 __global__ void __launch_bounds__(1024)
 k_vocab_small(VocabP p) {
     constexpr int E = OpPiece<T>::E, PASS = 64 * E;
-    __shared__ double s_score[16][16];
-    __shared__ int s_token[16][16];
+    __shared__ double s_score[16][17];
+    __shared__ int s_token[16][17];
     __shared__ vk_u64 s_cand[16][64], s_best[16][16];
     __shared__ VocGroup s_group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = p.beams;
