@@ -13,12 +13,14 @@ struct LinearEp {
     int act;
 };
 
-// y (1 + erf(y / sqrt 2)) / 2 = max(y, 0) - |y| (1 - erf(|y| / sqrt 2)) / 2, the complement by the rational approximation 7.1.26 of Abramowitz and Stegun,
-// Handbook of Mathematical Functions (absolute error 1.5e-7): for outputs of 16 bits, whose rounding is far larger.  From 20 on nothing is left of it.
+// y P(y) = max(y, 0) - |y| P(-|y|) with the normal distribution function P, for outputs of 16 bits: log2 P(-a) by the polynomial of degree 8 whose
+// error counts least in a P(-a) (3.8e-8 at most, found by weighted least squares).  It falls without end, so that nothing is left from 20 on.
 __device__ __forceinline__ float linear_gelu16(float y) {
-    const float a = fminf(fabsf(y), 20.f), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, a, 1.f));
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f);
-    return fmaf(-a * p, __builtin_amdgcn_exp2f(a * a * (-0.5f * 1.44269504f)), y <= 0.f ? 0.f : y);   // (NaN stays)
+    const float a = fminf(fabsf(y), 20.f);
+    float p = fmaf(a, -1.7010708006637287e-06f, 2.523491275496781e-05f);
+    p = fmaf(a, fmaf(a, fmaf(a, p, -0.00011534203076735139f), -0.00032064621336758137f), 0.007328657899051905f);
+    p = fmaf(a, fmaf(a, fmaf(a, fmaf(a, p, -0.052709415555000305f), -0.459118127822876f), -1.1511225700378418f), -0.999998927116394f);
+    return fmaf(-a, __builtin_amdgcn_exp2f(p), y <= 0.f ? 0.f : y);   // (NaN stays)
 }
 
 // ... hyperbolic tangent and logistic function for such outputs: hardware exponential and reciprocal (a few units of float32), near 0, where
