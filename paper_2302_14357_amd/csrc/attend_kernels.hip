@@ -75,8 +75,8 @@ struct AttTile {
 };
 
 // DP: dim rounded up to 32, 64, 128 or 256 (PAD: it was not that already); QB: blocks of sixteen queries a wave takes together;
-// NW: waves, of which four write the outputs
-template <class T, int DP, int QB, bool PAD, int NW>
+// NW: waves, of which four write the outputs; GROUP: hypotheses together, otherwise row by row
+template <class T, int DP, int QB, bool PAD, int NW, bool GROUP>
 __global__ void __launch_bounds__(64 * NW, 2)
 k_attend(AttendP p) {
     typedef AttTile<T, DP> Tile;
@@ -87,7 +87,7 @@ k_attend(AttendP p) {
     __shared__ float s_ml[NW][2][QB * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, kg = lane >> 4;
-    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = p.splits - 1 - (int)blockIdx.z, N = p.beams, r0 = (int)blockIdx.y * N;   // (a row's end takes longest: first)
+    const int kvh = (int)blockIdx.x % p.kv_heads, qblk = (int)blockIdx.x / p.kv_heads, split = p.splits - 1 - (int)blockIdx.z, N = GROUP ? p.beams : 1, r0 = (int)blockIdx.y * N;   // (a row's end takes longest: first)
     // hypothesis `lane` of the group: its tokens, and those of them that are in the cache
     int n_l = 0, pos_l = -1;
     if (lane < N) n_l = att_tokens(p, r0 + lane, &pos_l);
@@ -285,11 +285,20 @@ k_attend(AttendP p) {
                     t[j] = __builtin_amdgcn_exp2f(t[j] - base);
                     l[b] += t[j];
                 }
+                // One hypothesis' own tokens add to its own columns only: the others' weights are 0 here, but 0 times a NaN or an infinity of this
+                // one's is not.  (1 % of the time of hypotheses together; row by row there are no others.)
+                auto add = [&](int i, const floatx4 &y) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[b][i][r] = !GROUP || mine ? y[r] : o[b][i][r];
+                };
                 if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                    for (int i = 0; i < W; ++i) {
+                        floatx4 y = o[b][i];
 #pragma unroll
-                        for (int i = 0; i < W; ++i) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][i]), t[r], o[b][i], 0, 0, 0);
+                        for (int r = 0; r < 4; ++r) y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][i]), t[r], y, 0, 0, 0);
+                        add(i, y);
+                    }
                 } else {
                     // A weight goes into the matrix instruction as two numbers of 16 bits, its rounding and what that left out: a weight's
                     // error is then 2^-17 (fp16: 2^-22) instead of 2^-9, and the output's own rounding is all that shows.  (The second half
@@ -308,8 +317,7 @@ k_attend(AttendP p) {
                         const unsigned sel = i & 1 ? 0x07060302u : 0x05040100u;
                         const uint4 a = make_uint4(__builtin_amdgcn_perm(x.v[1][i / 2], x.v[0][i / 2], sel), __builtin_amdgcn_perm(x.v[3][i / 2], x.v[2][i / 2], sel),
                                                    __builtin_amdgcn_perm(x.v[5][i / 2], x.v[4][i / 2], sel), __builtin_amdgcn_perm(x.v[7][i / 2], x.v[6][i / 2], sel));
-                        o[b][i] = op_mma<T>(a, ph, o[b][i]);
-                        o[b][i] = op_mma<T>(a, pl, o[b][i]);
+                        add(i, op_mma<T>(a, pl, op_mma<T>(a, ph, o[b][i])));
                     }
                 }
             }
@@ -517,25 +525,27 @@ extern "C" int64_t tbs_attend_workspace(const tbs_attend_args *args) {
     return args->rows == 0 ? 0 : attend_bytes(*args, attend_plan(*args));
 }
 
-template <class T, int DP, int QB, int NW>
+template <class T, int DP, int QB, int NW, bool GROUP>
 static void attend_launch(const AttendP &p, hipStream_t st) {
     const dim3 grid(p.kv_heads * p.qblocks, p.rows / p.beams, p.splits), block(64 * NW);
-    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false, NW>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_attend<T, DP, QB, true, NW>), grid, block, 0, st, p);
+    if (p.dim == DP) hipLaunchKernelGGL((k_attend<T, DP, QB, false, NW, GROUP>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_attend<T, DP, QB, true, NW, GROUP>), grid, block, 0, st, p);
 }
 
-template <class T, int QB, int NW>
+template <class T, int QB, int NW, bool GROUP>
 static void attend_dims(const AttendP &p, hipStream_t st) {
-    if (p.dim <= 32) attend_launch<T, 32, QB, NW>(p, st);
-    else if (p.dim <= 64) attend_launch<T, 64, QB, NW>(p, st);
-    else attend_launch<T, 128, QB, NW>(p, st);
+    if (p.dim > 128) {   // (one block of queries, four waves: attend_form)
+        if constexpr (QB == 1 && NW == 4) attend_launch<T, 256, 1, 4, GROUP>(p, st);
+    } else if (p.dim <= 32) attend_launch<T, 32, QB, NW, GROUP>(p, st);
+    else if (p.dim <= 64) attend_launch<T, 64, QB, NW, GROUP>(p, st);
+    else attend_launch<T, 128, QB, NW, GROUP>(p, st);
 }
 
 template <class T>
 static hipError_t attend_run(const AttendP &p, int qb, int waves, hipStream_t st) {
-    if (p.dim > 128) attend_launch<T, 256, 1, 4>(p, st);
-    else if (waves == 8) qb == 1 ? attend_dims<T, 1, 8>(p, st) : attend_dims<T, 2, 8>(p, st);
-    else qb == 1 ? attend_dims<T, 1, 4>(p, st) : attend_dims<T, 2, 4>(p, st);
+    if (p.beams == 1) qb == 1 ? attend_dims<T, 1, 4, false>(p, st) : attend_dims<T, 2, 4, false>(p, st);
+    else if (waves == 8) qb == 1 ? attend_dims<T, 1, 8, true>(p, st) : attend_dims<T, 2, 8, true>(p, st);
+    else qb == 1 ? attend_dims<T, 1, 4, true>(p, st) : attend_dims<T, 2, 4, true>(p, st);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
         int threads = 2;

@@ -379,6 +379,41 @@ def test_attend_hypotheses_of_different_lengths_and_partly_shared_pages(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv,dim,page,n", [(8, 8, 64, 16, 200), (32, 4, 128, 32, 500), (4, 2, 40, 7, 90), (4, 2, 256, 16, 150)])
+def test_attend_numbers_that_are_none_are_their_own_hypothesis_business(heads, kv, dim, page, n, dtype):
+    """A NaN or an infinity among one hypothesis' own tokens, its new one or its query: the others' outputs keep their bits, its own are those it has alone."""
+    from paper_2302_14357_amd import attend_paged
+    g, beams, rows, width = _gen(21), 4, 8, n // page + 1
+    tables = np.random.default_rng(3).permutation(rows * width).reshape(rows, width).astype(np.int32)
+    for i in range(0, rows, beams):
+        tables[i:i + beams, :width // 2] = tables[i, :width // 2]
+    k, v = (_randn(g, rows * width, page, kv, dim, dtype=dtype) for _ in range(2))
+    q, kn, vn = (_randn(g, rows, h, dim, dtype=dtype) for h in (heads, kv, kv))
+    td, ln = torch.from_numpy(tables).cuda(), torch.tensor([n, n, n - 3, n] * 2, dtype=torch.int32).cuda()
+    own = [(int(tables[1, t // page]), t % page) for t in (width // 2 * page, n - page - 1, n - 1)]   # row 1's own: the first, one between, the last in the cache
+
+    def run(form, **bad):
+        x = {name: t.cuda().clone() for name, t in dict(q=q, k=k, v=v, kn=kn, vn=vn).items()}
+        for name, (at, value) in bad.items():
+            x[name][at] = value
+        args = (x["q"], x["k"], x["v"], td, ln)
+        if form:
+            return _attend_by(form, *args, x["kn"], x["vn"], beams, None)
+        return attend_paged(*args, k_new=x["kn"], v_new=x["vn"], beams=beams)
+    others = [0, 2, 3, 4, 5, 6, 7]
+    for form in (None, (1, 0), (2, 0), (2, 128)):
+        want = run(form)
+        assert torch.isfinite(want).all()
+        for value in (math.nan, math.inf, -math.inf):
+            for bad in [dict(v=(own[0], value)), dict(v=(own[1], value)), dict(v=(own[2] + (0,), value)), dict(k=(own[1], value)), dict(kn=(1, value)), dict(vn=(1, value)),
+                        dict(vn=((1, kv - 1, dim - 1), value)), dict(q=(1, value)), dict(k=(own[0], value), v=(own[0], value), vn=(1, -value))]:
+                got = run(form, **bad)
+                assert torch.equal(got[others], want[others]), (form, bad)
+                assert torch.equal(torch.isfinite(got[1]), torch.isfinite(run((1, 0), **bad)[1])), (form, bad)
+                assert not torch.isfinite(got[1]).all() or "k" in bad or "kn" in bad
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_attend_large_scores(dtype):
     """Weights of one token alone, of equal scores, and scores whose exponentials would overflow."""
     _attend_case([70, 130, 10], heads=4, kv=2, dim=64, page=16, dtype=dtype, q_scale=30.0)
