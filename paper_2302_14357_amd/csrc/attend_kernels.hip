@@ -58,6 +58,21 @@ __device__ __forceinline__ int att_tokens(const AttendP &p, int r, int *pos) {
     return (int)(len < cap ? len : cap);
 }
 
+// two numbers cut to the first bits that their 16-bit type holds (none of them is above its largest)
+__device__ __forceinline__ void att_first_bits(float a, float b, __bf16 *to) {
+    const unsigned u = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    __builtin_memcpy(to, &u, 4);
+}
+__device__ __forceinline__ void att_first_bits(float a, float b, _Float16 *to) {
+    const auto u = __builtin_amdgcn_cvt_pkrtz(a, b);
+    __builtin_memcpy(to, &u, 4);
+}
+// what weights are made larger by: enough for 16 bits to hold the excess (fp16: of weights from 2^-26 of the row's largest on)
+template <class T>
+struct AttMore {
+    static constexpr float F = sizeof(T) == 4 ? 1.f : __is_same(T, __bf16) ? 1.f + 0x1p-16f : 1.f + 0x1p-11f;
+};
+
 template <int N>
 struct AttWords {
     unsigned w[N];
@@ -300,15 +315,15 @@ k_attend(AttendP p) {
                         add(i, y);
                     }
                 } else {
-                    // A weight goes into the matrix instruction as two numbers of 16 bits, its rounding and what that left out: a weight's
-                    // error is then 2^-17 (fp16: 2^-22) instead of 2^-9, and the output's own rounding is all that shows.  (The second half
-                    // of the products costs no time: memory bounds the kernel.)
+                    // A weight goes into the matrix instruction as two numbers of 16 bits, what its first bits are and what they leave out: a weight's
+                    // error is then 2^-16 (fp16: 2^-21) instead of 2^-9, and the output's own rounding is all that shows.  (The second half
+                    // of the products costs no time: memory bounds the kernel.)  Both are made a little larger together, and the sum of the weights with
+                    // them, so that the second is never 0 or below where the weight is not: times an infinity it would be NaN, not that infinity.
                     T hi[8], lo[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        hi[j] = (T)t[j];
-                        lo[j] = (T)(t[j] - (float)hi[j]);
-                    }
+                    for (int j = 0; j < 8; j += 2) att_first_bits(t[j], t[j + 1], hi + j);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) lo[j] = (T)fmaf(t[j], AttMore<T>::F, -(float)hi[j]);
                     uint4 ph, pl;
                     __builtin_memcpy(&ph, hi, 16);
                     __builtin_memcpy(&pl, lo, 16);
@@ -340,7 +355,7 @@ k_attend(AttendP p) {
         l[b] += __shfl_xor(l[b], 32);
         if (lane < 16) {
             s_ml[wave][0][b * 16 + c] = m[b];
-            s_ml[wave][1][b * 16 + c] = l[b];
+            s_ml[wave][1][b * 16 + c] = l[b] * AttMore<T>::F;
         }
     }
 #pragma unroll

@@ -414,6 +414,31 @@ def test_attend_numbers_that_are_none_are_their_own_hypothesis_business(heads, k
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("beams", [1, 4])
+@pytest.mark.parametrize("n", [0, 1, 31, 32, 300])
+def test_attend_an_infinity_comes_through(n, beams, dtype):
+    """An infinite value of a token that a row attends to makes that dimension infinite, two of both signs or a NaN make it NaN: what the formula gives."""
+    from paper_2302_14357_amd import attend_paged
+    g, rows, heads, kv, dim, page = _gen(31), 4, 4, 2, 64, 16
+    width = n // page + 1
+    tables = torch.arange(rows * width, dtype=torch.int32).view(rows, width)
+    k, v = (_randn(g, rows * width, page, kv, dim, dtype=dtype) for _ in range(2))
+    q, kn, vn = (_randn(g, rows, h, dim, dtype=dtype) for h in (heads, kv, kv))
+    vn[0] = math.inf
+    vn[1, 0, 5], vn[1, 1, 6] = -math.inf, math.nan
+    if n:
+        v[tables[2, 0], 0, 1] = math.inf
+        v[tables[3, (n - 1) // page], (n - 1) % page, :, 7:9] = torch.tensor([math.inf, -math.inf], dtype=dtype)
+        vn[3, 1, 7] = -math.inf
+    got = attend_paged(q.cuda(), k.cuda(), v.cuda(), tables.cuda(), torch.full((rows,), n, dtype=torch.int32).cuda(), k_new=kn.cuda(), v_new=vn.cuda(), beams=beams).cpu()
+    for r in range(rows):
+        keys, vals = (torch.cat([c[tables[r].long()].reshape(-1, kv, dim)[:n], x[r][None]]).double().repeat_interleave(heads // kv, 1) for c, x in ((k, kn), (v, vn)))
+        p = torch.softmax((q[r].double() * keys).sum(2) / math.sqrt(dim), 0)
+        want = (p[:, :, None] * vals).sum(0)
+        assert torch.equal(torch.isnan(got[r]), torch.isnan(want)) and torch.equal(got[r] == math.inf, want == math.inf) and torch.equal(got[r] == -math.inf, want == -math.inf)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_attend_large_scores(dtype):
     """Weights of one token alone, of equal scores, and scores whose exponentials would overflow."""
     _attend_case([70, 130, 10], heads=4, kv=2, dim=64, page=16, dtype=dtype, q_scale=30.0)
