@@ -402,8 +402,8 @@ int64_t tbs_beam_select_workspace(const tbs_beam_select_args *args);
  * copied to the first of them.  So nothing is allocated or freed: a group starts with tables whose rows share nothing (or whole pages
  * at their heads only) and holds the tokens of every hypothesis for good.  What that needs: where a place's parent is shorter, in whole pages,
  * than the row without children that gives its pages, those in between belong to that row alone (hypotheses of one length never come to
- * this, nor do ones of different lengths that shared nothing there).  A place that this does not hold for is dropped (length -1) and
- * counted in *status.
+ * this, nor do ones of different lengths that shared nothing there); where the giver has length -1 it is all pages behind the parent's whole ones, since
+ * what that row shared is not known any more.  A place that this does not hold for is dropped (length -1) and counted in *status.
  * Parents outside 0 .. beams - 1 are places without a hypothesis: length -1 and some row's table.  Otherwise the new length is that of the
  * parent with its appended tokens; with finished[c] its complement ~length: it takes no part in the steps to come. */
 #define TBS_MAX_CACHES 128

@@ -22,12 +22,13 @@ k_pages_reorder(PagesP p) {
     const int N = p.beams, row = blockIdx.x, c = row % N, r0 = row - c, lane = threadIdx.x & 63;
     const bool writer = blockIdx.y == 0 && blockIdx.z == 0;
     // every wave does the same
-    int parent = -1, len = 0;   // of place `lane`; tokens of row `lane` now
+    int parent = -1, len = 0, whole_l = 0;   // of place `lane`; tokens of row `lane` now, and how many pages at its table's head others may name too
     if (lane < N) {
         parent = p.parents[r0 + lane];
         if ((unsigned)parent >= (unsigned)N) parent = -1;
         const int x = p.lens[r0 + lane];
         len = x >= 0 ? min(x, p.width * p.page - p.appended) + p.appended : min(~x, p.width * p.page);   // (no more than a table holds)
+        whole_l = x == -1 ? p.width : len / p.page;   // (a row without a hypothesis has had one perhaps, or a dropped one's place: any of its pages may be shared)
     }
     bool first = parent >= 0;
     unsigned has_child = 0;
@@ -43,14 +44,16 @@ k_pages_reorder(PagesP p) {
     const int giver = is_first ? mine : __ffs(left) - 1;
     const int L = mine >= 0 ? __shfl(len, max(mine, 0)) : 0, full = L / p.page;
     // The giver's own pages begin behind its whole ones.  Where it has more of these than the child keeps of its parent's, those in between are free only if
-    // the giver alone names them.
-    const int given = __shfl(len, giver) / p.page;
+    // the giver alone names them.  (Columns to lanes, rows to waves.  A first step of 64 groups of eight with tables of 256 pages, 24 caches, one
+    // hypothesis a group: 42 us, 25 where all have tokens.)
+    const int given = __shfl(whole_l, giver);
     bool drop = false;
     if (mine >= 0 && !is_first && given > full) {   // (the same for the whole workgroup)
         int shared = 0;
-        for (int i = threadIdx.x; i < (given - full) * N; i += 256) {
-            const int col = full + i / N, other = i % N;
-            shared |= col < p.width && other != giver && p.tables[(int64_t)(r0 + other) * p.ld + col] == p.tables[(int64_t)(r0 + giver) * p.ld + col];
+        for (int col = full + lane; col < min(given, p.width); col += 64) {
+            const int id = p.tables[(int64_t)(r0 + giver) * p.ld + col];   // (an entry that names no page is shared with nobody)
+            for (int other = threadIdx.x >> 6; other < N; other += 4)
+                shared |= other != giver && (unsigned)id < (unsigned)p.pages && p.tables[(int64_t)(r0 + other) * p.ld + col] == id;
         }
         drop = __syncthreads_or(shared);
     }
@@ -143,7 +146,7 @@ extern "C" int tbs_beam_reorder(const tbs_beam_reorder_args *args, void *stream)
     p.out_tables = a.out_tables, p.out_lens = a.out_lens, p.status = a.status;
     p.ld = a.ld_tables, p.ld_out = a.ld_out_tables;
     p.cp = a.cache_page * es, p.ct = a.cache_token * es, p.ch = a.cache_head * es;
-    p.beams = a.beams, p.width = a.table_width, p.pages = a.pages, p.page = a.page, p.heads = a.kv_heads, p.head_bytes = (int)(a.dim * es);
+    p.beams = a.beams, p.width = a.table_width, p.pages = a.n_caches > 0 ? a.pages : INT32_MAX, p.page = a.page, p.heads = a.kv_heads, p.head_bytes = (int)(a.dim * es);
     p.appended = a.appended;
     if (a.n_caches > 0 && p.heads > 1 && p.ch == p.head_bytes && (int64_t)p.heads * p.head_bytes < INT32_MAX / 2) {   // a token's heads side by side: one row
         p.head_bytes *= p.heads;

@@ -671,6 +671,86 @@ def test_reorder_finished_absent_and_full():
     assert _reorder_check([0, 0, 0, 0], [0, 39, 39, 39], beams=4, page=8, width=5, same=[(2, 1, 3)]) == 2
 
 
+def _reorder_many_steps(seed, *, groups, beams, page, steps, absent, heirs, ended=0.05):
+    """Groups of hypotheses of different lengths, step by step with random parents, places that are empty (`absent` of them) and ones that end.  A cache's entries are
+    the tokens themselves; every hypothesis' tokens are kept beside it in a list.  heirs: places of length -1 are parents as well.  Returns (dropped, empty)."""
+    from paper_2302_14357_amd import beam_reorder
+    r = np.random.default_rng(seed)
+    rows, width = groups * beams, 16 // page + -(-steps // page) + 1
+    tables = r.permutation(rows * width).reshape(rows, width).astype(np.int32)
+    lens = np.where(r.random(rows) < 0.2, -1, r.integers(0, 14, rows)).astype(np.int32)
+    cache = torch.full((rows * width, page, 1, 1), -7.0, device="cuda")
+    said, count, status = [[] for _ in range(rows)], 0, torch.zeros(1, dtype=torch.int32, device="cuda")
+    drops = empty = 0
+    for step in range(-1, steps):
+        # tokens to places of their rows: the given ones, then one a step for those that take part
+        new = [(i, t) for i in range(rows) for t in (range(max(lens[i], 0)) if step < 0 else [lens[i]] * int(lens[i] >= 0))]
+        for i, _ in new:
+            count += 1
+            said[i] = said[i] + [count]
+        at = np.array([(tables[i, t // page], t % page) for i, t in new], np.int64).reshape(-1, 2)
+        assert step < 0 or len({tuple(a) for a in at}) == len(at)
+        cache[torch.from_numpy(at[:, 0]), torch.from_numpy(at[:, 1])] = torch.arange(count - len(new) + 1, count + 1, device="cuda")[:, None, None].float()
+        if step < 0:
+            continue
+        parents = np.where(r.random(rows) < absent, -1, r.integers(0, beams, rows)).astype(np.int32)
+        first = np.arange(rows) // beams * beams
+        if not heirs:   # a place whose parent is without a hypothesis has none itself
+            parents[(parents >= 0) & (lens[first + np.maximum(parents, 0)] == -1)] = -1
+        done = r.random(rows) < ended
+        t, n = beam_reorder(torch.from_numpy(parents).cuda(), torch.from_numpy(tables).cuda(), torch.from_numpy(lens).cuda(), [cache], beams=beams,
+                            finished=torch.from_numpy(done).cuda(), status=status)
+        before, tables, lens = lens, t.cpu().numpy(), n.cpu().numpy()
+        said = [list(said[f + p]) if p >= 0 else [] for f, p in zip(first, parents)]
+        lost = [i for i in range(rows) if lens[i] == -1 and parents[i] >= 0 and before[first[i] + parents[i]] != -1]
+        drops, empty = drops + len(lost), empty + int((lens == -1).sum())
+        assert status.item() == drops
+        held = cache.cpu().numpy().reshape(-1, page)
+        for i in range(rows):
+            if parents[i] < 0 or (heirs and before[first[i] + parents[i]] == -1):
+                assert lens[i] == -1
+            if lens[i] == -1:
+                said[i] = []
+                continue
+            k = max(lens[i], ~lens[i])
+            assert k == len(said[i]) and held[tables[i, :-(-k // page)]].reshape(-1)[:k].tolist() == said[i], (step, i)
+            own = set(tables[i, k // page:].tolist())   # what it goes on to write is no other hypothesis'
+            for q in range(first[i], first[i] + beams):
+                assert q == i or lens[q] == -1 or not own & set(tables[q].tolist()), (step, i, q)
+    return drops, empty
+
+
+@pytest.mark.parametrize("absent", [0.0, 0.1, 0.4])
+@pytest.mark.parametrize("beams,page", [(2, 1), (3, 4), (4, 4), (8, 3)])
+def test_reorder_step_by_step_overwrites_nobody(beams, page, absent):
+    """Different lengths, empty places, dropped ones that give their pages on: every hypothesis that is there holds its tokens, and its pages to come are its own."""
+    drops, empty = _reorder_many_steps(beams * 10 + page, groups=60, beams=beams, page=page, steps=20, absent=absent, heirs=False)
+    assert empty > 0 and (drops > 0 or beams == 2 or absent > 0)   # (groups with empty places die out early)
+
+
+def test_reorder_gives_no_page_on_that_another_names():
+    """Two steps: the first leaves a place that is dropped, or empty, with pages that a living hypothesis names; the second must not give them to another."""
+    from paper_2302_14357_amd import beam_reorder
+    for lens, first, second in (([11, 30, 30], [0, 0, 1], [0, 0, 2]), ([20, 20, 9], [0, -1, 2], [0, 2, 2])):
+        page, width = 8, 6
+        tables = np.arange(3 * width).reshape(3, width).astype(np.int32)
+        if first[1] == 0:
+            tables[2, :2] = tables[1, :2]
+        else:
+            tables[1, :2] = tables[0, :2]
+        cache = torch.arange(3 * width * page, device="cuda").float().view(3 * width, page, 1, 1)
+        t, n, status = torch.from_numpy(tables).cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        kept = 1 if first[1] == 0 else 0   # the hypothesis (its row at the start) that both steps keep
+        length = lens[kept]
+        want = cache[t[kept].long()].reshape(-1)[:length].tolist()
+        for parents in (first, second):
+            t, n = beam_reorder(torch.tensor(parents, dtype=torch.int32).cuda(), t, n, [cache], beams=3, status=status)
+        place = 2 if kept == 1 else 0
+        assert n[place].item() == length + 2
+        assert cache[t[place].long()].reshape(-1)[:length].tolist() == want
+        assert n[1 if kept == 1 else 2].item() == -1 or not set(t[1].tolist()) & set(t[place].tolist())
+
+
 def test_reorder_many_caches():
     _reorder_check([0, 0, 1, 1], [5, 5, 9, 9], beams=2, page=4, width=4, layers=70)
 
