@@ -404,8 +404,10 @@ int64_t tbs_beam_select_workspace(const tbs_beam_select_args *args);
  * than the row without children that gives its pages, those in between belong to that row alone (hypotheses of one length never come to
  * this, nor do ones of different lengths that shared nothing there); where the giver has length -1 it is all pages behind the parent's whole ones, since
  * what that row shared is not known any more.  A place that this does not hold for is dropped (length -1) and counted in *status.
- * Parents outside 0 .. beams - 1 are places without a hypothesis: length -1 and some row's table.  Otherwise the new length is that of the
- * parent with its appended tokens; with finished[c] its complement ~length: it takes no part in the steps to come. */
+ * Parents outside 0 .. beams - 1 are places without a hypothesis: length -1 and some row's table.  So are the children of a row of length -1: a place that
+ * is empty or was dropped does not come back by itself.  Otherwise the new length is that of the parent with its appended tokens; with
+ * finished[c] its complement ~length: it takes no part in the steps to come.  A place with a hypothesis that is not finished and length -1 was dropped: its tokens are gone,
+ * and the caller gives it the score -inf before it selects again. */
 #define TBS_MAX_CACHES 128
 typedef struct tbs_beam_reorder_args {
     const int32_t *parents;    /* [rows] places in the group */

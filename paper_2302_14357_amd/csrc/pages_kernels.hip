@@ -22,14 +22,15 @@ k_pages_reorder(PagesP p) {
     const int N = p.beams, row = blockIdx.x, c = row % N, r0 = row - c, lane = threadIdx.x & 63;
     const bool writer = blockIdx.y == 0 && blockIdx.z == 0;
     // every wave does the same
-    int parent = -1, len = 0, whole_l = 0;   // of place `lane`; tokens of row `lane` now, and how many pages at its table's head others may name too
+    int parent = -1, was = 0, len = 0, whole_l = 0;   // of place `lane`; tokens of row `lane` before and now, and how many pages at its table's head others may name too
     if (lane < N) {
         parent = p.parents[r0 + lane];
         if ((unsigned)parent >= (unsigned)N) parent = -1;
-        const int x = p.lens[r0 + lane];
-        len = x >= 0 ? min(x, p.width * p.page - p.appended) + p.appended : min(~x, p.width * p.page);   // (no more than a table holds)
-        whole_l = x == -1 ? p.width : len / p.page;   // (a row without a hypothesis has had one perhaps, or a dropped one's place: any of its pages may be shared)
+        was = p.lens[r0 + lane];
+        len = was >= 0 ? min(was, p.width * p.page - p.appended) + p.appended : min(~was, p.width * p.page);   // (no more than a table holds)
+        whole_l = was == -1 ? p.width : len / p.page;   // (a row without a hypothesis has had one perhaps, or a dropped one's place: any of its pages may be shared)
     }
+    if (__shfl(was, max(parent, 0)) == -1) parent = -1;   // (nothing to go on from: its children are places without a hypothesis as well)
     bool first = parent >= 0;
     unsigned has_child = 0;
     for (int i = 0; i < N; ++i) {

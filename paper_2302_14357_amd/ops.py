@@ -106,6 +106,7 @@ def beam_reorder(parents, tables, lens, caches, *, beams, finished=None, appende
     parents and finished are beam_select's; tables int32 [rows, table width] and lens int32 [rows] the ones this step ran with; caches the key and
     value caches [pages, page, kv_heads, dim] of every layer (a list of tensors alike in shape, strides and type, or one tensor with
     their number in front).  Full pages are shared, not copied.  `appended`: the step wrote a token per row that took part.  `status`
-    (int32, one number) counts hypotheses that had to be dropped; include/tbs.h says when.
+    (int32, one number) counts hypotheses that had to be dropped; include/tbs.h says when.  Their places, and those of their children, have the length -1:
+    where `(lens == -1) & ~finished`, give the score -inf before the next beam_select.
     """
     return (_binding or _load()).beam_reorder(parents, tables, lens, caches, beams, finished, appended, status)

@@ -728,6 +728,26 @@ def test_reorder_step_by_step_overwrites_nobody(beams, page, absent):
     assert empty > 0 and (drops > 0 or beams == 2 or absent > 0)   # (groups with empty places die out early)
 
 
+@pytest.mark.parametrize("absent", [0.0, 0.1])
+@pytest.mark.parametrize("beams,page", [(2, 1), (3, 4), (4, 4), (8, 3)])
+def test_reorder_a_place_without_a_hypothesis_has_no_heirs(beams, page, absent):
+    """Dropped and empty places as parents: their children have the length -1, and never a place in a living hypothesis' pages."""
+    drops, empty = _reorder_many_steps(beams * 10 + page + 1, groups=60, beams=beams, page=page, steps=20, absent=absent, heirs=True)
+    assert empty > 0
+
+
+def test_reorder_children_of_no_hypothesis():
+    from paper_2302_14357_amd import beam_reorder
+    tables, lens = torch.arange(24, dtype=torch.int32).view(4, 6).cuda(), torch.tensor([20, -1, 7, ~9], dtype=torch.int32).cuda()
+    for finished in (None, torch.tensor([False, True, False, True]).cuda()):
+        for appended in (True, False):
+            cache, status = torch.zeros(24, 4, 1, 8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+            t, n = beam_reorder(torch.tensor([1, 1, 0, 3], dtype=torch.int32).cuda(), tables, lens, [cache], beams=4, finished=finished, appended=appended, status=status)
+            assert n.tolist() == [-1, -1, 20 + appended, 9 if finished is None else ~9] and status.item() == 0
+            assert t[2].tolist() == tables[0].tolist() and t[3].tolist() == tables[3].tolist()
+            assert sorted(t[:2].reshape(-1).tolist()) == tables[1:3].reshape(-1).tolist()   # (pages of the rows without children: nobody's get lost)
+
+
 def test_reorder_gives_no_page_on_that_another_names():
     """Two steps: the first leaves a place that is dropped, or empty, with pages that a living hypothesis names; the second must not give them to another."""
     from paper_2302_14357_amd import beam_reorder
