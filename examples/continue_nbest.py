@@ -75,7 +75,7 @@ class Beams:
 @torch.no_grad()
 def continue_nbest(lm, nbest, beams, steps, page=16):
     """nbest: per utterance up to `beams` (tokens, log score).  Returns the same after `steps` tokens more (fewer for those that end), best first, and how
-    many hypotheses were dropped (beam_reorder's status).  A score is the list's plus the model's logarithms of all tokens, the first one's behind END."""
+    many hypotheses were dropped on the way (beam_reorder's status; they do not come back).  A score is the list's plus the model's logarithms of all tokens, the first one's behind END."""
     device = lm.embed.device
     rows = len(nbest) * beams
     said = [[END] + list(nb[i][0]) if i < len(nb) else [] for nb in nbest for i in range(beams)]
@@ -101,8 +101,9 @@ def continue_nbest(lm, nbest, beams, steps, page=16):
     for t in range(steps):
         scores, tokens, parents, done = beam_select(logits, scores, beams=beams, finished=done, eos=END)
         path.append((tokens, parents))
-        state.tables, state.lens = beam_reorder(parents, state.tables, state.lens, state.caches, beams=beams, finished=done, status=dropped)
         if t + 1 < steps:
+            state.tables, state.lens = beam_reorder(parents, state.tables, state.lens, state.caches, beams=beams, finished=done, status=dropped)
+            scores = scores.masked_fill((state.lens == -1) & ~done, -torch.inf)   # a hypothesis that was dropped has no tokens to go on from
             logits = state.logits(tokens)
     # the sequences, from the last step back
     path = [(t.view(-1, beams).tolist(), p.view(-1, beams).tolist()) for t, p in path]

@@ -82,6 +82,24 @@ def test_continue_nbest_float32(page):
     assert clear >= 2
 
 
+def test_continue_nbest_with_dropped_hypotheses():
+    """Lists of very different lengths and about equal scores, pages of one token: some hypotheses have to be dropped, and none of theirs comes back with a score
+    that is not its own."""
+    from continue_nbest import Lm, continue_nbest
+    lm = Lm(40, width=64, layers=1, heads=4, kv_heads=2, dtype=torch.float32, seed=3)
+    g = torch.Generator().manual_seed(8)
+    nbest = []
+    for u in range(8):
+        lists = [tuple(torch.randint(1, 40, (n,), generator=g).tolist()) for n in (0, 3, 9, 14)]
+        nbest.append([(t, -_plain_score(lm, 0.0, t) - 3.0 * float(torch.rand(1, generator=g))) for t in lists])
+    got, dropped = continue_nbest(lm, nbest, 4, 10, page=1)
+    assert dropped > 0
+    for mine, start in zip(got, nbest):
+        assert mine and all(a[1] >= b[1] for a, b in zip(mine, mine[1:]))
+        for t, s in mine:
+            assert min(abs(s - _plain_score(lm, b, t)) for p, b in start if t[:len(p)] == p) < TOL
+
+
 def test_example_runs_on_the_transducers_lists(capsys, monkeypatch):
     import continue_nbest
     monkeypatch.setattr(sys, "argv", ["continue_nbest.py", "--utts", "3", "--beam", "4", "--steps", "6"])
