@@ -323,8 +323,8 @@ enum tbs_act { TBS_ACT_NONE = 0, TBS_ACT_RELU = 1, TBS_ACT_TANH = 2, TBS_ACT_GEL
                TBS_ACT_SILU = 4 };
 
 /* out[i, j] = act(sum_k x[i, k] w[j, k] + bias[j]) + residual[i, j] for i < m, j < n.  x, w: dtype; bias float32 or NULL; residual
- * (may be NULL) and out: out_dtype, which is dtype or TBS_F32.  out may be residual itself (same stride); other overlaps are not
- * allowed.  m = 0 is no work.  Any sizes and strides; rows on 16-byte boundaries and k in whole 16-byte pieces are faster.
+ * (may be NULL) and out: out_dtype, which is dtype or TBS_F32.  out may be residual itself (same stride); other overlaps of out with
+ * what is read are refused.  m = 0 is no work.  Any sizes and strides; rows on 16-byte boundaries and k in whole 16-byte pieces are faster.
  * The same call gives the same bits. */
 typedef struct tbs_linear_args {
     const void *x;         /* [m, k], row stride ld_x */

@@ -62,7 +62,7 @@ def linear(x, weight, bias=None, *, act="none", residual=None, out=None, out_dty
 
     x [..., K] and weight [N, K] in float32, bfloat16 or float16; bias [N] float32; residual and the result [..., N] in x's type or, with
     out_dtype=torch.float32, in float32.  act: "none", "relu", "tanh", "gelu" (by the error function) or "silu".  `out` may be
-    `residual`.  Rows of any stride; the sum is float32 and rounded once.
+    `residual`, and lie over nothing else that is read (slices of one tensor beside each other are fine).  Rows of any stride; the sum is float32 and rounded once.
     """
     code = _ACTS.get(act)
     if code is None:

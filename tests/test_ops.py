@@ -148,6 +148,39 @@ def test_linear_in_place_residual_leading_dimensions_and_no_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 3, 70])
+def test_linear_results_beside_what_is_read(m, dtype):
+    """Slices of one tensor beside each other, rows between rows and memory end to end are no overlap; a result over x, the weights, the bias or another residual is refused."""
+    from paper_2302_14357_amd import TbsError, linear
+    g, n, k = _gen(m), 48, 64
+    x, w, r = _randn(g, m, k, dtype=dtype).cuda(), _randn(g, n, k, dtype=dtype).cuda(), _randn(g, m, n, dtype=dtype).cuda()
+    want = linear(x, w, residual=r)
+    for order in ((0, 1, 2), (2, 0, 1), (1, 2, 0)):
+        room = torch.zeros(m, n + k + n, dtype=dtype, device="cuda")
+        parts = dict(zip(order, room.split([(k, n, n)[i] for i in order], 1)))
+        parts[0].copy_(x), parts[2].copy_(r)
+        assert torch.equal(linear(parts[0], w, residual=parts[2], out=parts[1]), want)
+        assert torch.equal(parts[0], x) and torch.equal(parts[2], r)
+    flat = torch.zeros(m * (k + n) + n * k, dtype=dtype, device="cuda")
+    xs, out, ws = flat[:m * k].view(m, k), flat[m * k:m * (k + n)].view(m, n), flat[m * (k + n):].view(n, k)
+    xs.copy_(x), ws.copy_(w)
+    assert torch.equal(linear(xs, ws, residual=r, out=out), want) and torch.equal(ws, w)
+    square = _randn(g, k, k, dtype=dtype).cuda()
+    with pytest.raises(TbsError):
+        linear(x, square, out=x)
+    with pytest.raises(TbsError):
+        linear(xs, ws, out=flat[m * k - 1:m * (k + n) - 1].view(m, n))
+    with pytest.raises(TbsError):
+        linear(square[:1], square, out=square[3:4])
+    b = torch.zeros(max(m * n, n), device="cuda")
+    with pytest.raises(TbsError):
+        linear(x.float(), w.float(), b[-n:], out=b.view(-1, n))
+    wide = torch.zeros(m * n + 1, dtype=dtype, device="cuda")
+    with pytest.raises(TbsError):
+        linear(x, w, residual=wide[1:].view(m, n), out=wide[:-1].view(m, n))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m", [2, 50, 900])
 def test_linear_of_numbers_that_are_none(m, dtype):
     """A row with a NaN or an infinity is none of the other rows' business; an infinity of the bias or the residual comes through."""

@@ -28,6 +28,21 @@ def test_linear_refuses(bad):
     assert L.tbs_linear(C.byref(_linear(ops, **bad)), None) == -1
 
 
+# x [6, 64] by rows of 256 bytes, w [32, 64], out [6, 32] by rows of 128, in bf16, each in memory of its own; what lies over the result
+A, B, D, R, W = (P * i for i in (2, 3, 4, 5, 6))
+
+
+@pytest.mark.parametrize("bad", [dict(out=A, ld_out=128), dict(out=A + 64, ld_out=128), dict(out=A + 126, ld_out=128), dict(out=A - 62, ld_out=128), dict(out=A - 256 * 5 - 62, ld_out=128),
+                                 dict(out=A + 256 * 5, ld_out=128), dict(out=A + 126), dict(out=A - 5 * 64 - 62), dict(out=A + 5 * 256 + 126), dict(out=B), dict(out=B - 62, m=1),
+                                 dict(out=B + 64 * 2 * 32 - 2), dict(out=B, ld_out=64), dict(out=W + 126), dict(out=W - 6 * 64 + 2), dict(residual=D, ld_residual=64),
+                                 dict(residual=D + 2, ld_residual=32), dict(residual=D + 62, ld_residual=32), dict(residual=D - 6 * 64 + 2, ld_residual=32),
+                                 dict(residual=D + 62, ld_residual=100, m=1), dict(residual=D - 4, ld_residual=33)])
+def test_linear_refuses_a_result_over_what_it_reads(bad):
+    L, ops = _ops()
+    kw = dict(x=A, ld_x=128, m=6, w=B, out=D, bias=W, n=32, k=64)
+    assert L.tbs_linear(C.byref(_linear(ops, **{**kw, **bad})), None) == -1
+
+
 def test_linear_of_no_rows():
     L, ops = _ops()
     assert L.tbs_linear(C.byref(_linear(ops, m=0, x=None, out=None)), None) == 0
