@@ -35,10 +35,15 @@ struct Refused {
 };
 PyObject *g_raise = nullptr;
 
+// whether the caller records gradients (the calls themselves do not)
+bool g_grad = false;
+
 const Tensor *tensor(PyObject *o, const char *name, bool may_lack = false) {
     if (o == Py_None && may_lack) return nullptr;
     WANT(THPVariable_Check(o), name << " has to be a tensor");
-    return &THPVariable_Unpack(o);
+    const Tensor &t = THPVariable_Unpack(o);
+    WANT(!g_grad || !t.requires_grad(), name << " requires a gradient, and this operator has none: call it under torch.no_grad(), or on a detached tensor");
+    return &t;
 }
 
 int32_t dtype_of(const Tensor &t, const char *name) {
@@ -137,6 +142,7 @@ Tensor workspace(int64_t (*fn)(const Args *), Args &a, const at::Device &d) {
 template <class F>
 PyObject *guarded(F f) {
     try {
+        g_grad = at::GradMode::is_enabled();
         const at::NoGradGuard no_grad;
         return f();
     } catch (const Refused &r) {
@@ -316,7 +322,7 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         ARGS(8);
         const Tensor &parents = *tensor(o[0], "parents"), &tables = *tensor(o[1], "tables"), &lens = *tensor(o[2], "lens");
         const Tensor *finished = tensor(o[5], "finished", true), *status = tensor(o[7], "status", true);
-        const at::Device d = gpu(parents);
+        const at::Device d = parents.device();
         WANT(tables.dim() == 2 && tables.scalar_type() == at::kInt, "tables [rows, table width] in int32 is wanted");
         const int64_t rows = tables.size(0), width = tables.size(1);
         on(tables, "tables", d);
@@ -324,7 +330,7 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         c10::SmallVector<void *, 64> ptrs;
         Tensor first;
         if (THPVariable_Check(o[3])) {
-            const Tensor &all = THPVariable_Unpack(o[3]);
+            const Tensor &all = *tensor(o[3], "caches");
             WANT(all.dim() == 5 && all.size(0) > 0, "caches has shape " << all.sizes() << ": [caches, pages, page, kv_heads, dim] is wanted");
             first = all.select(0, 0);
             for (int64_t i = 0; i < all.size(0); ++i) ptrs.push_back((char *)all.data_ptr() + i * all.stride(0) * all.element_size());
@@ -341,6 +347,7 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
                 ptrs.push_back(c.data_ptr());
             }
         }
+        gpu(parents);
         tbs_beam_reorder_args a = {};
         a.dtype = dtype_of(first, "caches");
         cache_of(first, "caches", first.scalar_type(), d, a.cache_page, a.cache_token, a.cache_head);

@@ -2,7 +2,7 @@
 new token over a paged cache, selection over beams and vocabulary, reordering of the cached states.
 
 Each function checks its tensors, makes the outputs and enqueues the kernels on the current stream of the tensors' device; nothing
-synchronises.  What the library refuses is a TbsError, a tensor of the wrong type, shape or device a ValueError.
+synchronises.  They serve and have no gradients: with grad mode on, a tensor that requires one is refused.  What the library refuses is a TbsError, a tensor of the wrong type, shape or device a ValueError.
 """
 
 from __future__ import annotations

@@ -151,3 +151,29 @@ def test_tensors_that_do_not_fit():
         beam_select(x, torch.zeros(3, dtype=torch.float64), beams=3)
     with pytest.raises(ValueError):
         beam_reorder(torch.zeros(3, dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), [cache], beams=3)
+
+
+def test_tensors_that_require_a_gradient():
+    """None of the operators has a gradient, so a call that would lose one is refused; without grad mode it is a call like another (here: not on a GPU)."""
+    import torch
+    from paper_2302_14357_amd import attend_paged, beam_reorder, beam_select, linear
+    x, w, b, r = torch.zeros(3, 8), torch.zeros(4, 8), torch.zeros(4), torch.zeros(3, 4)
+    q, cache, kn = torch.zeros(2, 4, 8), torch.zeros(5, 4, 2, 8), torch.zeros(2, 2, 8)
+    tables, lens = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    leaf = lambda t: t.clone().requires_grad_()   # noqa: E731
+    calls = [lambda f: linear(f(x), w, b, residual=r), lambda f: linear(x, f(w), b, residual=r), lambda f: linear(x, w, f(b), residual=r), lambda f: linear(x, w, b, residual=f(r)),
+             lambda f: linear(x, w, out=f(r)), lambda f: attend_paged(f(q), cache, cache, tables, lens), lambda f: attend_paged(q, f(cache), cache, tables, lens),
+             lambda f: attend_paged(q, cache, f(cache), tables, lens), lambda f: attend_paged(q, cache, cache, tables, lens, k_new=f(kn), v_new=kn),
+             lambda f: attend_paged(q, cache, cache, tables, lens, k_new=kn, v_new=f(kn)), lambda f: beam_select(f(x), torch.zeros(3, dtype=torch.float64), beams=3),
+             lambda f: beam_select(x, f(torch.zeros(3, dtype=torch.float64)), beams=3), lambda f: beam_reorder(lens, tables, lens, [cache, f(cache)], beams=2),
+             lambda f: beam_reorder(lens, tables, lens, f(torch.zeros(2, 5, 4, 2, 8)), beams=2)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call(leaf)
+        for f in (leaf, lambda t: t):
+            with torch.no_grad(), pytest.raises(ValueError) as e:
+                call(f)
+            assert "gradient" not in str(e.value)
+        with pytest.raises(ValueError) as e:
+            call(lambda t: t)
+        assert "gradient" not in str(e.value)
