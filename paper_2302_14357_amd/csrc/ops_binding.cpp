@@ -127,6 +127,11 @@ void call(int (*fn)(const Args *, void *), const Args &a, const at::Device &d) {
     if (rc) throw Refused{rc};
 }
 
+// A tensor of the caller's was written: autograd sees that what it had kept of it is gone (a tensor made in inference mode has no version)
+void written(const Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A call's workspace, kept until it is enqueued (the allocator hands its memory on in the order of the stream).
 template <class Args>
 Tensor workspace(int64_t (*fn)(const Args *), Args &a, const at::Device &d) {
@@ -214,6 +219,7 @@ PyObject *py_linear(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
             call(tbs_linear, a, d);
         }
         if (out) {
+            written(*out);
             Py_INCREF(o[5]);
             return o[5];
         }
@@ -266,8 +272,10 @@ PyObject *py_attend(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         if (rows > 0) {
             const Tensor work = workspace(tbs_attend_workspace, a, d);
             call(tbs_attend_paged, a, d);
+            if (kn) written(kc), written(vc);
         }
         if (out) {
+            written(*out);
             Py_INCREF(o[10]);
             return o[10];
         }
@@ -329,6 +337,11 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         // a list or tuple of tensors, or one tensor with their number in front
         c10::SmallVector<void *, 64> ptrs;
         Tensor first;
+        auto caches = [&](auto f) {   // of a list or tuple, or the one
+            if (THPVariable_Check(o[3])) f(THPVariable_Unpack(o[3]));
+            else
+                for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(o[3]); ++i) f(THPVariable_Unpack(PySequence_Fast_GET_ITEM(o[3], i)));
+        };
         if (THPVariable_Check(o[3])) {
             const Tensor &all = *tensor(o[3], "caches");
             WANT(all.dim() == 5 && all.size(0) > 0, "caches has shape " << all.sizes() << ": [caches, pages, page, kv_heads, dim] is wanted");
@@ -373,6 +386,8 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
                 if (i) a.status = nullptr;
                 call(tbs_beam_reorder, a, d);
             }
+            caches(written);
+            if (status) written(*status);
         }
         return tuple_of({t, n});
     });

@@ -863,6 +863,28 @@ def test_a_beam_decode_keeps_every_hypothesis(dtype):
             assert all(not a & b for i, a in enumerate(own) for b in own[:i])
 
 
+def test_what_a_call_writes_has_a_new_version():
+    """Autograd's count of writes goes up where a call writes a tensor of the caller's, and only there; tensors made in inference mode have none."""
+    from paper_2302_14357_amd import attend_paged, beam_reorder, linear
+    x, w, out = torch.zeros(3, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), torch.zeros(3, 4, device="cuda")
+    q, kn, k, v = torch.zeros(2, 2, 8, device="cuda"), torch.zeros(2, 1, 8, device="cuda"), torch.zeros(4, 4, 1, 8, device="cuda"), torch.zeros(4, 4, 1, 8, device="cuda")
+    tables, lens, status = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2), torch.ones(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    parents, layers = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 4, 4, 1, 8, device="cuda")
+    o = torch.zeros(2, 2, 8, device="cuda")
+    for call, changed in [(lambda: linear(x, w), []), (lambda: linear(x, w, residual=out, out=out), [out]), (lambda: attend_paged(q, k, v, tables, lens), []),
+                          (lambda: attend_paged(q, k, v, tables, lens, k_new=kn, v_new=kn, out=o), [k, v, o]), (lambda: beam_reorder(parents, tables, lens, [k, v], beams=2, status=status), [k, v, status]),
+                          (lambda: beam_reorder(parents, tables, lens, layers, beams=2), [layers])]:
+        tensors = [x, w, out, q, kn, k, v, tables, lens, status, parents, layers, o]
+        before = [t._version for t in tensors]
+        call()
+        assert [t._version - b for t, b in zip(tensors, before)] == [int(any(t is c for c in changed)) for t in tensors]
+    with torch.inference_mode():
+        k, v = torch.zeros(4, 4, 1, 8, device="cuda"), torch.zeros(4, 4, 1, 8, device="cuda")
+        attend_paged(q, k, v, tables, lens, k_new=kn, v_new=kn)
+    attend_paged(q, k, v, tables, lens, k_new=kn, v_new=kn)
+    beam_reorder(parents, tables, lens, (k, v), beams=2)
+
+
 # ------------------------------------------------------------------ streams and graphs
 
 def _step(s):
