@@ -330,6 +330,9 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         ARGS(8);
         const Tensor &parents = *tensor(o[0], "parents"), &tables = *tensor(o[1], "tables"), &lens = *tensor(o[2], "lens");
         const Tensor *finished = tensor(o[5], "finished", true), *status = tensor(o[7], "status", true);
+        const int appended = PyObject_IsTrue(o[6]);
+        if (appended < 0) PyErr_Clear();
+        WANT(appended >= 0, "appended has to be True or False");
         const at::Device d = parents.device();
         WANT(tables.dim() == 2 && tables.scalar_type() == at::kInt, "tables [rows, table width] in int32 is wanted");
         const int64_t rows = tables.size(0), width = tables.size(1);
@@ -376,7 +379,7 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
             a.status = (int32_t *)status->data_ptr();
         }
         a.rows = size32(rows, "rows"), a.beams = number(o[4], "beams"), a.table_width = size32(width, "table width");
-        a.appended = PyObject_IsTrue(o[6]) ? 1 : 0;
+        a.appended = appended;
         Tensor t = made({rows, width}, at::kInt, d), n = made({rows}, at::kInt, d);
         if (rows > 0) {
             a.tables = (const int32_t *)tables.data_ptr(), a.out_tables = (int32_t *)t.data_ptr(), a.out_lens = (int32_t *)n.data_ptr();

@@ -177,3 +177,11 @@ def test_tensors_that_require_a_gradient():
         with pytest.raises(ValueError) as e:
             call(lambda t: t)
         assert "gradient" not in str(e.value)
+
+
+def test_reorder_appended_that_is_no_truth_value():
+    import torch
+    from paper_2302_14357_amd import beam_reorder
+    row, tables = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="appended"):
+        beam_reorder(row, tables, row, [torch.zeros(5, 4, 2, 8)], beams=2, appended=torch.zeros(2))
