@@ -34,7 +34,7 @@ template <int ACT, bool F32>
 __device__ __forceinline__ float linear_act(float y) {
     if constexpr (ACT == TBS_ACT_RELU) return y > 0.f || y != y ? y : 0.f;   // (NaN stays)
     else if constexpr (ACT == TBS_ACT_TANH) return F32 ? tanhf(y) : linear_tanh16(y);
-    else if constexpr (ACT == TBS_ACT_GELU) return F32 ? 0.5f * y * (1.f + erff(y * 0.70710678f)) : linear_gelu16(y);
+    else if constexpr (ACT == TBS_ACT_GELU) return F32 ? 0.5f * y * erfcf(y * -0.70710678f) : linear_gelu16(y);   // (1 + erf would cancel where y is far below 0)
     else if constexpr (ACT == TBS_ACT_SILU) return F32 ? y / (1.f + expf(-y)) : y * __builtin_amdgcn_rcpf(1.f + __expf(-y));
     else return y;
 }

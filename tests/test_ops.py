@@ -98,6 +98,17 @@ def test_linear_strides_and_alignment(m, n, k, pad, shift, dtype):
     _linear_case(m, n, k, dtype, "relu", True, True, pad=pad, shift=shift)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_gelu_far_below_zero_in_float32(dtype):
+    """Where 1 + erf has lost its digits: pre-activations from -10 to -4, exact, without a residual."""
+    from paper_2302_14357_amd import linear
+    y = torch.linspace(-10, -4, 4000).to(dtype).view(500, 8)
+    got = linear(y.cuda(), torch.eye(8, dtype=dtype, device="cuda"), act="gelu", out_dtype=torch.float32)
+    ref = 0.5 * y.double() * torch.special.erfc(-y.double() * math.sqrt(0.5))   # (torch's ndtr is 1 + erf, too)
+    # erfc's argument is rounded twice, each worth y^2 half steps of the result; erfc is within 16 units, the products within one each
+    _close(got, ref, ref.abs() * (2 * y.double() ** 2 + 32 + 2) * 2.0**-24)
+
+
 def _linear_by(kernel, x, w, b, act, r, out):
     import ctypes
     from paper_2302_14357_amd import ops
