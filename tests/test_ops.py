@@ -109,6 +109,18 @@ def test_linear_gelu_far_below_zero_in_float32(dtype):
     _close(got, ref, ref.abs() * (2 * y.double() ** 2 + 32 + 2) * 2.0**-24)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_linear_gelu_far_below_zero_in_16_bits(dtype):
+    """Half a step of the type and a quarter of one: pre-activations from -10 to -4, exact, without a residual; and 0 from where nothing is left."""
+    from paper_2302_14357_amd import linear
+    y = torch.linspace(-10, -4, 4000).to(dtype).view(500, 8)
+    eye = torch.eye(8, dtype=dtype, device="cuda")
+    ref = 0.5 * y.double() * torch.special.erfc(-y.double() * math.sqrt(0.5))
+    _close(linear(y.cuda(), eye, act="gelu"), ref, 1.5 * _half_step(ref, dtype))
+    far = linear(torch.full((3, 8), -20.0, dtype=dtype, device="cuda"), eye, act="gelu")
+    assert bool((far == 0).all())
+
+
 def _linear_by(kernel, x, w, b, act, r, out):
     import ctypes
     from paper_2302_14357_amd import ops
