@@ -324,8 +324,9 @@ enum tbs_act { TBS_ACT_NONE = 0, TBS_ACT_RELU = 1, TBS_ACT_TANH = 2, TBS_ACT_GEL
 
 /* out[i, j] = act(sum_k x[i, k] w[j, k] + bias[j]) + residual[i, j] for i < m, j < n.  x, w: dtype; bias float32 or NULL; residual
  * (may be NULL) and out: out_dtype, which is dtype or TBS_F32.  out may be residual itself (same stride); other overlaps of out with
- * what is read are refused.  m = 0 is no work.  Any sizes and strides; rows on 16-byte boundaries and k in whole 16-byte pieces are faster.
- * The same call gives the same bits. */
+ * what is read are refused.  m = 0 is no work.  Any sizes, strides of a row's length or more; rows on 16-byte boundaries and k in whole 16-byte
+ * pieces are faster.  Activations are accurate to a few units of float32 where out is float32 (GELU far below 0: y^2 of them), else to a
+ * quarter of half a step of out's type (results above 1e-36).  The same call gives the same bits. */
 typedef struct tbs_linear_args {
     const void *x;         /* [m, k], row stride ld_x */
     const void *w;         /* [n, k], row stride ld_w */
@@ -341,12 +342,14 @@ int tbs_linear(const tbs_linear_args *args, void *stream);
 /* Attention of one new token per row over a paged cache.  Row r attends to n = lens[r] + 1 tokens (lens[r] of them in the cache, then
  * the new one) or, without k_new and v_new, to the n = lens[r] in the cache; token t of the row is token t % page of page
  * tables[r, t / page].  Query head h reads key head h / (heads / kv_heads).  For every query head
- *     out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t - max),  and 0 where n = 0.
- * The new token is written to its place in the cache as well: no other row's table may name that page (tbs_beam_reorder sees to it).
+ *     out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t - max),  and 0 where n = 0 or every score is -inf.
+ * A NaN or an infinity is its own row's business: what a row does not attend to never reaches its output.
+ * The new token is written to its place in the cache as well: no other row's table may name that page (tbs_beam_reorder sees to it).  out may be q itself
+ * (same strides); out and the caches that are written lie over nothing else that is read.
  * lens[r] < 0: the row takes no part; its output is 0 and nothing is written for it.  A table entry outside [0, pages) is a page
  * whose tokens do not exist: not attended to, not written (a new token is attended to all the same).  Tokens beyond table_width * page
  * do not exist either.  What the cache holds behind a row's last token is not looked at.
- * dim is a multiple of 8 up to 256, heads a multiple of kv_heads, a page's stride and `page` tokens' below 4 GiB.  max_len: about how many tokens the longest row attends to (0: as
+ * dim is a multiple of 8 up to 256, heads a multiple of kv_heads, rows and heads at most 65535, a page's stride and `page` tokens' below 4 GiB.  max_len: about how many tokens the longest row attends to (0: as
  * many as its table holds); it decides how the work is split, never the result's correctness.  beams: rows beams * i .. beams * i +
  * beams - 1 are hypotheses of one utterance, whose tables may name the same pages (1: rows share nothing); rows is a multiple of it.  It
  * is a hint too: pages that several rows of a group have in common are then read once.
@@ -380,7 +383,7 @@ int64_t tbs_attend_workspace(const tbs_attend_args *args);
  * workspace: tbs_beam_select_workspace(args) bytes on a 16-byte boundary (0: none).  The same call gives the same bits. */
 #define TBS_MAX_VOCAB 524288
 typedef struct tbs_beam_select_args {
-    const void *logits;       /* [rows, vocab] in dtype, row stride ld_logits */
+    const void *logits;       /* [rows, vocab] in dtype, row stride ld_logits, vocab or more; at most 65535 rows */
     const double *scores;     /* [rows] */
     const uint8_t *finished;  /* [rows] or NULL: none is */
     double *out_scores;       /* [rows], every group best first */

@@ -551,8 +551,11 @@ static hipError_t linear_few_launch(const tbs_linear_args &a, const LinearEp &ep
 //     1000 x 4096 x 1024 19 / 22, 64 x 32000 x 1024 22 / 18
 //   128 x 128, two a CU: 12.5 K for one a CU, 18 K + 4 for two: 1000 x 4096 x 1024 15.5 / 16.5, 8000 x 1024 x 4096 79 / 75
 //   192 x 256: 22 K + 6 a turn: 2560 x 4096 x 1024 30 / 30;  256 x 256: 28 K + 9 a turn: 8000 x 4096 x 1024 76 / 81, 8192 x 4096 x 4096 244 / 237
-//   float32's matrix instructions take their own time: 64 x 64 11 K and 20 K, 128 x 128 32 K and 70 K, 192 x 256 112 K, 256 x 256 137 K
-//   k_linear_any, where the tiles' alignment is missing: 10 K, or 18.5 K for every 1024 tiles (float32 15 and 48)
+//   float32's matrix instructions take their own time: 64 x 64 11 K and 20 K: 256 x 4096 x 1024 25 / 28, 1000 x 4096 x 1024 83 / 94, 8000 x 1024 x 4096 643 / 612;
+//     128 x 128 32 K and 70 K: 256 x 4096 x 1024 67 / 71, 1000 x 4096 x 1024 67 / 83, 8000 x 1024 x 4096 563 / 563;  192 x 256 112 K: 2560 x 4096 x 1024 232 / 204, 8192 x
+//     4096 x 4096 2708 / 2209;  256 x 256 137 K: 8000 x 1024 x 4096 1107 / 970, 8192 x 4096 x 4096 2212 / 1955
+//   k_linear_any, where the tiles' alignment is missing: 10 K, or 18.5 K for every 1024 tiles: 300 x 1001 x 2001 23 / 18, 1000 x 1000 x 999 13 / 11, 2000 x 2001 x 2001
+//     39 / 52, 4000 x 4999 x 4999 442 / 792 (nothing else comes near there); float32 15 and 48: 62 / 54, 32 / 33, 191 / 196, 2281 / 1964
 struct LinearChoice {
     int kernel;
     double us;

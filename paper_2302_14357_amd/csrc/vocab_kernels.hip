@@ -249,8 +249,8 @@ __device__ __forceinline__ double voc_sum(const float (&v)[VOC_ELEMS], float top
 }
 
 // A slice's best: as voc_wave_best, with the line drawn by all 256 lane maxima, so that the four waves together collect little more than N.
-// Eight waves a SIMD: a slice's loads wait behind other slices' arithmetic.  (512 rows of 131000 in float32, groups of 16: 78 us, 3.4 TB/s; the float64
-// exponentials, sixteen instructions a logit, keep the vector units busy most of that.  Slices of 4096 100 us; waves that go on through 32768 each with a list
+// Eight waves a SIMD: a slice's loads wait behind other slices' arithmetic.  (512 rows of 131000 in float32, groups of 16: 75 to 79 us, 3.5 TB/s; the float64
+// exponentials, sixteen instructions a logit, are most of what keeps the vector units busy for 69 % of that.  Slices of 4096 100 us; waves that go on through 32768 each with a list
 // of its own 106.)
 template <class T>
 __global__ void __launch_bounds__(256, 8)

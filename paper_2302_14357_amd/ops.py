@@ -62,7 +62,8 @@ def linear(x, weight, bias=None, *, act="none", residual=None, out=None, out_dty
 
     x [..., K] and weight [N, K] in float32, bfloat16 or float16; bias [N] float32; residual and the result [..., N] in x's type or, with
     out_dtype=torch.float32, in float32.  act: "none", "relu", "tanh", "gelu" (by the error function) or "silu".  `out` may be
-    `residual`, and lie over nothing else that is read (slices of one tensor beside each other are fine).  Rows of any stride; the sum is float32 and rounded once.
+    `residual`, and lie over nothing else that is read (slices of one tensor beside each other are fine).  Rows apart by
+    their length or more; the sum is float32 and rounded once.
     """
     code = _ACTS.get(act)
     if code is None:
@@ -81,7 +82,7 @@ def attend_paged(q, k_cache, v_cache, tables, lens, *, k_new=None, v_new=None, s
     q [rows, heads, dim], k_new and v_new [rows, kv_heads, dim] (both or neither), k_cache and v_cache [pages, page, kv_heads, dim] (any
     strides, a head's elements side by side; a layout [pages, kv_heads, page, dim] is given as its transpose), all in one of float32,
     bfloat16 and float16; tables int32 [rows, table width] of page numbers; lens int32 [rows], the tokens in the cache before this one,
-    negative for a row that takes no part.  Returns [rows, heads, dim].  `beams` rows are hypotheses of one utterance and may share
+    negative for a row that takes no part.  Returns [rows, heads, dim] (`out`, which may be `q`).  `beams` rows are hypotheses of one utterance and may share
     pages; `max_len` is about the longest row's tokens (default: what a table holds).  include/tbs.h says what holds at the edges.
     """
     return (_binding or _load()).attend_paged(q, k_cache, v_cache, tables, lens, k_new, v_new, scale, beams, max_len, out)
