@@ -16,13 +16,15 @@ struct LinearEp {
 // y P(y) = max(y, 0) - |y| P(-|y|) with the normal distribution function P, for outputs of 16 bits: log2 P(-a) by a polynomial of degree 8, found by linear
 // programming over 0 <= a <= 13.2, where a P(-a) leaves the normal numbers.  |y| P(-|y|) is then off by 2.2e-7 at most and, as a part of itself, by 8.1e-5 down to
 // 6e-5 (a sixth of fp16's half step; below it numbers of fp16 are 6e-8 apart, and it is off by 4.9e-9) and 1e-3 below (a quarter of bf16's).  The polynomial falls
-// without end, so that nothing is left from 20 on.
+// without end, so that nothing is left from 20 on.  Half of it is the exponent and the exponential goes in twice: it is 0 where its result is below the normal
+// numbers, which P is before a P is.
 __device__ __forceinline__ float linear_gelu16(float y) {
     const float a = fminf(fabsf(y), 20.f);
-    float p = fmaf(a, 4.814969756239407e-08f, -2.7616981697065057e-06f);
-    p = fmaf(a, fmaf(a, fmaf(a, p, 6.779101386200637e-05f), -0.0009465293842367828f), 0.008517805486917496f);
-    p = fmaf(a, fmaf(a, fmaf(a, fmaf(a, p, -0.05395275354385376f), -0.4584517180919647f), -1.151276707649231f), -0.99998939037323f);
-    return fmaf(-a, __builtin_amdgcn_exp2f(p), y <= 0.f ? 0.f : y);   // (NaN stays)
+    float p = fmaf(a, 2.4074848781197034e-08f, -1.3808490848532529e-06f);
+    p = fmaf(a, fmaf(a, fmaf(a, p, 3.389550693100318e-05f), -0.0004732646921183914f), 0.004258902743458748f);
+    p = fmaf(a, fmaf(a, fmaf(a, fmaf(a, p, -0.02697637677192688f), -0.22922585904598236f), -0.5756383538246155f), -0.499994695186615f);
+    const float e = __builtin_amdgcn_exp2f(p);
+    return fmaf(-a * e, e, y <= 0.f ? 0.f : y);   // (NaN stays)
 }
 
 // ... hyperbolic tangent and logistic function for such outputs: hardware exponential and reciprocal (a few units of float32), near 0, where

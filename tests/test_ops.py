@@ -121,6 +121,19 @@ def test_linear_gelu_far_below_zero_in_16_bits(dtype):
     assert bool((far == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act,low,high", [("gelu", -13.0, 100.0), ("silu", -80.0, 100.0), ("tanh", -100.0, 100.0)])
+def test_linear_activations_in_16_bits(act, low, high, dtype):
+    """All over their range, exact pre-activations of every size: half a step of the type and a quarter of one."""
+    from paper_2302_14357_amd import linear
+    g = _gen(41)
+    y = torch.cat([torch.linspace(low, high, 4000), torch.linspace(-6, 6, 4000), torch.exp(torch.linspace(-14, 2.5, 2000)), -torch.exp(torch.linspace(-14, 2.5, 2000)), _randn(g, 2000)])
+    y = y.to(dtype).view(-1, 8)
+    x = y.double()
+    ref = {"gelu": 0.5 * x * torch.special.erfc(-x * math.sqrt(0.5)), "silu": x / (1 + torch.exp(-x)), "tanh": torch.tanh(x)}[act]
+    _close(linear(y.cuda(), torch.eye(8, dtype=dtype, device="cuda"), act=act), ref, 1.25 * _half_step(ref, dtype))
+
+
 def _linear_by(kernel, x, w, b, act, r, out):
     import ctypes
     from paper_2302_14357_amd import ops
