@@ -508,6 +508,23 @@ def test_attend_an_infinity_comes_through(n, beams, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("beams,n", [(1, 40), (4, 40), (4, 3000)])
+def test_attend_into_the_queries_place(beams, n, dtype):
+    """The result may be q itself, also as a slice beside the new keys and values."""
+    from paper_2302_14357_amd import attend_paged
+    g, rows, heads, kv, dim, page = _gen(51), 4, 6, 2, 64, 16
+    width = n // page + 1
+    tables, lens = torch.randperm(rows * width, generator=g).int().view(rows, width).cuda(), torch.full((rows,), n, dtype=torch.int32).cuda()
+    k, v = (_randn(g, rows * width, page, kv, dim, dtype=dtype).cuda() for _ in range(2))
+    qkv = _randn(g, rows, heads + 2 * kv, dim, dtype=dtype).cuda()
+    q, kn, vn = qkv.split((heads, kv, kv), 1)
+    want = attend_paged(q, k, v, tables, lens, k_new=kn, v_new=vn, beams=beams)
+    kept = qkv[:, heads:].clone()
+    assert attend_paged(q, k, v, tables, lens, k_new=kn, v_new=vn, beams=beams, out=q) is q
+    assert torch.equal(q, want) and torch.equal(qkv[:, heads:], kept)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_attend_large_scores(dtype):
     """Weights of one token alone, of equal scores, and scores whose exponentials would overflow."""
     _attend_case([70, 130, 10], heads=4, kv=2, dim=64, page=16, dtype=dtype, q_scale=30.0)
