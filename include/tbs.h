@@ -314,7 +314,8 @@ int tbs_gemm_bf16(const void *A, const void *B, const float *bias, float *C, int
 /* ---- operators of an autoregressive model beside the search ----
  * One step of a transformer's beam decode (a language model or an attention decoder that continues or rescores
  * hypotheses), without a context: products with their epilogue, attention of one new token per hypothesis over a paged cache, the
- * selection over beams and vocabulary, and the states' reordering.  Every argument block is read before the call returns; all
+ * selection over beams and vocabulary, and the states' reordering; and before the first step the prompts' way into the cache: pages, places, positions,
+ * causal attention.  Every argument block is read before the call returns; all
  * pointers in it are DEVICE and borrowed until the work enqueued on `stream` is done.  Kernels run on the current device, nothing is
  * allocated or synchronised, and the calls may be captured into a graph.  Blocks are zeroed by the caller first: fields that are not named
  * are 0.  Strides count elements.  Sums, softmax statistics and scores are held in float32 or more; each output is rounded once. */
@@ -426,6 +427,89 @@ typedef struct tbs_beam_reorder_args {
     int32_t n_caches, rows, beams, table_width, pages, page, kv_heads, dim, dtype, appended;   /* n_caches up to TBS_MAX_CACHES */
 } tbs_beam_reorder_args;
 int tbs_beam_reorder(const tbs_beam_reorder_args *args, void *stream);
+
+/* Pages for prompts.  Prompt i of lens[i] tokens (negative: there is none) gets `beams` table rows with pages for its tokens and `room` more: rows beams * i .. of
+ * the tables share its lens[i] / page whole pages, which nothing writes again, and have the other ceil((lens[i] + room) / page) - lens[i] / page for themselves.
+ * Pages are the next ones of the list free_pages behind the *taken first: prompt after prompt, the shared ones, then those of its first row, and so on.  Entries
+ * behind a row's pages are -1.  out_lens[beams * i] is lens[i] and those of the prompt's other rows are -1: places without a hypothesis yet, as tbs_beam_reorder takes them.
+ * A prompt whose pages end behind the list's end, or that wants more than table_width of them, has no pages and lengths of -1 (and so has every later one that wants
+ * any, where the list is too short).  *out_taken: the pages taken now, of all calls (a negative *taken counts as 0).  prompts * beams is below 2^31. */
+typedef struct tbs_page_tables_args {
+    const int32_t *lens;         /* [prompts] */
+    const int32_t *free_pages;   /* [free_count] page numbers */
+    const int32_t *taken;        /* one number */
+    int32_t *tables;             /* [prompts * beams, table_width], row stride ld_tables */
+    int32_t *out_lens;           /* [prompts * beams] */
+    int32_t *out_taken;          /* one number, not the one that is read */
+    int64_t ld_tables;
+    int32_t prompts, beams, page, table_width, room, free_count;   /* page up to 65536, room up to 2^30 */
+} tbs_page_tables_args;
+int tbs_page_tables(const tbs_page_tables_args *args, void *stream);
+
+/* Where the tokens of a packed batch stand and go.  The batch holds lens[i] new tokens of prompt i, prompt after prompt; past[i] tokens came before them.
+ * starts[i] is the first token of prompt i and starts[prompts] the first behind all (each at most `tokens`); token t of prompt i has the position
+ * past[i] + t - starts[i] and the slot tables[i, position / page] * page + position % page, -1 where the table has no page for it.  Tokens of no prompt: position and
+ * slot -1.  Negative lens and past count as 0. */
+typedef struct tbs_page_slots_args {
+    const int32_t *lens;     /* [prompts] */
+    const int32_t *past;     /* [prompts] or NULL: none have any */
+    const int32_t *tables;   /* [prompts, table_width], row stride ld_tables */
+    int32_t *starts;         /* [prompts + 1] */
+    int32_t *positions;      /* [tokens] */
+    int64_t *slots;          /* [tokens] */
+    int64_t ld_tables;
+    int32_t prompts, tokens, page, table_width;
+} tbs_page_slots_args;
+int tbs_page_slots(const tbs_page_slots_args *args, void *stream);
+
+/* Rotary positions, and keys and values into the cache.  Pair j < pairs of a head, its elements j and pairs + j (interleaved: 2 j and 2 j + 1), is turned by the angle
+ * positions[t] * freqs[j] (radians, in float64): (a, b) becomes (a cos - b sin, b cos + a sin), rounded once; elements from 2 * pairs on stay as they are.
+ * With slots (then v, k_cache and v_cache as well; otherwise none of them) the turned key and the value of token t are written to token slots[t] % page of page slots[t] / page, if
+ * 0 <= slots[t] < pages * page; of tokens with one slot, each 16 bytes are one's.  q_out and k_out may be q and k themselves (same strides) and lie over nothing else that is
+ * read; the caches lie over nothing else either.  dim is at most 512. */
+typedef struct tbs_rotary_args {
+    const void *q;               /* [tokens, heads, dim]; elements of a head side by side everywhere */
+    const void *k, *v;           /* [tokens, kv_heads, dim] */
+    const int32_t *positions;    /* [tokens] */
+    const double *freqs;         /* [pairs] */
+    const int64_t *slots;        /* [tokens] or NULL */
+    void *q_out, *k_out;
+    void *k_cache, *v_cache;     /* [pages, page, kv_heads, dim] */
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, q_out_row, q_out_head, k_out_row, k_out_head;
+    int64_t k_cache_page, k_cache_token, k_cache_head, v_cache_page, v_cache_token, v_cache_head;
+    int32_t tokens, heads, kv_heads, dim, pairs, interleaved, pages, page, dtype;
+} tbs_rotary_args;
+int tbs_rotary(const tbs_rotary_args *args, void *stream);
+
+/* Causal attention of packed prompts.  Prompt i has the new tokens starts[i] .. starts[i + 1] - 1 of the batch and, where past is given, past[i] tokens before them in the
+ * cache (token t of these is token t % page of page tables[i, t / page]).  Every new token attends to all that came before it in its prompt and to itself:
+ *     out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t - max),  and 0 where every score is -inf.
+ * Query head h reads key head h / (heads / kv_heads).  The new tokens' keys and values are read from k and v, whether the cache has them already or not.  A NaN or an
+ * infinity reaches no output of a token that does not attend to it.  (Of a value that is infinite and has a weight that 16 bits, or float32, hold as 0 the product is
+ * NaN.)  Weights are rounded to the type of the values.  Rows of no prompt, before starts[0] and from starts[prompts] on, are 0.  starts rises from 0 to at most `tokens`; other
+ * numbers give wrong rows, nothing worse.  Tokens of the cache beyond table_width * page and on pages outside [0, pages) do not exist; a negative past counts as 0.
+ * out may be q itself (same strides) and lies over nothing else that is read.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
+ * a table's tokens with the batch's below 2^31 and 2^30.  Rows and heads on 16-byte boundaries are faster.  The same call gives the same bits.
+ * workspace: tbs_attend_prompts_workspace(args) bytes on a 16-byte boundary (0: none), free again when the work is done. */
+typedef struct tbs_attend_prompts_args {
+    const void *q;                       /* [tokens, heads, dim]; elements of a head side by side everywhere */
+    const void *k, *v;                   /* [tokens, kv_heads, dim] */
+    const void *k_cache, *v_cache;       /* [pages, page, kv_heads, dim], with past only */
+    const int32_t *starts;               /* [prompts + 1] */
+    const int32_t *past;                 /* [prompts] or NULL */
+    const int32_t *tables;               /* [prompts, table_width], row stride ld_tables; with past only */
+    void *out;                           /* [tokens, heads, dim] */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+    int64_t k_cache_page, k_cache_token, k_cache_head, v_cache_page, v_cache_token, v_cache_head;
+    int64_t ld_tables;
+    int32_t tokens, prompts, heads, kv_heads, dim, page, pages, table_width, dtype;
+    float scale;                         /* 0: 1 / sqrt(dim) */
+} tbs_attend_prompts_args;
+int tbs_attend_prompts(const tbs_attend_prompts_args *args, void *stream);
+/* Bytes of workspace that tbs_attend_prompts wants for these sizes (of the pointers only past is looked at); negative: an error code. */
+int64_t tbs_attend_prompts_workspace(const tbs_attend_prompts_args *args);
 
 #ifdef __cplusplus
 }

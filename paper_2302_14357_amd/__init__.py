@@ -16,4 +16,4 @@ from .tbs import (  # noqa: F401
     KERNEL,
     EXPORTED_SYMBOLS,
 )
-from .ops import attend_paged, beam_reorder, beam_select, linear  # noqa: F401
+from .ops import attend_paged, attend_prompts, beam_reorder, beam_select, linear, page_slots, page_tables, rotary  # noqa: F401

@@ -285,14 +285,6 @@ k_linear_few(const T *__restrict__ x, const T *__restrict__ w, int64_t ld_x, int
 #define LT_VMCNT(n) (((n) & 15) | (7 << 4) | (15 << 8) | (((n) >> 4) << 14))   // ... all but n loads from memory
 __device__ const uint4 linear_zeros = {0, 0, 0, 0};
 
-// A direct load to LDS, 16 bytes a lane, lane l's at lds + 16 l.  The compiler, which does not see these loads for what they are, adds no
-// waits of its own: it would wait for all of them in front of every fragment read (it counts a direct load against any read
-// of the array), and the loads of the next K tiles would be on their way for half a K tile only.  Every wait stands in the kernel.
-__device__ __forceinline__ void lt_load(const char *from, unsigned lds) {
-    unsigned m0_was;   // (whatever the compiler may keep there)
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" : "=&s"(m0_was) : "s"(lds), "v"(from) : "memory");
-}
-
 // what lanes of a wave wrote to LDS is there for its others
 __device__ __forceinline__ void lt_wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -339,7 +331,7 @@ k_linear_stream(const char *__restrict__ x, const char *__restrict__ w, int64_t 
         for (int q = 0; q < L; ++q) {
             const bool behind = at + STEP > k_bytes && at + piece[q] >= k_bytes;   // (pieces behind K, in the last step only)
 #pragma unroll
-            for (int r = 0; r < R; ++r) lt_load(behind ? (const char *)&linear_zeros : p[r][q] + at, lds + (slot_in * R + r) * BLOCK + q * 1024);
+            for (int r = 0; r < R; ++r) op_load_lds(behind ? (const char *)&linear_zeros : p[r][q] + at, lds + (slot_in * R + r) * BLOCK + q * 1024);
         }
         slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
         ++asked;
@@ -401,12 +393,12 @@ k_linear_tile(const char *__restrict__ x, const char *__restrict__ w, int64_t ld
         }
 #pragma unroll
         for (int i = 0; i < RA; ++i) {
-            lt_load(pa[i], dst + i * 64 * LT_ROW);
+            op_load_lds(pa[i], dst + i * 64 * LT_ROW);
             pa[i] += LT_ROW;
         }
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            lt_load(pb[i], dst + (BM + i * 64) * LT_ROW);
+            op_load_lds(pb[i], dst + (BM + i * 64) * LT_ROW);
             pb[i] += LT_ROW;
         }
         ++asked;

@@ -1,5 +1,5 @@
-// What the operators of an autoregressive model (linear, attention over a paged cache, selection over a vocabulary) share: element
-// types, 16-byte pieces and the matrix instruction over them.
+// What the operators of an autoregressive model (linear, attention over a paged cache and of prompts, selection over a vocabulary) share: element
+// types, 16-byte pieces and the matrix instructions over them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -10,6 +10,7 @@
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 op_bf16x8;
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 op_f16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
 // A fragment is 16 bytes a lane: a piece of one row, row (lane & 15) of sixteen, piece (lane >> 4) of four.
 template <class T>
@@ -60,6 +61,90 @@ __device__ __forceinline__ floatx4 op_mma(const uint4 &a, const uint4 &b, floatx
         __builtin_memcpy(&y, &b, 16);
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
     }
+}
+
+// The same over two pieces a row and 32 rows of each side: a fragment is row (lane & 31), piece (lane >> 5) of two; a lane holds of column lane & 31, with
+// h = lane >> 5, the rows 8 (i / 4) + 4 h + i % 4 as its i-th number.
+template <class T>
+__device__ __forceinline__ floatx16 op_mma32(const uint4 &a, const uint4 &b, floatx16 c) {
+    if constexpr (sizeof(T) == 4) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    } else if constexpr (__is_same(T, __bf16)) {
+        op_bf16x8 x, y;
+        __builtin_memcpy(&x, &a, 16);
+        __builtin_memcpy(&y, &b, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+    } else {
+        op_f16x8 x, y;
+        __builtin_memcpy(&x, &a, 16);
+        __builtin_memcpy(&y, &b, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
+    }
+}
+
+// A direct load to LDS, 16 bytes a lane, lane l's at lds + 16 l.  The compiler, which does not see these loads for what they are, adds no
+// waits of its own: it would wait for all of them in front of every fragment read (it counts a direct load against any read
+// of the array), and the loads of what comes next would be on their way for a part of the time only.  Every wait stands in the kernel.
+__device__ __forceinline__ void op_load_lds(const char *from, unsigned lds) {
+    unsigned m0_was;   // (whatever the compiler may keep there)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" : "=&s"(m0_was) : "s"(lds), "v"(from) : "memory");
+}
+
+// Rows of bytes: whether two sets of them have one in common.  (Rows of one stride, as of two slices of a tensor, by what their distance leaves; others
+// row by row, where the memory between their ends overlaps at all.)
+struct OpRows {
+    const void *at;
+    int64_t rows, ld, width;
+};
+static inline bool op_overlap(OpRows a, OpRows b) {
+    if (a.rows > b.rows) {
+        const OpRows t = a;
+        a = b, b = t;
+    }
+    const int64_t d = (int64_t)((uintptr_t)b.at - (uintptr_t)a.at);
+    if (d >= (a.rows - 1) * a.ld + a.width || -d >= (b.rows - 1) * b.ld + b.width) return false;
+    auto floor_div = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };
+    if (a.ld == b.ld) {
+        const int64_t q = floor_div(d, a.ld), r = d - q * a.ld;   // row j of b begins r bytes behind row q + j of a
+        return (r < a.width && q < a.rows && q + b.rows > 0) || (r + b.width > a.ld && q + 1 < a.rows && q + 1 + b.rows > 0);
+    }
+    for (int64_t i = 0; i < a.rows; ++i) {
+        const int64_t s = i * a.ld - d;   // row i of a, from b's first byte
+        const int64_t first = floor_div(s - b.width, b.ld) + 1, last = floor_div(s + a.width - 1, b.ld);
+        if ((first > 0 ? first : 0) <= (last < b.rows ? last : b.rows - 1)) return true;
+    }
+    return false;
+}
+
+// [tokens, heads, dim] by elements, a head's side by side
+struct OpHeads {
+    const void *at;
+    int64_t tokens, heads, dim, row, head;
+};
+static inline bool op_same(const OpHeads &a, const OpHeads &b) {
+    return a.at == b.at && (a.row == b.row || a.tokens <= 1) && (a.head == b.head || a.heads <= 1);
+}
+// whether its heads may lie over each other: tokens in rows, or (a head's tokens together) heads in rows
+static inline bool op_folded(const OpHeads &a) {
+    const int64_t token = (a.heads > 1 ? (a.heads - 1) * a.head : 0) + a.dim, head = (a.tokens > 1 ? (a.tokens - 1) * a.row : 0) + a.dim;
+    const bool by_token = (a.heads <= 1 || a.head >= a.dim) && (a.tokens <= 1 || a.row >= token);
+    const bool by_head = (a.tokens <= 1 || a.row >= a.dim) && (a.heads <= 1 || a.head >= head);
+    return !by_token && !by_head;
+}
+// whether heads of the one lie over heads of the other: rows of a token's heads, or of a head's tokens, where both are that; all memory between first and last otherwise
+static inline bool op_overlap(const OpHeads &a, const OpHeads &b, int64_t size) {
+    if (a.tokens < 1 || b.tokens < 1) return false;
+    auto by = [&](const OpHeads &x, bool heads) {
+        const int64_t n = heads ? x.heads : x.tokens, m = heads ? x.tokens : x.heads, ld = heads ? x.head : x.row, in = heads ? x.row : x.head;
+        OpRows r = {x.at, n, ld * size, ((m - 1) * in + x.dim) * size};
+        if (r.rows > 1 && r.ld < r.width) r.width += (r.rows - 1) * r.ld, r.rows = 1;
+        if (r.rows == 1) r.ld = r.width;
+        return r;
+    };
+    return op_overlap(by(a, false), by(b, false)) && op_overlap(by(a, true), by(b, true));
 }
 
 static inline size_t op_dtype_size(int32_t dtype) { return dtype == TBS_F32 ? 4 : 2; }

@@ -78,6 +78,25 @@ int32_t size32(int64_t v, const char *name) {
     return (int32_t)v;
 }
 
+// a factor of the scores (None: 0, the library's own)
+float scale_of(PyObject *o) {
+    if (o == Py_None) return 0.f;
+    const double s = PyFloat_AsDouble(o);
+    if (s == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        WANT(false, "scale has to be a number");
+    }
+    WANT((float)s != 0.f, "scale has to be other than 0");
+    return (float)s;
+}
+
+// one number in int32
+int32_t *one_of(const Tensor &t, const char *name, const at::Device &d) {
+    WANT(t.scalar_type() == at::kInt && t.numel() == 1, name << ": one number in int32 is wanted");
+    on(t, name, d);
+    return (int32_t *)t.data_ptr();
+}
+
 Tensor made(at::IntArrayRef shape, at::ScalarType type, const at::Device &d) {
     return at::empty(shape, at::TensorOptions().dtype(type).device(d));
 }
@@ -260,15 +279,7 @@ PyObject *py_attend(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         a.page = size32(kc.size(1), "page"), a.pages = size32(kc.size(0), "pages"), a.table_width = size32(tables.size(1), "table width");
         a.max_len = o[9] == Py_None ? 0 : number(o[9], "max_len");
         a.beams = number(o[8], "beams");
-        if (o[7] != Py_None) {
-            const double s = PyFloat_AsDouble(o[7]);
-            if (s == -1.0 && PyErr_Occurred()) {
-                PyErr_Clear();
-                WANT(false, "scale has to be a number");
-            }
-            WANT((float)s != 0.f, "scale has to be other than 0");
-            a.scale = (float)s;
-        }
+        a.scale = scale_of(o[7]);
         if (rows > 0) {
             const Tensor work = workspace(tbs_attend_workspace, a, d);
             call(tbs_attend_paged, a, d);
@@ -374,9 +385,7 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
         a.ld_tables = rows_of(tables, "tables", rows, width);
         a.ld_out_tables = width;
         if (status) {
-            WANT(status->scalar_type() == at::kInt && status->numel() == 1, "status: one number in int32 is wanted");
-            on(*status, "status", d);
-            a.status = (int32_t *)status->data_ptr();
+            a.status = one_of(*status, "status", d);
         }
         a.rows = size32(rows, "rows"), a.beams = number(o[4], "beams"), a.table_width = size32(width, "table width");
         a.appended = appended;
@@ -396,6 +405,144 @@ PyObject *py_reorder(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
     });
 }
 
+// lens, page, width, beams, room, free, taken
+PyObject *py_tables(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+    return guarded([&]() -> PyObject * {
+        ARGS(7);
+        const Tensor &lens = *tensor(o[0], "lens"), &free = *tensor(o[5], "free"), &taken = *tensor(o[6], "taken");
+        const at::Device d = gpu(lens);
+        const int64_t prompts = lens.numel();
+        tbs_page_tables_args a = {};
+        a.lens = (const int32_t *)vector_of(lens, "lens", prompts, at::kInt, d);
+        a.free_pages = (const int32_t *)vector_of(free, "free", free.numel(), at::kInt, d);
+        a.taken = one_of(taken, "taken", d);
+        a.prompts = size32(prompts, "prompts"), a.page = number(o[1], "page"), a.table_width = number(o[2], "width"), a.beams = number(o[3], "beams"), a.room = number(o[4], "room");
+        a.free_count = size32(free.numel(), "free");
+        WANT(a.beams >= 1 && a.table_width >= 1, "beams = " << a.beams << ", width = " << a.table_width << ": 1 or more are wanted");
+        const int64_t rows = prompts * a.beams;
+        size32(rows, "prompts x beams");
+        Tensor t = made({rows, a.table_width}, at::kInt, d), n = made({rows}, at::kInt, d), now = made({1}, at::kInt, d);
+        a.tables = (int32_t *)t.data_ptr(), a.out_lens = (int32_t *)n.data_ptr(), a.out_taken = (int32_t *)now.data_ptr();
+        a.ld_tables = a.table_width;
+        call(tbs_page_tables, a, d);
+        return tuple_of({t, n, now});
+    });
+}
+
+// lens, tables, page, tokens, past
+PyObject *py_slots(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+    return guarded([&]() -> PyObject * {
+        ARGS(5);
+        const Tensor &lens = *tensor(o[0], "lens"), &tables = *tensor(o[1], "tables"), *past = tensor(o[4], "past", true);
+        const at::Device d = gpu(lens);
+        const int64_t prompts = lens.numel();
+        tbs_page_slots_args a = {};
+        a.lens = (const int32_t *)vector_of(lens, "lens", prompts, at::kInt, d);
+        if (past) a.past = (const int32_t *)vector_of(*past, "past", prompts, at::kInt, d);
+        WANT(tables.dim() == 2 && tables.scalar_type() == at::kInt, "tables [prompts, table width] in int32 is wanted");
+        on(tables, "tables", d);
+        a.ld_tables = rows_of(tables, "tables", prompts, tables.size(1));
+        a.tables = (const int32_t *)tables.data_ptr();
+        a.prompts = size32(prompts, "prompts"), a.page = number(o[2], "page"), a.tokens = number(o[3], "tokens"), a.table_width = size32(tables.size(1), "table width");
+        WANT(a.tokens >= 0, "tokens = " << a.tokens << ": 0 or more are wanted");
+        Tensor starts = made({prompts + 1}, at::kInt, d), positions = made({a.tokens}, at::kInt, d), slots = made({a.tokens}, at::kLong, d);
+        a.starts = (int32_t *)starts.data_ptr(), a.positions = (int32_t *)positions.data_ptr(), a.slots = (int64_t *)slots.data_ptr();
+        call(tbs_page_slots, a, d);
+        return tuple_of({starts, positions, slots});
+    });
+}
+
+// q, k, positions, freqs, interleaved, v, k_cache, v_cache, slots
+PyObject *py_rotary(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+    return guarded([&]() -> PyObject * {
+        ARGS(9);
+        const Tensor &q = *tensor(o[0], "q"), &k = *tensor(o[1], "k"), &positions = *tensor(o[2], "positions"), &freqs = *tensor(o[3], "freqs");
+        const Tensor *v = tensor(o[5], "v", true), *kc = tensor(o[6], "k_cache", true), *vc = tensor(o[7], "v_cache", true), *slots = tensor(o[8], "slots", true);
+        tbs_rotary_args a = {};
+        a.dtype = dtype_of(q, "q");
+        a.interleaved = PyObject_IsTrue(o[4]);
+        if (a.interleaved < 0) PyErr_Clear();
+        WANT(a.interleaved >= 0, "interleaved has to be True or False");
+        const at::ScalarType kind = q.scalar_type();
+        WANT(q.dim() == 3 && k.dim() == 3, "q [tokens, heads, dim] and k [tokens, kv_heads, dim] are wanted");
+        WANT(!v == !slots && !kc == !slots && !vc == !slots, "v, k_cache, v_cache and slots belong together");
+        const int64_t tokens = q.size(0), heads = q.size(1), dim = q.size(2), kv = k.size(1);
+        const at::Device d = gpu(q);
+        heads_of(q, "q", tokens, heads, dim, kind, d, a.q_row, a.q_head);
+        heads_of(k, "k", tokens, kv, dim, kind, d, a.k_row, a.k_head);
+        a.positions = (const int32_t *)vector_of(positions, "positions", tokens, at::kInt, d);
+        a.freqs = (const double *)vector_of(freqs, "freqs", freqs.numel(), at::kDouble, d);
+        WANT(2 * freqs.numel() <= dim, freqs.numel() << " frequencies for heads of " << dim << ": half as many at most are wanted");
+        a.tokens = size32(tokens, "tokens"), a.heads = size32(heads, "heads"), a.kv_heads = size32(kv, "kv_heads"), a.dim = size32(dim, "dim"), a.pairs = (int32_t)freqs.numel();
+        if (slots) {
+            heads_of(*v, "v", tokens, kv, dim, kind, d, a.v_row, a.v_head);
+            cache_of(*kc, "k_cache", kind, d, a.k_cache_page, a.k_cache_token, a.k_cache_head);
+            cache_of(*vc, "v_cache", kind, d, a.v_cache_page, a.v_cache_token, a.v_cache_head);
+            WANT(kc->size(2) == kv && kc->size(3) == dim && vc->sizes() == kc->sizes(), "k has " << kv << " heads of " << dim << ", k_cache is " << kc->sizes() << ", v_cache " << vc->sizes());
+            a.slots = (const int64_t *)vector_of(*slots, "slots", tokens, at::kLong, d);
+            a.pages = size32(kc->size(0), "pages"), a.page = size32(kc->size(1), "page");
+        }
+        Tensor q2 = made({tokens, heads, dim}, kind, d), k2 = made({tokens, kv, dim}, kind, d);
+        if (tokens > 0) {
+            a.q = q.data_ptr(), a.k = k.data_ptr(), a.q_out = q2.data_ptr(), a.k_out = k2.data_ptr();
+            a.q_out_row = heads * dim, a.q_out_head = dim, a.k_out_row = kv * dim, a.k_out_head = dim;
+            if (slots) a.v = v->data_ptr(), a.k_cache = kc->data_ptr(), a.v_cache = vc->data_ptr();
+            call(tbs_rotary, a, d);
+            if (slots) written(*kc), written(*vc);
+        }
+        return tuple_of({q2, k2});
+    });
+}
+
+// q, k, v, starts, past, k_cache, v_cache, tables, scale, out
+PyObject *py_prompts(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+    return guarded([&]() -> PyObject * {
+        ARGS(10);
+        const Tensor &q = *tensor(o[0], "q"), &k = *tensor(o[1], "k"), &v = *tensor(o[2], "v"), &starts = *tensor(o[3], "starts");
+        const Tensor *past = tensor(o[4], "past", true), *kc = tensor(o[5], "k_cache", true), *vc = tensor(o[6], "v_cache", true), *tables = tensor(o[7], "tables", true),
+                     *out = tensor(o[9], "out", true);
+        tbs_attend_prompts_args a = {};
+        a.dtype = dtype_of(q, "q");
+        const at::ScalarType kind = q.scalar_type();
+        WANT(q.dim() == 3 && k.dim() == 3, "q [tokens, heads, dim] and k [tokens, kv_heads, dim] are wanted");
+        WANT(!past == !kc && !past == !vc && !past == !tables, "past, k_cache, v_cache and tables belong together");
+        const int64_t tokens = q.size(0), heads = q.size(1), dim = q.size(2), kv = k.size(1), prompts = starts.numel() - 1;
+        const at::Device d = gpu(q);
+        heads_of(q, "q", tokens, heads, dim, kind, d, a.q_row, a.q_head);
+        heads_of(k, "k", tokens, kv, dim, kind, d, a.k_row, a.k_head);
+        heads_of(v, "v", tokens, kv, dim, kind, d, a.v_row, a.v_head);
+        WANT(prompts >= 0, "starts: the first tokens of all prompts and the first behind them are wanted");
+        a.starts = (const int32_t *)vector_of(starts, "starts", prompts + 1, at::kInt, d);
+        if (past) {
+            a.past = (const int32_t *)vector_of(*past, "past", prompts, at::kInt, d);
+            cache_of(*kc, "k_cache", kind, d, a.k_cache_page, a.k_cache_token, a.k_cache_head);
+            cache_of(*vc, "v_cache", kind, d, a.v_cache_page, a.v_cache_token, a.v_cache_head);
+            WANT(kc->size(2) == kv && kc->size(3) == dim && vc->sizes() == kc->sizes(), "k has " << kv << " heads of " << dim << ", k_cache is " << kc->sizes() << ", v_cache " << vc->sizes());
+            WANT(tables->dim() == 2 && tables->scalar_type() == at::kInt, "tables [prompts, table width] in int32 is wanted");
+            on(*tables, "tables", d);
+            a.ld_tables = rows_of(*tables, "tables", prompts, tables->size(1));
+            a.pages = size32(kc->size(0), "pages"), a.page = size32(kc->size(1), "page"), a.table_width = size32(tables->size(1), "table width");
+            if (prompts > 0) a.tables = (const int32_t *)tables->data_ptr(), a.k_cache = kc->data_ptr(), a.v_cache = vc->data_ptr();
+            else a.past = nullptr;
+        }
+        Tensor result = out ? *out : made({tokens, heads, dim}, kind, d);
+        heads_of(result, "out", tokens, heads, dim, kind, d, a.out_row, a.out_head);
+        a.q = q.data_ptr(), a.k = k.data_ptr(), a.v = v.data_ptr(), a.out = result.data_ptr();
+        a.tokens = size32(tokens, "tokens"), a.prompts = size32(prompts, "prompts"), a.heads = size32(heads, "heads"), a.kv_heads = size32(kv, "kv_heads"), a.dim = size32(dim, "dim");
+        a.scale = scale_of(o[8]);
+        if (tokens > 0) {
+            const Tensor work = workspace(tbs_attend_prompts_workspace, a, d);
+            call(tbs_attend_prompts, a, d);
+        }
+        if (out) {
+            written(*out);
+            Py_INCREF(o[9]);
+            return o[9];
+        }
+        return THPVariable_Wrap(std::move(result));
+    });
+}
+
 PyObject *py_raise_by(PyObject *, PyObject *f) {
     Py_XDECREF(g_raise);
     Py_INCREF(f);
@@ -407,6 +554,10 @@ PyMethodDef methods[] = {{"linear", (PyCFunction)(void *)py_linear, METH_FASTCAL
                          {"attend_paged", (PyCFunction)(void *)py_attend, METH_FASTCALL, nullptr},
                          {"beam_select", (PyCFunction)(void *)py_select, METH_FASTCALL, nullptr},
                          {"beam_reorder", (PyCFunction)(void *)py_reorder, METH_FASTCALL, nullptr},
+                         {"page_tables", (PyCFunction)(void *)py_tables, METH_FASTCALL, nullptr},
+                         {"page_slots", (PyCFunction)(void *)py_slots, METH_FASTCALL, nullptr},
+                         {"rotary", (PyCFunction)(void *)py_rotary, METH_FASTCALL, nullptr},
+                         {"attend_prompts", (PyCFunction)(void *)py_prompts, METH_FASTCALL, nullptr},
                          {"raise_by", py_raise_by, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbs_ops", nullptr, -1, methods};

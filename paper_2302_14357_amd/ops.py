@@ -1,5 +1,6 @@
 """Operators of an autoregressive model beside the search (include/tbs.h): products with their epilogue, attention of one
-new token over a paged cache, selection over beams and vocabulary, reordering of the cached states.
+new token over a paged cache, selection over beams and vocabulary, reordering of the cached states; and for prompts, before the first step: their
+pages, the places of a packed batch's tokens, rotary positions, causal attention.
 
 Each function checks its tensors, makes the outputs and enqueues the kernels on the current stream of the tensors' device; nothing
 synchronises.  They serve and have no gradients: with grad mode on, a tensor that requires one is refused.  What the library refuses is a TbsError, a tensor of the wrong type, shape or device a ValueError.
@@ -39,6 +40,30 @@ class _Reorder(C.Structure):
     _fields_ = ([(n, _P) for n in ("parents", "tables", "lens", "finished", "out_tables", "out_lens", "status", "caches")] +
                 [(n, _I64) for n in ("cache_page", "cache_token", "cache_head", "ld_tables", "ld_out_tables")] +
                 [(n, _I32) for n in ("n_caches", "rows", "beams", "table_width", "pages", "page", "kv_heads", "dim", "dtype", "appended")])
+
+
+class _Tables(C.Structure):
+    _fields_ = ([(n, _P) for n in ("lens", "free_pages", "taken", "tables", "out_lens", "out_taken")] + [("ld_tables", _I64)] +
+                [(n, _I32) for n in ("prompts", "beams", "page", "table_width", "room", "free_count")])
+
+
+class _Slots(C.Structure):
+    _fields_ = ([(n, _P) for n in ("lens", "past", "tables", "starts", "positions", "slots")] + [("ld_tables", _I64)] +
+                [(n, _I32) for n in ("prompts", "tokens", "page", "table_width")])
+
+
+class _Rotary(C.Structure):
+    _fields_ = ([(n, _P) for n in ("q", "k", "v", "positions", "freqs", "slots", "q_out", "k_out", "k_cache", "v_cache")] +
+                [(n, _I64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "q_out_row", "q_out_head", "k_out_row", "k_out_head",
+                                     "k_cache_page", "k_cache_token", "k_cache_head", "v_cache_page", "v_cache_token", "v_cache_head")] +
+                [(n, _I32) for n in ("tokens", "heads", "kv_heads", "dim", "pairs", "interleaved", "pages", "page", "dtype")])
+
+
+class _Prompts(C.Structure):
+    _fields_ = ([(n, _P) for n in ("q", "k", "v", "k_cache", "v_cache", "starts", "past", "tables", "out", "workspace")] +
+                [(n, _I64) for n in ("workspace_bytes", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row", "out_head", "k_cache_page",
+                                     "k_cache_token", "k_cache_head", "v_cache_page", "v_cache_token", "v_cache_head", "ld_tables")] +
+                [(n, _I32) for n in ("tokens", "prompts", "heads", "kv_heads", "dim", "page", "pages", "table_width", "dtype")] + [("scale", C.c_float)])
 
 
 _binding = None
@@ -111,3 +136,46 @@ def beam_reorder(parents, tables, lens, caches, *, beams, finished=None, appende
     where `(lens == -1) & ~finished`, give the score -inf before the next beam_select.
     """
     return (_binding or _load()).beam_reorder(parents, tables, lens, caches, beams, finished, appended, status)
+
+
+def page_tables(lens, *, page, width, free, taken, beams=1, room=0):
+    """Pages for prompts: (tables int32 [prompts * beams, width], lens int32 [prompts * beams], taken int32 [1]), new tensors.
+
+    lens int32 [prompts], the tokens of each (negative: there is none); free int32, page numbers, of which the first `taken` (int32, one number)
+    are in use; the returned one is the next call's.  A prompt's `beams` rows share its full pages and have the others, for its last tokens and `room`
+    more, for themselves, as beam_reorder wants them.  The first row's length is the prompt's, the others are places without a hypothesis yet (length -1:
+    give them the score -inf at the first beam_select).  A prompt that finds no pages, or wants more than `width` a row, has lengths of -1 and tables of -1.
+    """
+    return (_binding or _load()).page_tables(lens, page, width, beams, room, free, taken)
+
+
+def page_slots(lens, tables, *, page, tokens, past=None):
+    """Where the tokens of a packed batch stand and go: (starts int32 [prompts + 1], positions int32 [tokens], slots int64 [tokens]).
+
+    lens int32 [prompts], the new tokens of each prompt, which lie one prompt after the other; tables int32 [prompts, table width] (of page_tables' rows
+    every `beams`-th one: tables[::beams]); past int32 [prompts], tokens that are in the cache before them.  `tokens` is the batch's size: tokens behind the last
+    prompt have the position and the slot -1, as have the slots of tokens without a page.
+    """
+    return (_binding or _load()).page_slots(lens, tables, page, tokens, past)
+
+
+def rotary(q, k, positions, freqs, *, interleaved=False, v=None, k_cache=None, v_cache=None, slots=None):
+    """Queries and keys turned by their positions: (q, k), new tensors; with `slots` the keys and the values `v` are written to the caches as well.
+
+    q [tokens, heads, dim], k and v [tokens, kv_heads, dim] in one of float32, bfloat16 and float16, positions int32 [tokens], freqs float64 [pairs], the radians
+    a position of each pair: base ** -(arange(pairs) / pairs) for instance, or what a long context makes of them.  Elements j and pairs + j of a head are a pair, with
+    interleaved 2 j and 2 j + 1; elements from 2 * pairs on stay as they are (no pairs at all: a copy into the cache).  k_cache and v_cache [pages, page, kv_heads, dim] in any
+    strides, a head's elements side by side; slots int64 [tokens] as page_slots gives them, -1 for a token that is not written.
+    """
+    return (_binding or _load()).rotary(q, k, positions, freqs, interleaved, v, k_cache, v_cache, slots)
+
+
+def attend_prompts(q, k, v, starts, *, past=None, k_cache=None, v_cache=None, tables=None, scale=None, out=None):
+    """Causal attention of packed prompts, [tokens, heads, dim] (`out`, which may be `q`).
+
+    q [tokens, heads, dim], k and v [tokens, kv_heads, dim] in one of float32, bfloat16 and float16; starts int32 [prompts + 1], the first token of each prompt and the
+    first behind all.  Where a prompt has tokens before these in a paged cache: past int32 [prompts], their number, k_cache and v_cache [pages, page, kv_heads, dim] and
+    tables int32 [prompts, table width] (all four, or none).  Every token attends to what came before it in its prompt and to itself.  Rows of no prompt are 0.
+    include/tbs.h says what holds at the edges.
+    """
+    return (_binding or _load()).attend_prompts(q, k, v, starts, past, k_cache, v_cache, tables, scale, out)

@@ -17,6 +17,7 @@ EXPORTED_SYMBOLS = [
     "tbs_strerror", "tbs_last_hip_error", "tbs_gemm_bf16", "tbs_stream_begin", "tbs_push_segment",
     "tbs_profile_overhead", "tbs_debug_hyps_noalloc", "tbs_path", "tbs_one_launch",
     "tbs_linear", "tbs_attend_paged", "tbs_attend_workspace", "tbs_beam_select", "tbs_beam_select_workspace", "tbs_beam_reorder",
+    "tbs_page_tables", "tbs_page_slots", "tbs_rotary", "tbs_attend_prompts", "tbs_attend_prompts_workspace",
 ]
 
 TBS_MAX_LAYERS = 4
@@ -97,9 +98,9 @@ def load_library():
     L.tbs_strerror.restype = C.c_char_p
     L.tbs_last_hip_error.argtypes = [vp]
     L.tbs_gemm_bf16.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
-    for name in ("tbs_linear", "tbs_attend_paged", "tbs_beam_select", "tbs_beam_reorder"):
+    for name in ("tbs_linear", "tbs_attend_paged", "tbs_beam_select", "tbs_beam_reorder", "tbs_page_tables", "tbs_page_slots", "tbs_rotary", "tbs_attend_prompts"):
         getattr(L, name).argtypes = [vp, vp]
-    for name in ("tbs_attend_workspace", "tbs_beam_select_workspace"):
+    for name in ("tbs_attend_workspace", "tbs_beam_select_workspace", "tbs_attend_prompts_workspace"):
         getattr(L, name).argtypes = [vp]
         getattr(L, name).restype = C.c_int64
     _lib = L

@@ -1,0 +1,464 @@
+"""The operators that bring prompts into the paged cache against plain implementations in 64 bits.
+
+Tolerances are sums of what can be lost: half a step of the output's type (eps / 2 relative), float32 sums of n terms (n 2^-24 of the sum of
+their magnitudes), and what is named where it is used.  Whole numbers, written cache entries and copied elements are equal.
+"""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _randn(g, *shape, dtype=torch.float32, scale=1.0):
+    return (torch.randn(shape, generator=g) * scale).to(dtype)
+
+
+def _half_step(ref, dtype):
+    """Half a step of the type at ref (and of its smallest numbers)."""
+    return ref.abs() * (torch.finfo(dtype).eps / 2) + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2
+
+
+def _close(got, ref, tol):
+    off = (got.double().cpu() - ref).abs()
+    assert torch.isfinite(got.float()).all()
+    assert bool((off <= tol).all()), (float((off - tol).max()), float((off / tol.clamp(min=1e-300)).max()))
+
+
+def _i32(x):
+    return torch.tensor(np.asarray(x, np.int32)).cuda()
+
+
+# ------------------------------------------------------------------ pages for prompts
+
+def _tables_ref(lens, beams, page, width, room, free, taken):
+    tables, out = np.full((len(lens) * beams, width), -1, np.int64), np.full(len(lens) * beams, -1, np.int64)
+    at = now = max(taken, 0)
+    for i, n in enumerate(lens):
+        if n < 0:
+            continue
+        whole, need = n // page, -(-(n + room) // page)
+        if need > width:
+            continue
+        count = whole + beams * (need - whole)
+        first, at = at, at + count
+        if count and at > len(free):
+            continue
+        now = at if count else now
+        out[i * beams] = n
+        for b in range(beams):
+            tables[i * beams + b, :whole] = free[first:first + whole]
+            tables[i * beams + b, whole:need] = free[first + whole + b * (need - whole):first + whole + (b + 1) * (need - whole)]
+    return tables, out, now
+
+
+def _tables_check(lens, *, beams=1, page=16, width, room=0, free=None, taken=0, seed=0):
+    from paper_2302_14357_amd import page_tables
+    r = np.random.default_rng(seed)
+    need = sum(max(n, 0) // page + beams * ((max(n, 0) + room) // page + 1) for n in lens)
+    pages = r.permutation(max(taken, 0) + need + 5 if free is None else free).astype(np.int32)
+    f, t = _i32(pages), _i32([taken])
+    tables, out, now = page_tables(_i32(lens), page=page, width=width, beams=beams, room=room, free=f, taken=t)
+    want = _tables_ref(lens, beams, page, width, room, pages, taken)
+    assert tables.dtype == out.dtype == now.dtype == torch.int32 and tables.shape == (len(lens) * beams, width) and now.shape == (1,)
+    assert np.array_equal(tables.cpu().numpy(), want[0]) and np.array_equal(out.cpu().numpy(), want[1]) and int(now) == want[2]
+    assert torch.equal(f.cpu(), torch.from_numpy(pages)) and int(t) == taken
+
+
+@pytest.mark.parametrize("beams", [1, 2, 5, 32])
+@pytest.mark.parametrize("page", [1, 3, 16, 64])
+def test_tables(beams, page):
+    r = np.random.default_rng(beams * 100 + page)
+    _tables_check([37], beams=beams, page=page, width=60, room=10)
+    _tables_check([0], beams=beams, page=page, width=1)
+    _tables_check([0, 16, 15, 17, -1, 48, ~5, 1], beams=beams, page=page, width=150, room=100, taken=9)
+    _tables_check(list(r.integers(-3, 200, 300)), beams=beams, page=page, width=240, room=7, seed=1)
+    _tables_check(list(r.integers(0, 200, 65)), beams=beams, page=page, width=100, room=33, seed=2)   # (some want more than a table holds)
+
+
+def test_tables_where_the_list_ends():
+    r = np.random.default_rng(3)
+    for free in (0, 1, 7, 8, 50, 399, 400):
+        _tables_check([40, 0, 17, -1, 3, 0, 90] * 3, beams=3, page=8, width=20, room=5, free=free, taken=0, seed=free)
+        _tables_check([40, 0, 17, -1, 3, 0, 90] * 3, beams=3, page=8, width=20, room=0, free=free, taken=min(5, free), seed=free)
+    _tables_check([5, 6], page=4, width=3, free=10, taken=11)      # all are taken, and more
+    _tables_check([5, 6], page=4, width=3, free=10, taken=-4)      # (a negative number counts as 0)
+    _tables_check([], page=4, width=3, free=10, taken=2)
+    _tables_check([-1, -7], page=4, width=3, free=10, taken=2)
+    _tables_check([2**31 - 1, 2**30, 12], page=65536, width=3, room=2**30, free=10, taken=2)
+    _tables_check(list(r.integers(0, 60, 5000)), beams=2, page=8, width=9, room=9, free=20000, taken=2)
+
+
+@pytest.mark.parametrize("prompts", [1023, 1025, 2500, 70001])
+def test_tables_of_many_prompts(prompts):
+    _tables_check(list(np.random.default_rng(prompts).integers(-2, 40, prompts)), beams=2, page=16, width=4, room=20)
+
+
+# ------------------------------------------------------------------ the places of a packed batch's tokens
+
+def _slots_check(lens, *, past=None, page, width, tokens=None, every=1, seed=0):
+    from paper_2302_14357_amd import page_slots
+    r = np.random.default_rng(seed)
+    tokens = int(sum(max(n, 0) for n in lens)) if tokens is None else tokens
+    tables = r.integers(0, 2**31 // page, (len(lens), width)).astype(np.int32)
+    tables[r.random(tables.shape) < 0.1] = -1
+    td = torch.full((len(lens) * every, width), 77, dtype=torch.int32, device="cuda")
+    td[::every] = _i32(tables)
+    starts, positions, slots = page_slots(_i32(lens), td[::every], page=page, tokens=tokens, past=None if past is None else _i32(past))
+    assert starts.dtype == positions.dtype == torch.int32 and slots.dtype == torch.int64
+    n = np.maximum(np.asarray(lens, np.int64).reshape(-1), 0)
+    edge = np.concatenate([[0], np.cumsum(n)])
+    assert np.array_equal(starts.cpu().numpy(), np.minimum(edge, tokens))
+    t = np.arange(min(int(edge[-1]), tokens))
+    prompt = np.searchsorted(edge[1:], t, side="right")
+    pos = t - edge[prompt] + (0 if past is None else np.maximum(np.asarray(past, np.int64), 0)[prompt])
+    want_p, want_s = np.full(tokens, -1, np.int64), np.full(tokens, -1, np.int64)
+    want_p[:len(t)] = pos
+    column = pos // page
+    entry = tables[prompt, np.minimum(column, width - 1)].astype(np.int64)
+    want_s[:len(t)] = np.where((column < width) & (entry >= 0), entry * page + pos % page, -1)
+    assert np.array_equal(positions.cpu().numpy(), want_p) and np.array_equal(slots.cpu().numpy(), want_s)
+
+
+@pytest.mark.parametrize("page", [1, 7, 16, 64, 65536])
+def test_slots(page):
+    r = np.random.default_rng(page)
+    _slots_check([1], page=page, width=1)
+    _slots_check([40], page=page, width=4)
+    _slots_check([0, 0, 5, 0, 1, 200, 0], page=page, width=20)
+    _slots_check([3, -4, 9], page=page, width=5, past=[10, 2, -8])
+    _slots_check(list(r.integers(0, 30, 300)), page=page, width=10, past=r.integers(0, 60, 300), every=5)
+    _slots_check(list(r.integers(0, 30, 50)), page=page, width=10, tokens=2000)
+    _slots_check(list(r.integers(0, 30, 50)), page=page, width=10, tokens=300)       # (a batch that ends inside a prompt)
+
+
+def test_slots_at_the_edges():
+    _slots_check([], page=4, width=3, tokens=5)
+    _slots_check([4, 5], page=4, width=3, tokens=0)
+    _slots_check([0, 0], page=4, width=3)
+    _slots_check([2**31 - 1, 2**31 - 1, 2**31 - 1], page=4, width=3, tokens=3000)
+    _slots_check([500], page=65536, width=2**14, past=[2**30 - 501])
+    for n in (1023, 1024, 1025, 2048, 3000, 70000):
+        _slots_check(list(np.random.default_rng(n).integers(0, 4, n)), page=2, width=2)
+        _slots_check([0] * n + [7], page=2, width=3)
+    _slots_check([5000, 1, 70000, 1023, 1025], page=16, width=5000, past=[3, 1, 0, 9, 12])
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def _rotary_check(tokens, heads, kv, dim, pairs, dtype, *, interleaved=False, cache=None, far=100, base=10000.0, layout="fused", shift=0, seed=0):
+    """cache: None, or (pages, page, layout)."""
+    from paper_2302_14357_amd import rotary
+    g = _gen(seed + tokens + dim)
+    qkv = _randn(g, tokens, heads + 2 * kv, dim, dtype=dtype)
+    room = torch.empty(qkv.numel() + shift, dtype=dtype, device="cuda")[shift:].view(qkv.shape).copy_(qkv)
+    q, k, v = room[:, :heads], room[:, heads:heads + kv], room[:, heads + kv:]
+    if layout == "heads":   # a head's tokens together
+        q, k, v = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    positions = torch.randint(-3, far + 1, (tokens,), generator=g, dtype=torch.int32)
+    freqs = base ** -(torch.arange(pairs, dtype=torch.float64) / max(pairs, 1))
+    kw = {}
+    if cache:
+        pages, page, kind = cache
+        slots = torch.randperm(pages * page, generator=g)[:tokens].clone()
+        for i, bad in enumerate((-1, pages * page, 2**62, -2**63)):
+            slots[i + 1::11] = bad
+        shape = (pages, page, kv, dim)
+        if kind == "head":
+            kc, vc = (torch.full((pages, kv, page, dim), 77.0, dtype=dtype, device="cuda").transpose(1, 2) for _ in range(2))
+        elif kind == "both":
+            both = torch.full((pages * page * kv * 2 * dim + 1,), 77.0, dtype=dtype, device="cuda")[1:].view(pages, page, kv, 2, dim)
+            kc, vc = both[..., 0, :], both[..., 1, :]
+        else:
+            kc, vc = (torch.full(shape, 77.0, dtype=dtype, device="cuda") for _ in range(2))
+        kw = dict(v=v, k_cache=kc, v_cache=vc, slots=slots.cuda())
+    before = room.clone()
+    got = rotary(q, k, positions.cuda(), freqs.cuda(), interleaved=interleaved, **kw)
+    assert torch.equal(room, before)
+    angle = positions.double()[:, None, None] * freqs
+    c, s = torch.cos(angle), torch.sin(angle)
+    a_at, b_at = (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2)) if interleaved else (slice(0, pairs), slice(pairs, 2 * pairs))
+    for x, y in zip((qkv[:, :heads], qkv[:, heads:heads + kv]), got):
+        assert y.shape == x.shape and y.dtype == dtype and y.is_contiguous()
+        ref = x.double()
+        tol = torch.zeros_like(ref)
+        a, b = ref[..., a_at].clone(), ref[..., b_at].clone()
+        ref[..., a_at], ref[..., b_at] = a * c - b * s, b * c + a * s
+        # sine and cosine within four units of float32 at 1, two roundings of the products; the reference's own angle: 2^-53 of it, twice
+        loss = (a.abs() + b.abs()) * (4 * 2.0**-24 + 2 * 2.0**-24 + angle.abs() * 2.0**-51)
+        tol[..., a_at], tol[..., b_at] = loss, loss
+        _close(y, ref, tol + torch.where(tol > 0, _half_step(ref, dtype) * (1 + 2.0**-10), 0.0) + (tol > 0) * 1e-40)
+        assert torch.equal(y[..., 2 * pairs:].cpu(), x[..., 2 * pairs:])
+    if cache:
+        for cache_, new in ((kc, got[1]), (vc, v)):
+            want = torch.full((pages * page, kv, dim), 77.0, dtype=dtype, device="cuda")
+            ok = ((slots >= 0) & (slots < pages * page)).cuda()
+            want[slots.cuda()[ok]] = new[ok]
+            assert torch.equal(cache_.reshape(pages * page, kv, dim), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,kv,dim,pairs", [(1, 1, 1, 2, 1), (5, 8, 2, 64, 32), (7, 3, 3, 80, 16), (40, 4, 1, 128, 64), (33, 5, 5, 96, 17), (9, 2, 1, 37, 18), (3, 2, 2, 512, 256),
+                                                       (6, 1, 1, 8, 0), (300, 16, 2, 256, 32), (4, 2, 1, 20, 3), (2100, 6, 2, 64, 32)])
+def test_rotary_sizes(tokens, heads, kv, dim, pairs, interleaved, dtype):
+    _rotary_check(tokens, heads, kv, dim, pairs, dtype, interleaved=interleaved)
+    _rotary_check(tokens, heads, kv, dim, pairs, dtype, interleaved=interleaved, cache=(tokens // 3 + 2, 7, "token"), seed=1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("layout,shift,kind", [("heads", 0, "head"), ("fused", 1, "both"), ("fused", 3, "token"), ("heads", 8, "both")])
+def test_rotary_layouts(layout, shift, kind, interleaved, dtype):
+    for dim, pairs in ((64, 32), (40, 9), (48, 24)):
+        _rotary_check(50, 6, 3, dim, pairs, dtype, interleaved=interleaved, cache=(5, 16, kind), layout=layout, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rotary_far_positions(dtype):
+    for base, far in ((10000.0, 10**6), (500000.0, 2**31 - 10), (1.0, 10**5)):
+        _rotary_check(200, 2, 1, 64, 32, dtype, far=far, base=base)
+
+
+def test_rotary_of_no_tokens_and_numbers_that_are_none():
+    from paper_2302_14357_amd import rotary
+    q, k = rotary(torch.empty(0, 4, 64, device="cuda"), torch.empty(0, 2, 64, device="cuda"), _i32([]), torch.ones(32, dtype=torch.float64, device="cuda"))
+    assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
+    x = torch.ones(3, 2, 16, device="cuda")
+    x[1, 0, 3] = math.nan
+    x[2, 1, 15] = math.inf
+    q, k = rotary(x, x, _i32([0, 1, 2]), torch.ones(4, dtype=torch.float64, device="cuda"))   # 4 pairs: elements 3 and 7 belong together
+    bad = ~torch.isfinite(q.cpu())
+    want = torch.zeros(3, 2, 16, dtype=torch.bool)
+    want[1, 0, 3] = want[1, 0, 7] = want[2, 1, 15] = True
+    assert torch.equal(bad, want) and torch.equal(torch.isnan(k), torch.isnan(q))
+
+
+# ------------------------------------------------------------------ attention of whole prompts
+
+def _prompts_ref(q, k, v, lens, past, kc, vc, tables, page, scale, dtype):
+    """(reference, tolerance) in float64 on the CPU, for packed prompts from row 0 on."""
+    tokens, heads, dim = q.shape
+    kv = k.shape[1]
+    ref, tol = torch.zeros(tokens, heads, dim, dtype=torch.float64), torch.zeros(tokens, heads, dim, dtype=torch.float64)
+    s = scale if scale is not None else 1 / math.sqrt(dim)
+    at = 0
+    for i, n in enumerate(lens):
+        if n == 0:
+            continue
+        had = past[i] if past is not None else 0
+        keys, vals, there = k[at:at + n], v[at:at + n], torch.ones(n, dtype=torch.bool)
+        if had:
+            t = torch.arange(had)
+            id_ = torch.full((had,), -1, dtype=torch.long)
+            inside = t // page < tables.shape[1]
+            id_[inside] = tables[i][(t // page)[inside]].long()
+            ok = (id_ >= 0) & (id_ < kc.shape[0])
+            old = [torch.where(ok[:, None, None], c[id_.clamp(0, kc.shape[0] - 1), t % page], torch.zeros((), dtype=dtype)) for c in (kc, vc)]
+            keys, vals, there = torch.cat([old[0], keys]), torch.cat([old[1], vals]), torch.cat([ok, there])
+        x = q[at:at + n].double().transpose(0, 1)                                                             # [heads, n, dim]
+        y, z = (u.double().repeat_interleave(heads // kv, 1).transpose(0, 1) for u in (keys, vals))           # [heads, keys, dim]
+        sees = there[None, :] & (torch.arange(had + n)[None, :] <= had + torch.arange(n)[:, None])
+        score = s * (x @ y.transpose(1, 2))
+        p = torch.softmax(score.masked_fill(~sees, -math.inf), -1)
+        # a score's error: a float32 sum of dim terms, its scaling (two units) and the exponential's argument; then the weight's rounding to its type (fp16: and
+        # of the smallest weights to steps of 2^-25, at a largest one of 2^7 or more), and sums over the keys and the tiles
+        e = (abs(s) * (dim + 2) * 2.0**-24 * (x.abs() @ y.abs().transpose(1, 2))).masked_fill(~sees, 0).amax(-1) + score.masked_fill(~sees, 0).abs().amax(-1) * 2.0**-21 + 2.0**-22
+        size = p @ z.abs()
+        ref[at:at + n] = (p @ z).transpose(0, 1)
+        more = 2 * e + (had + n + 64) * 2.0**-23 + (torch.finfo(dtype).eps / 2 * (1 + 2.0**-7) if dtype != torch.float32 else 0)
+        least = (had + n) * 2.0**-32 * z.abs().amax(1, keepdim=True) if dtype == torch.float16 else 0
+        tol[at:at + n] = (more[..., None] * size + least).transpose(0, 1)
+        at += n
+    return ref, tol + _half_step(ref, dtype) * (1 + 2.0**-6) + 1e-30
+
+
+def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, layout="plain", cache_layout="token", holes=(), scale=None, seed=0, q_scale=1.0, into=None, width=0, shift=0):
+    """lens: new tokens of every prompt; past: tokens of each in the cache; pad: rows behind the last; holes: (prompt, column) entries that name no page;
+    into: None, "out" (with room around every head) or "q"."""
+    from paper_2302_14357_amd import attend_prompts
+    g, r = _gen(seed + dim + page + sum(lens)), np.random.default_rng(seed + len(lens))
+    tokens = sum(lens) + pad
+    qkv = _randn(g, tokens, heads + 2 * kv, dim, dtype=dtype)
+    qkv[:, :heads] *= q_scale
+    if pad:
+        qkv[sum(lens):] = math.nan
+    q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+    room = torch.empty(qkv.numel() + shift, dtype=dtype, device="cuda")[shift:].view(qkv.shape).copy_(qkv)
+    qd, kd, vd = room[:, :heads], room[:, heads:heads + kv], room[:, heads + kv:]
+    if layout == "plain":
+        qd, kd, vd = (x.contiguous() for x in (qd, kd, vd))
+    elif layout == "heads":
+        qd, kd, vd = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (qd, kd, vd))
+    kw, kc, vc, tables = {}, None, None, None
+    if past is not None:
+        width = max(width, -(-max(past) // page), 1)
+        pages = len(lens) * width + 3
+        tables = r.permutation(pages)[:len(lens) * width].reshape(len(lens), width).astype(np.int32)
+        kc, vc = _randn(g, pages, page, kv, dim, dtype=dtype), _randn(g, pages, page, kv, dim, dtype=dtype)
+        seen = np.zeros((pages, page), bool)
+        for i, n in enumerate(past):
+            t = np.arange(min(n, width * page))
+            seen[tables[i, t // page], t % page] = True
+        kc[torch.from_numpy(~seen)], vc[torch.from_numpy(~seen)] = math.nan, math.inf   # what nobody may look at
+        for i, j in holes:
+            tables[i, j] = (-1, pages, -2**31, 2**31 - 1)[(i + j) % 4]
+        kcd, vcd = kc.cuda(), vc.cuda()
+        if cache_layout == "head":
+            kcd, vcd = (t.transpose(1, 2).contiguous().transpose(1, 2) for t in (kcd, vcd))
+        elif cache_layout == "both":
+            both = torch.empty(pages * page * kv * 2 * dim + 1, dtype=dtype, device="cuda")[1:].view(pages, page, kv, 2, dim)
+            kcd, vcd = both[..., 0, :].copy_(kcd), both[..., 1, :].copy_(vcd)
+        kw = dict(past=_i32(past), k_cache=kcd, v_cache=vcd, tables=_i32(tables))
+        tables = torch.from_numpy(tables)
+    starts = _i32(np.concatenate([[0], np.cumsum(lens)]) if len(lens) else [0])
+    before = [t.clone() for t in (kd, vd)]
+    plain = attend_prompts(qd, kd, vd, starts, scale=scale, **kw)
+    assert torch.equal(kd.nan_to_num(nan=5e4), before[0].nan_to_num(nan=5e4)) and torch.equal(vd.nan_to_num(nan=5e4), before[1].nan_to_num(nan=5e4))
+    if into == "out":
+        big = torch.full((tokens + 2, heads + 1, dim + 8), 77.0, dtype=dtype, device="cuda")
+        out = big[1:tokens + 1, :heads, :dim]
+        assert attend_prompts(qd, kd, vd, starts, scale=scale, out=out, **kw) is out
+        assert torch.equal(out, plain)
+        out.fill_(77.0)
+        assert bool((big == 77.0).all())
+    elif into == "q":
+        assert attend_prompts(qd, kd, vd, starts, scale=scale, out=qd, **kw) is qd
+        assert torch.equal(qd, plain)
+    else:
+        assert torch.equal(attend_prompts(qd, kd, vd, starts, scale=scale, **kw), plain)
+    ref, tol = _prompts_ref(q, k, v, lens, past, kc, vc, tables, page, scale, dtype)
+    _close(plain, ref, tol)
+    assert bool((plain[sum(lens):] == 0).all())
+    return plain
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv,dim", [(1, 1, 64), (8, 2, 32), (8, 8, 64), (4, 1, 128), (6, 2, 80), (3, 1, 96), (5, 5, 24), (4, 4, 8), (4, 2, 256), (2, 1, 136), (24, 1, 40), (16, 2, 128)])
+def test_prompts_heads(heads, kv, dim, dtype):
+    _prompts_case([1, 37, 0, 64, 130], heads=heads, kv=kv, dim=dim, dtype=dtype, pad=5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens", [[1], [2], [0], [0, 0, 3], [31, 32, 33], [63, 64, 65], [127, 128, 129, 1], [255, 257], [700], [1] * 70, [5] * 130 + [0] * 10 + [300], []])
+def test_prompts_lengths(lens, dtype):
+    _prompts_case(lens, heads=4, kv=2, dim=64, dtype=dtype, pad=0 if lens else 3)
+    _prompts_case(lens, heads=2, kv=2, dim=128, dtype=dtype, pad=200)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,past,page,dim", [([5], [20], 16, 64), ([1, 1, 1], [0, 15, 500], 16, 128), ([40, 0, 70, 3], [100, 50, 0, 63], 7, 32), ([64, 64], [64, 128], 64, 128), ([33, 2], [31, 999], 1, 80),
+                                                ([10, 20], [48, 1], 48, 256), ([130], [70], 128, 96), ([3, 100], [1000, 1], 100, 128)])
+@pytest.mark.parametrize("cache_layout", ["token", "head", "both"])
+def test_prompts_behind_a_cache(lens, past, page, dim, cache_layout, dtype):
+    _prompts_case(lens, past=past, page=page, heads=6, kv=2, dim=dim, dtype=dtype, cache_layout=cache_layout, pad=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_pages_that_do_not_exist(dtype):
+    _prompts_case([20, 9, 70], past=[100, 40, 64], page=16, heads=4, kv=2, dim=64, dtype=dtype, holes=[(0, 0), (0, 3), (0, 6), (1, 0), (1, 1), (1, 2), (2, 1)])
+    _prompts_case([20, 9], past=[300, 40], page=1, heads=4, kv=4, dim=32, dtype=dtype, holes=[(0, j) for j in range(0, 300, 3)])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_past_that_the_tables_do_not_hold(dtype):
+    """past beyond the table's tokens: those do not exist; a negative one is 0."""
+    from paper_2302_14357_amd import attend_prompts
+    g = _gen(3)
+    q, k, v = (_randn(g, 30, 4, 64, dtype=dtype).cuda() for _ in range(3))
+    kc, vc = (_randn(g, 8, 16, 4, 64, dtype=dtype).cuda() for _ in range(2))
+    tables = _i32([[0, 1, 2], [3, 4, 5]])
+    starts = _i32([0, 10, 30])
+    run = lambda past: attend_prompts(q, k, v, starts, past=_i32(past), k_cache=kc, v_cache=vc, tables=tables)   # noqa: E731
+    assert torch.equal(run([1000, 2**31 - 1]), run([48, 48]))
+    assert torch.equal(run([-1, -2**31]), run([0, 0]))
+    assert torch.equal(run([0, 0]), attend_prompts(q, k, v, starts))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("layout,shift", [("fused", 0), ("heads", 0), ("fused", 1), ("heads", 3), ("fused", 4)])
+def test_prompts_layouts(layout, shift, dtype):
+    for into in (None, "out", "q"):
+        _prompts_case([40, 3, 90], heads=6, kv=3, dim=40, dtype=dtype, layout=layout, shift=shift, into=into, pad=4)
+        _prompts_case([70, 33], past=[30, 80], heads=4, kv=2, dim=64, dtype=dtype, layout=layout, shift=shift, into=into, pad=4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [0.5, -0.3, 1e-4, 3.0])
+def test_prompts_scales(scale, dtype):
+    _prompts_case([50, 90], heads=2, kv=1, dim=64, dtype=dtype, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_large_scores(dtype):
+    """Scores that rise and fall by hundreds: the reference of the weights moves often, and most weights are 0."""
+    _prompts_case([300, 40], heads=2, kv=2, dim=64, dtype=dtype, q_scale=30.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("past,n", [(0, 1500), (0, 4100), (3000, 70), (5000, 1), (2500, 700)])
+def test_prompts_long(past, n, dtype):
+    _prompts_case([n, 5], past=[past, past // 2] if past else None, heads=2, kv=1, dim=64, dtype=dtype, page=32)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim,kv", [(64, 2), (80, 1), (128, 2), (256, 1)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_prompts_numbers_that_are_none_reach_nobody_else(bad, dim, kv, dtype):
+    """A token's key or value that is no number: outputs before it in its prompt, and of other prompts, are bit for bit as without it."""
+    from paper_2302_14357_amd import attend_prompts
+    g = _gen(dim)
+    lens, past, page, heads = [70, 100, 33], [40, 0, 90], 16, 4
+    q, k, v = (_randn(g, sum(lens), n, dim, dtype=dtype).cuda() for n in (heads, kv, kv))
+    width = 6
+    tables = torch.arange(3 * width, dtype=torch.int32).view(3, width)
+    kc, vc = (_randn(g, 3 * width, page, kv, dim, dtype=dtype).cuda() for _ in range(2))
+    starts = _i32([0, 70, 170, 203])
+    run = lambda q, k, v, kc, vc: attend_prompts(q, k, v, starts, past=_i32(past), k_cache=kc, v_cache=vc, tables=tables.cuda())   # noqa: E731
+    ref, tol = _prompts_ref(q.cpu(), k.cpu(), v.cpu(), lens, past, kc.cpu(), vc.cpu(), tables, page, None, dtype)
+    _close(run(q, k, v, kc, vc), ref, tol)
+    first = slice(0, heads // kv)   # the query heads of the key head that is touched
+    for token, end in ((0, 70), (33, 70), (69, 70), (71, 170), (169, 170), (171, 203), (202, 203)):
+        for which in range(2):
+            x = [k.clone(), v.clone()]
+            x[which][token, 0, dim - 1] = bad
+            got = run(q, *x, kc, vc)
+            keep = torch.ones(ref.shape, dtype=torch.bool)   # what the number may not reach
+            keep[token:end, first] = False
+            if which == 1:   # of the values only its dimension, and there it is what comes out
+                keep[token:end, first, :dim - 1] = True
+                touched = got[token:end, first, dim - 1].float()
+                assert bool((torch.isnan(touched) if math.isnan(bad) else touched == bad).all()), (token, touched)
+            _close(got.cpu()[keep], ref[keep], tol[keep])
+    for prompt, t in ((0, 3), (2, 89)):   # in the cache: its own prompt's business
+        x = vc.clone()
+        x[tables[prompt, t // page], t % page, 0, 0] = bad
+        got = run(q, k, v, kc, x).cpu()
+        keep = torch.ones(ref.shape, dtype=torch.bool)
+        keep[sum(lens[:prompt]):sum(lens[:prompt + 1]), first, 0] = False
+        assert not torch.isfinite(got[~keep].float()).any()
+        _close(got[keep], ref[keep], tol[keep])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prompts_starts_in_no_order_stay_in_bounds(dtype):
+    """Numbers that no batch has give wrong rows and nothing worse: what lies around the outputs stays."""
+    from paper_2302_14357_amd import attend_prompts
+    g = _gen(1)
+    q, k, v = (_randn(g, 100, 2, 64, dtype=dtype).cuda() for _ in range(3))
+    for starts in ([0, 50, 20, 100], [-5, 40, 1000], [2**31 - 1, -2**31, 100], [100, 0], [60, 60, 60], [0, 100, 0, 100, 0, 100], [30, 60]):
+        big = torch.full((300, 2, 64), 77.0, dtype=dtype, device="cuda")
+        attend_prompts(q, k, v, _i32(starts), out=big[100:200])
+        assert bool((big[:100] == 77.0).all()) and bool((big[200:] == 77.0).all())
+    got = attend_prompts(q, k, v, _i32([30, 60]))   # (rows before the first prompt are nobody's, too)
+    assert bool((got[:30] == 0).all()) and bool((got[60:] == 0).all())
+    assert torch.equal(got[30:60], attend_prompts(q[30:60], k[30:60], v[30:60], _i32([0, 30])))
