@@ -17,17 +17,35 @@
 #include "op_device.h"
 
 #define PROMPTS_SLACK 8.f
+#define PROMPTS_INLINE __attribute__((always_inline))   // (a function that is called would have everything that it looks at in memory)
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short prompts_b64;
 
 struct PromptsP {
     const char *q, *k, *v, *k_cache, *v_cache;
     const int *starts, *past, *tables;
     char *out;
-    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, kp, kt, kh, vp, vt, vh, ld_tables;   // bytes (ld_tables: elements)
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, kh, vh, ld_tables;   // bytes (ld_tables: elements)
+    unsigned kp, kt, vp, vt;
     int tokens, prompts, heads, kv_heads, group, dim, page, pages, width;
     bool direct;    // everything on 16-byte boundaries
+    bool runs;      // ... and sixteen keys from a multiple of sixteen on in one page
+    unsigned page_mul, page_shift;
     float scale2;   // |scale| log2(e)
     unsigned flip;  // sign bits of a word of queries where the scale is negative
+    // where the keys of a tile are shared among workgroups (otherwise null): the list of pieces, and what they leave
+    struct PromptsPiece *pieces;
+    int *count;               // pieces, and tiles
+    struct PromptsSplit *splits;
+    float *part_o, *part_ml;  // [pieces, kv_heads, rows, dim], [pieces, kv_heads, rows, 2]
+};
+
+// Steps k0 .. k1 - 1 of a tile's keys; apart: not all of them, and the piece's sums go to its place in part_o
+struct PromptsPiece {
+    int prompt, tile, k0, k1, apart;
+};
+// A tile's pieces
+struct PromptsSplit {
+    int prompt, tile, first, count;
 };
 
 struct PromptsAt {
@@ -89,19 +107,62 @@ struct PromptsTile {
     }
 };
 
+// t / page = 2 t / (2 page) for 0 <= t <= 2^30 by multiplication, as for one token over the cache: page_mul = floor(2^(32 + s) / (2 page)) + 1 with
+// s = floor(log2 (2 page)) is at most 2^(s + 1) / 2^(32 + s) of a unit too large for numerators below 2^31 (powers of two: exact)
+__device__ __forceinline__ unsigned prompts_page(const PromptsP &p, int t) { return __umulhi((unsigned)t << 1, p.page_mul) >> p.page_shift; }
+
+// what all lanes have alike, in scalar registers
+__device__ __forceinline__ const char *prompts_uniform(const char *x) {
+    const uint64_t u = (uint64_t)(uintptr_t)x;
+    return (const char *)(uintptr_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
+}
+
+// A direct load to LDS from base + offset: no register pair of addresses a lane
+__device__ __forceinline__ void prompts_load_lds(const char *base, unsigned offset, unsigned lds) {
+    unsigned m0_was;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(m0_was) : "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
+template <bool B>
+struct PromptsIs {
+    static constexpr bool value = B;
+};
+
+// The order of N matrix instructions and the R LDS reads that each wants: those of the first A instructions, then an instruction and the reads of the one A
+// behind it.  (All reads first would take 64 registers.)
+template <int N, int R, int A>
+__device__ __forceinline__ void prompts_interleave() {
+    __builtin_amdgcn_sched_group_barrier(0x100, R * (A < N ? A : N), 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, A < N ? A : N, 0);
+}
+
 // DP: dim rounded up to 32, 64, 96, 128 or 256; NW: waves of 32 rows each
 template <class T, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, DP > 128 || sizeof(T) == 4 ? 1 : 2)
+__global__ void __launch_bounds__(64 * NW, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
 k_prompts(PromptsP p) {
     typedef PromptsTile<T, DP> Tile;
     constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, KB = TK / 32, DB = DP / 32, KS = DP * (int)sizeof(T) / 32, ROWS = 32 * NW;
     constexpr int CHUNKS = TK * PITCH / 64, MINE = (CHUNKS + NW - 1) / NW;   // loads of 64 pieces, and those of a wave
     constexpr int VS = sizeof(T) == 4 ? 1 : DB;   // addresses of V
+    constexpr int RUN = 64 / PITCH;   // rows of a load
+    constexpr int KINDS = NW * RUN % 16 == 0 ? 1 : MINE;   // (the permutation repeats every sixteen rows)
     __shared__ __align__(16) char s_kv[2][2][Tile::BYTES];
-    __shared__ unsigned long long s_there[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int kvh = (int)blockIdx.x % p.kv_heads, unit = (int)blockIdx.x / p.kv_heads;
-    const int2 found = prompts_find(p, unit, ROWS);
+    PromptsPiece piece = {0, 0, 0, INT32_MAX, 0};
+    int2 found;
+    if (p.pieces) {
+        const int n = *p.count;
+        if (unit < n) piece = p.pieces[unit];
+        found = unit < n ? make_int2(piece.prompt, piece.tile) : make_int2(-1, n);
+    } else {
+        found = prompts_find(p, unit, ROWS);
+    }
     if (found.x < 0) {   // rows of no prompt are 0: those before the first and behind the last, shared among the workgroups without a tile
         const int first = p.prompts > 0 ? prompts_start(p, 0) : p.tokens, last = p.prompts > 0 ? max(prompts_start(p, p.prompts), first) : p.tokens;
         const int spare = (int)gridDim.x / p.kv_heads - found.y, rows = first + p.tokens - last;
@@ -114,17 +175,26 @@ k_prompts(PromptsP p) {
         }
         return;
     }
-    const PromptsAt at = prompts_at(p, found.x);
-    const int *table = p.past ? p.tables + found.x * p.ld_tables : nullptr;
-    const int rows = at.n * p.group, row0 = found.y * ROWS;   // (below 2^31: tokens x heads is)
-    const int keys = at.past + (min(row0 + ROWS, rows) - 1) / p.group + 1, steps = (keys + TK - 1) / TK;
+    const int prompt = __builtin_amdgcn_readfirstlane(found.x), tile = __builtin_amdgcn_readfirstlane(found.y);
+    PromptsAt at = prompts_at(p, prompt);
+    at.start = __builtin_amdgcn_readfirstlane(at.start), at.n = __builtin_amdgcn_readfirstlane(at.n), at.past = __builtin_amdgcn_readfirstlane(at.past);   // (in scalar registers)
+    const int *table = p.past ? p.tables + prompt * p.ld_tables : nullptr;
+    const int rows = at.n * p.group, row0 = tile * ROWS;   // (below 2^31: tokens x heads is)
+    const int keys = at.past + (min(row0 + ROWS, rows) - 1) / p.group + 1, first_step = __builtin_amdgcn_readfirstlane(piece.k0), steps = min((keys + TK - 1) / TK, __builtin_amdgcn_readfirstlane(piece.k1));
     // this lane's query, and the last key that it sees; the first and last of the wave's
-    const int row = row0 + wave * 32 + c, token = row / p.group, head = kvh * p.group + row - token * p.group;
+    const int row = row0 + wave * 32 + c, token = row / p.group;
     const bool live = row < rows;
     const int sees = live ? at.past + token : -1;
     const int w0 = row0 + wave * 32, wave_first = w0 + 32 <= rows ? at.past + w0 / p.group : -1, wave_last = w0 < rows ? at.past + (min(w0 + 32, rows) - 1) / p.group : -1;
+    bool holes = false;   // whether some of its pages do not exist
+    if (at.past > 0) {
+        const int from = first_step * TK, to = min(at.past, steps * TK);
+        for (int i = (int)prompts_page(p, from) + threadIdx.x; from < to && i <= (int)prompts_page(p, to - 1); i += 64 * NW) holes |= (unsigned)table[i] >= (unsigned)p.pages;
+        holes = __syncthreads_or(holes);
+    }
     uint4 q[KS];
     {
+        const int head = kvh * p.group + row - token * p.group;
         const T *src = (const T *)(p.q + (int64_t)(at.start + (live ? token : 0)) * p.q_row + (live ? head : 0) * p.q_head);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -133,50 +203,108 @@ k_prompts(PromptsP p) {
         }
     }
 
-    // ---- tiles into LDS
+    // ---- tiles into LDS: a lane's pieces are places of its rows
     const char *k_new = p.k + (int64_t)at.start * p.k_row + kvh * p.k_head, *v_new = p.v + (int64_t)at.start * p.v_row + kvh * p.v_head;
     const char *k_old = p.k_cache + kvh * p.kh, *v_old = p.v_cache + kvh * p.vh;
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&s_kv[0][0][0];
-    int id[MINE], id_mask = 0;   // the pages of this lane's keys in the tile to be asked for next, and of key `lane` of it
-    auto page_of = [&](int t) { return t < at.past ? table[(unsigned)t / (unsigned)p.page] : 0; };
-    auto row_of = [&](int i) { return ((wave + i * NW) * 64 + lane) / PITCH; };
-    auto look = [&](int step) {
-        if (step * TK >= at.past) return;
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) id[i] = page_of(step * TK + row_of(i));
-        if (wave == 0) id_mask = page_of(step * TK + (lane & (TK - 1)));
+    auto row_of = [&](int i, int lane) PROMPTS_INLINE { return ((wave + i * NW) * 64 + lane) / PITCH; };
+    auto piece_of = [&](int i, int lane, bool values) PROMPTS_INLINE {
+        return (((wave + i * NW) * 64 + lane) % PITCH) ^ (values ? Tile::v_swizzle(row_of(i, lane)) : Tile::k_swizzle(row_of(i, lane)));
     };
-    auto ask = [&](int step) {
-        const int t0 = step * TK, buffer = step & 1;
-        const bool old = t0 < at.past;
+    // (for what is seldom wanted: worked out where it is, not kept in registers)
+    auto again = [&] PROMPTS_INLINE {
+        int x = lane;
+        asm volatile("" : "+v"(x));
+        return x;
+    };
+    // Bytes from the first key of a load: among new tokens, and in a page
+    unsigned k_new_off[KINDS], v_new_off[KINDS], k_old_off[KINDS], v_old_off[KINDS];
+    bool k_in[KINDS], v_in[KINDS];   // (pieces behind the head's end are not there)
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-            const int chunk = wave + i * NW;
-            if (CHUNKS % NW && chunk >= CHUNKS) continue;
-            const int r = row_of(i), slot = (chunk * 64 + lane) % PITCH;
-            const int t = min(t0 + r, keys - 1);   // (behind the last: anything that is there)
-            const char *k = k_new + (int64_t)(t - at.past) * p.k_row, *v = v_new + (int64_t)(t - at.past) * p.v_row;
-            if (old && t < at.past) {
-                const unsigned page = (unsigned)t / (unsigned)p.page, off = (unsigned)t - page * (unsigned)p.page;
-                const int n = (unsigned)id[i] < (unsigned)p.pages ? id[i] : 0;   // (a page that does not exist: the first's, masked)
-                k = k_old + n * p.kp + off * p.kt;
-                v = v_old + n * p.vp + off * p.vt;
+    for (int i = 0; i < KINDS; ++i) {
+        const unsigned r = lane / PITCH, ks = piece_of(i, lane, false), vs = piece_of(i, lane, true);
+        k_new_off[i] = r * (unsigned)p.k_row + ks * 16, v_new_off[i] = r * (unsigned)p.v_row + vs * 16;
+        k_old_off[i] = r * p.kt + ks * 16, v_old_off[i] = r * p.vt + vs * 16;
+        k_in[i] = (int)ks * E < p.dim, v_in[i] = (int)vs * E < p.dim;
+    }
+    // The pages of the tile that is asked for next, looked up a tile ahead: of this lane's keys, or, where a load's keys lie in one page, lane i has the i-th load's.
+    int id[MINE];
+    auto page_of = [&](int t) PROMPTS_INLINE { return t < at.past ? table[prompts_page(p, t)] : 0; };
+    auto look = [&](int step) PROMPTS_INLINE {
+        const int t0 = step * TK, lane = again();
+        if (t0 >= at.past) return;
+        if (p.runs) {
+            id[0] = lane < MINE ? page_of(t0 + (wave + lane * NW) * RUN) : 0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) id[i] = page_of(t0 + row_of(i, lane));
+        }
+    };
+    auto ask = [&](int step) PROMPTS_INLINE {
+        const int t0 = step * TK, buffer = step & 1;
+        const unsigned to = lds + buffer * 2 * Tile::BYTES;
+        const bool fresh = t0 >= at.past;
+        if (fresh ? p.direct && t0 + TK <= keys : p.runs && t0 + TK <= at.past) {   // new tokens or ones of the cache, all there: scalar addresses
+            constexpr bool SAME = KINDS == 1;
+            unsigned n[MINE], ko[KINDS], vo[KINDS];
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) n[i] = fresh ? 0 : (unsigned)__builtin_amdgcn_readlane(id[0], i);   // (all of them before the first load: it would be waited for)
+#pragma unroll
+            for (int i = 0; i < KINDS; ++i) ko[i] = fresh ? k_new_off[i] : k_old_off[i], vo[i] = fresh ? v_new_off[i] : v_old_off[i];
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                const int chunk = wave + i * NW, t = t0 + chunk * RUN;
+                if (CHUNKS % NW && chunk >= CHUNKS) continue;
+                const char *k, *v;
+                if (fresh) {
+                    k = k_new + (int64_t)(t - at.past) * p.k_row;
+                    v = v_new + (int64_t)(t - at.past) * p.v_row;
+                } else {
+                    const unsigned use = n[i] < (unsigned)p.pages ? n[i] : 0, off = (unsigned)t - prompts_page(p, t) * (unsigned)p.page;   // (a page that does not exist: the first's, masked)
+                    k = k_old + (uint64_t)use * p.kp + off * p.kt;
+                    v = v_old + (uint64_t)use * p.vp + off * p.vt;
+                }
+                k = prompts_uniform(k), v = prompts_uniform(v);
+                if (k_in[SAME ? 0 : i]) prompts_load_lds(k, ko[SAME ? 0 : i], to + chunk * 1024);
+                if (v_in[SAME ? 0 : i]) prompts_load_lds(v, vo[SAME ? 0 : i], to + Tile::BYTES + chunk * 1024);
             }
-            const int ks = slot ^ Tile::k_swizzle(r), vs = slot ^ Tile::v_swizzle(r);
-            const unsigned to = lds + buffer * 2 * Tile::BYTES + chunk * 1024;
-            if (p.direct) {
-                if (ks * E < p.dim) op_load_lds(k + ks * 16, to);
-                if (vs * E < p.dim) op_load_lds(v + vs * 16, to + Tile::BYTES);
-            } else {
-                if (ks * E < p.dim) *(uint4 *)(&s_kv[buffer][0][0] + chunk * 1024 + lane * 16) = op_load16((const T *)k + ks * E);
-                if (vs * E < p.dim) *(uint4 *)(&s_kv[buffer][1][0] + chunk * 1024 + lane * 16) = op_load16((const T *)v + vs * E);
+        } else {
+            const int lane = again();
+            int n[MINE];
+            if (!fresh) {
+#pragma unroll
+                for (int i = 0; i < MINE; ++i) {
+                    n[i] = p.runs ? __builtin_amdgcn_readlane(id[0], i) : id[i];
+                    asm volatile("" : "+v"(n[i]));   // (here, before the first load)
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                const int chunk = wave + i * NW;
+                if (CHUNKS % NW && chunk >= CHUNKS) continue;
+                const int t = min(t0 + row_of(i, lane), keys - 1);   // (behind the last: anything that is there)
+                const char *k = k_new + (int64_t)(t - at.past) * p.k_row, *v = v_new + (int64_t)(t - at.past) * p.v_row;
+                if (t < at.past) {
+                    const unsigned off = (unsigned)t - prompts_page(p, t) * (unsigned)p.page, use = (unsigned)n[i] < (unsigned)p.pages ? n[i] : 0;
+                    k = k_old + (uint64_t)use * p.kp + off * p.kt;
+                    v = v_old + (uint64_t)use * p.vp + off * p.vt;
+                }
+                const int ks = piece_of(i, lane, false), vs = piece_of(i, lane, true);
+                if (p.direct) {
+                    if (ks * E < p.dim) op_load_lds(k + ks * 16, to + chunk * 1024);
+                    if (vs * E < p.dim) op_load_lds(v + vs * 16, to + Tile::BYTES + chunk * 1024);
+                } else {
+                    if (ks * E < p.dim) *(uint4 *)(&s_kv[buffer][0][0] + chunk * 1024 + lane * 16) = op_load16((const T *)k + ks * E);
+                    if (vs * E < p.dim) *(uint4 *)(&s_kv[buffer][1][0] + chunk * 1024 + lane * 16) = op_load16((const T *)v + vs * E);
+                }
             }
         }
-        if (old && wave == 0) {
-            const int t = t0 + lane;
-            const unsigned long long there = __ballot(lane < TK && (t >= at.past || (unsigned)id_mask < (unsigned)p.pages));
-            if (lane == 0) s_there[buffer] = there;
-        }
+    };
+    auto landed = [&]() PROMPTS_INLINE {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
     // pieces behind the head's end are 0 in both buffers, and stay so
     if (p.dim < PITCH * E) {
@@ -185,237 +313,403 @@ k_prompts(PromptsP p) {
             if ((slot ^ ((i / (TK * PITCH)) & 1 ? Tile::v_swizzle(r) : Tile::k_swizzle(r))) * E >= p.dim) ((uint4 *)&s_kv[0][0][0])[i] = make_uint4(0, 0, 0, 0);
         }
     }
-    look(0);
-    ask(0);
-    look(1);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 
     // ---- fragments: where this lane's begin
-    int k_at[KS], v_at[VS];
+    const char *k_at[KS], *v_at[VS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) k_at[s] = (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
+    for (int s = 0; s < KS; ++s) k_at[s] = &s_kv[0][0][0] + (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
     const int v_row = sizeof(T) == 4 ? 4 * h : 4 * h + (lane >> 2 & 3);
+    auto v_place = [&](int d) PROMPTS_INLINE {
+        return &s_kv[0][1][0] + (sizeof(T) == 4 ? v_row * PITCH * 16 : (v_row * PITCH + ((d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ Tile::v_swizzle(v_row))) * 16 + (lane & 1) * 8);
+    };
 #pragma unroll
-    for (int d = 0; d < VS; ++d)
-        v_at[d] = sizeof(T) == 4 ? v_row * PITCH * 16 : (v_row * PITCH + ((d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ Tile::v_swizzle(v_row))) * 16 + (lane & 1) * 8;
+    for (int d = 0; d < VS; ++d) v_at[d] = v_place(d);
     // V^T of 16 keys from `key` on (in the order of the weights) and the d-th 32 dimensions
-    auto v_frag = [&](int buffer, int key, int d) {
+    auto v_frag = [&](auto apart, int buffer, int key, int d) PROMPTS_INLINE {
         uint4 u;
         typedef __attribute__((address_space(3))) prompts_b64 *Lds;
-        const unsigned from = lds + (buffer * 2 + 1) * Tile::BYTES + v_at[d] + key * PITCH * 16;
-        const prompts_b64 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(uintptr_t)from), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(uintptr_t)(from + 8 * PITCH * 16));
+        const char *from = (apart.value ? v_place(d) : v_at[d]) + buffer * 2 * Tile::BYTES;
+        const prompts_b64 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + key * PITCH * 16)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + (key + 8) * PITCH * 16));
         __builtin_memcpy(&u, &x, 8);
         __builtin_memcpy((char *)&u + 8, &y, 8);
         return u;
     };
-    auto v_one = [&](int buffer, int key, int d) {   // float32: dimension 32 d + c of key `key` + 4 h
-        return *(const float *)(&s_kv[buffer][1][0] + v_at[0] + key * PITCH * 16 + (((d * 8 + c / 4) ^ (PITCH >= 16 ? h << 3 : 0)) * 16 + c % 4 * 4));
+    auto v_one = [&](int buffer, int key, int d) PROMPTS_INLINE {   // float32: dimension 32 d + c of key `key` + 4 h
+        return *(const float *)(v_at[0] + buffer * 2 * Tile::BYTES + key * PITCH * 16 + (((d * 8 + c / 4) ^ (PITCH >= 16 ? h << 3 : 0)) * 16 + c % 4 * 4));
+    };
+    // which keys of a tile there are (bit i: key i), for all of the wave
+    constexpr unsigned long long WHOLE = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
+    auto there_of = [&](int step) PROMPTS_INLINE {
+        const int t0 = step * TK;
+        unsigned long long there = keys - t0 >= TK ? WHOLE : (1ull << (keys - t0)) - 1;
+        if (holes && t0 < at.past) {
+            const int t = t0 + (lane & (TK - 1));
+            there &= __ballot(t >= at.past || (unsigned)page_of(t) < (unsigned)p.pages);
+        }
+        return there;
+    };
+    // ... and which of them this lane's query sees
+    auto mine_of = [&](int step, unsigned long long there) PROMPTS_INLINE {
+        const int last = sees - step * TK;   // (its last key's place)
+        return last < 0 ? 0 : last >= 63 ? there : there & ((2ull << last) - 1);
     };
 
     floatx16 o[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m, l;
     // (float16: weights up to 2^7 more, so that small ones keep their digits: with the slack's 2^8 at most half its largest number)
     constexpr float MORE = __is_same(T, _Float16) ? 7.f : 0.f;
 
-    for (int step = 0; step < steps; ++step) {
-        const int t0 = step * TK, buffer = step & 1;
+    // All tiles.  A value that is NaN or infinite reaches, times the weight 0, the queries that do not see it; nothing of this pass is kept then, and in others, of 32
+    // dimensions each (apart: those from 32 d0 on, in o[0]), the keys of a tile that some query does not see all of are added one by one to the queries that see them.
+    auto pass = [&](auto apart, int d0) PROMPTS_INLINE {
+    constexpr int DB = apart.value ? 1 : DP / 32;
+    floatx16 s[KB];
+    uint4 w[sizeof(T) == 4 ? 1 : TK / 16];   // a tile's weights
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = floatx16{};
+    m = -INFINITY, l = 0.f;
+    // the weights of tile `step` with its values
+    auto values = [&](int step, unsigned long long there) PROMPTS_INLINE {
+        const int buffer = step & 1;
+        if (!apart.value || (there == WHOLE && step * TK + TK - 1 <= wave_first)) {
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_one(buffer, 8 * (i / 4) + i % 4, d0 + d), s[0][i], o[d], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < TK / 16; ++i)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(apart, buffer, i * 16, d0 + d), w[i], o[d]);
+                prompts_interleave<TK / 16 * DB, 2, 4>();
+            }
+            return;
+        }
+        const unsigned long long mine = mine_of(step, there);
+#pragma unroll 1
+        for (int key = 0; key < TK; ++key) {
+            const bool seen = mine >> key & 1;
+            if (!__any(seen)) continue;
+            const int half = key >> 2 & 1;   // its place in the fragments: half, and element
+            uint4 x, y = make_uint4(0, 0, 0, 0);
+            float one = 0.f;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) one = 8 * (i / 4) + i % 4 == (key & ~4) ? s[0][i] : one;
+            } else {
+#pragma unroll
+                for (int i = 0; i < TK / 16; ++i)
+                    if (i == key >> 4) y = w[i];
+            }
+            const int e = (key >> 3 & 1) * 4 + (key & 3);
+            const unsigned keep = h == half ? (e & 1 ? 0xffff0000u : 0xffffu) : 0;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                floatx16 z = {};
+                if constexpr (sizeof(T) == 4) {
+                    const float v = v_one(buffer, key & ~4, d0 + d);
+                    z = __builtin_amdgcn_mfma_f32_32x32x2f32(h == half ? v : 0.f, h == half && seen ? one : 0.f, z, 0, 0, 0);
+                } else {
+                    x = v_frag(apart, buffer, key & ~15, d0 + d);
+                    x.x &= e / 2 == 0 ? keep : 0, x.y &= e / 2 == 1 ? keep : 0, x.z &= e / 2 == 2 ? keep : 0, x.w &= e / 2 == 3 ? keep : 0;
+                    z = op_mma32<T>(x, y, z);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[d][j] = seen ? o[d][j] + z[j] : o[d][j];
+            }
+        }
+    };
+    auto scores = [&](int step) PROMPTS_INLINE {
+        const int buffer = (step & 1) * 2 * Tile::BYTES;
+#pragma unroll
+        for (int j = 0; j < KS; ++j)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) s[b] = op_mma32<T>(*(const uint4 *)(k_at[j] + buffer + b * 32 * PITCH * 16), q[j], j == 0 ? floatx16{} : s[b]);
+        if constexpr (sizeof(T) == 2) prompts_interleave<KS * KB, 1, 4>();
+    };
+    auto softmax = [&](int step, unsigned long long there) PROMPTS_INLINE {
+        const int t0 = step * TK;
+        if (there != WHOLE || t0 + TK - 1 > wave_first) {
+            const unsigned long long bits = mine_of(step, there) >> (4 * h);
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = bits >> (32 * b + 8 * (i / 4) + i % 4) & 1 ? s[b][i] : -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        {
+            typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
+            const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
+        }
+        if (__any(top > m + PROMPTS_SLACK)) {
+            const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+            m = m1;
+            l *= a;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= a;
+        }
+        const float base = m == -INFINITY ? 0.f : m - MORE;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], p.scale2, -base));
+                sum[i & 1] += s[b][i];
+            }
+        l += sum[0] + sum[1];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < TK / 16; ++i) {
+                T x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = (T)s[i / 2][i % 2 * 8 + j];
+                __builtin_memcpy(&w[i], x, 16);
+            }
+        }
+    };
+
+    look(first_step);
+    ask(first_step);
+    look(first_step + 1);
+    landed();
+    for (int step = first_step; step < steps; ++step) {
         if (step + 1 < steps) {
             ask(step + 1);
             look(step + 2);
         }
-        if (t0 <= wave_last) {
-            unsigned long long there = keys - t0 >= TK ? (TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1) : (1ull << (keys - t0)) - 1;
-            const unsigned long long whole = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
-            if (t0 < at.past) there &= s_there[buffer];
-            there = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(there >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)there);
-            const bool mixed = there != whole || t0 + TK - 1 > wave_first;   // some key is not some query's
-            floatx16 s[KB];
-#pragma unroll
-            for (int b = 0; b < KB; ++b) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-#pragma unroll
-                for (int j = 0; j < KS; ++j) s[b] = op_mma32<T>(*(const uint4 *)(&s_kv[buffer][0][0] + k_at[j] + b * 32 * PITCH * 16), q[j], s[b]);
-            }
-            unsigned long long mine = ~0ull;   // this lane's query's keys of the tile
-            if (mixed) {
-                const int last = sees - t0;   // (its last key's place)
-                mine = last < 0 ? 0 : last >= 63 ? there : there & ((2ull << last) - 1);
-                const unsigned long long bits = mine >> (4 * h);
-#pragma unroll
-                for (int b = 0; b < KB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = bits >> (32 * b + 8 * (i / 4) + i % 4) & 1 ? s[b][i] : -INFINITY;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            {
-                typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
-                const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
-            }
-            if (__any(top > m + PROMPTS_SLACK)) {
-                const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-                m = m1;
-                l *= a;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= a;
-            }
-            const float base = m == -INFINITY ? 0.f : m - MORE;
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], p.scale2, -base));
-                    l += s[b][i];
-                }
-            // A value that is NaN or infinite would reach, times the weight 0, the queries that do not see it.  Where some do not, such a tile's keys are
-            // added one by one to those that do.
-            bool odd = false;
-            if constexpr (sizeof(T) == 4) {
-                if (mixed) {
-                    floatx16 z = {};
-#pragma unroll
-                    for (int key = 0; key < TK; key += 8)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) z = __builtin_amdgcn_mfma_f32_32x32x2f32(v_one(buffer, key + r, d), 0.f, z, 0, 0, 0);
-                    bool none = false;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) none |= z[i] != 0.f;
-                    odd = __any(none);
-                }
-                if (!odd) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_one(buffer, 8 * (i / 4) + i % 4, d), s[0][i], o[d], 0, 0, 0);
-                } else {
-                    for (int key = 0; key < TK; ++key) {
-                        const bool seen = mine >> key & 1;
-                        if (!__any(seen)) continue;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (8 * (i / 4) + i % 4 != (key & ~4)) continue;
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                const float x = v_one(buffer, key & ~4, d);
-                                floatx16 z = {};
-                                z = __builtin_amdgcn_mfma_f32_32x32x2f32(h == (key >> 2 & 1) ? x : 0.f, h == (key >> 2 & 1) && seen ? s[0][i] : 0.f, z, 0, 0, 0);
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) o[d][j] = seen ? o[d][j] + z[j] : o[d][j];
-                            }
-                        }
-                    }
-                }
-            } else {
-                uint4 w[TK / 16];
-#pragma unroll
-                for (int i = 0; i < TK / 16; ++i) {
-                    T x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = (T)s[i / 2][i % 2 * 8 + j];
-                    __builtin_memcpy(&w[i], x, 16);
-                }
-                if (mixed) {
-                    floatx16 z = {};
-#pragma unroll
-                    for (int i = 0; i < TK / 16; ++i)
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) z = op_mma32<T>(v_frag(buffer, i * 16, d), make_uint4(0, 0, 0, 0), z);
-                    bool none = false;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) none |= z[i] != 0.f;
-                    odd = __any(none);
-                }
-                if (!odd) {
-#pragma unroll
-                    for (int i = 0; i < TK / 16; ++i)
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(buffer, i * 16, d), w[i], o[d]);
-                } else {
-                    for (int key = 0; key < TK; ++key) {
-                        const bool seen = mine >> key & 1;
-                        if (!__any(seen)) continue;
-                        // its place in the fragments: half and element
-                        const int half = key >> 2 & 1, e = (key >> 3 & 1) * 4 + (key & 3);
-                        const unsigned keep = h == half ? (e & 1 ? 0xffff0000u : 0xffffu) : 0;
-#pragma unroll
-                        for (int i = 0; i < TK / 16; ++i) {
-                            if (i != key >> 4) continue;
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                uint4 x = v_frag(buffer, i * 16, d);
-                                x.x &= e / 2 == 0 ? keep : 0, x.y &= e / 2 == 1 ? keep : 0, x.z &= e / 2 == 2 ? keep : 0, x.w &= e / 2 == 3 ? keep : 0;
-                                floatx16 z = {};
-                                z = op_mma32<T>(x, w[i], z);
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) o[d][j] = seen ? o[d][j] + z[j] : o[d][j];
-                            }
-                        }
-                    }
-                }
-            }
+        if (step * TK <= wave_last) {
+            const unsigned long long there = there_of(step);
+            __builtin_amdgcn_s_setprio(1);
+            scores(step);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            softmax(step, there);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            values(step, there);
+            __builtin_amdgcn_s_setprio(0);
         }
-        if (step + 1 < steps) {   // the next tile is there, and everybody has read this one
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
+        if (step + 1 < steps) landed();   // the next tile is there, and everybody has read this one
     }
+    };
 
-    l += __shfl_xor(l, 32);
-    const float f = l == 0.f ? 0.f : 1.f / l;   // (no weight at all: 0)
-    if (!live) return;
-    char *to = p.out + (int64_t)(at.start + token) * p.o_row + head * p.o_head;
+    auto store = [&](const floatx16 &x, int d) PROMPTS_INLINE {
+        const float sum = l + __shfl_xor(l, 32), f = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
+        if (!live) return;
+        if (piece.apart) {
+            const int64_t at = ((int64_t)unit * p.kv_heads + kvh) * ROWS + wave * 32 + c;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+            for (int b = 0; b < 4; ++b)
+                if (d * 32 + b * 8 + h * 4 < p.dim) *(float4 *)(p.part_o + at * p.dim + d * 32 + b * 8 + h * 4) = make_float4(x[b * 4], x[b * 4 + 1], x[b * 4 + 2], x[b * 4 + 3]);
+            if (h == 0 && d == 0) *(float2 *)(p.part_ml + at * 2) = make_float2(m, sum);
+            return;
+        }
+        char *to = p.out + (int64_t)(at.start + token) * p.o_row + (kvh * p.group + row - token * p.group) * p.o_head;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int e = d * 32 + b * 8 + h * 4;   // (dim is a multiple of 8)
             if (e >= p.dim) continue;
             T y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = (T)(l == 0.f ? 0.f : o[d][b * 4 + i] * f);
+            for (int i = 0; i < 4; ++i) y[i] = (T)(sum == 0.f ? 0.f : x[b * 4 + i] * f);
             __builtin_memcpy((T *)to + e, y, sizeof y);
         }
+    };
+    pass(PromptsIs<false>(), 0);
+    float none = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) none = fmaf(o[d][i], 0.f, none);
+    if (!__syncthreads_or(live && none != 0.f)) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) store(o[d], d);
+    } else {
+#pragma unroll 1
+        for (int d = 0; d < DB; ++d) {
+            pass(PromptsIs<true>(), d);
+            store(o[0], d);
+            __syncthreads();
+        }
+    }
 }
 
-static int64_t prompts_units(const tbs_attend_prompts_args &a, int rows) { return (int64_t)a.tokens * (a.heads / a.kv_heads) / rows + a.prompts + 1; }
+#define PROMPTS_PLAN 1024     // threads of the plan; tiles, and prompts, at most
+#define PROMPTS_SLOTS 512     // workgroups that the chip runs at a time, two a CU
+
+// Whose keys are shared, one workgroup: a thread a tile.  A piece is at most `len` steps long; of eight lengths, from an equal share of all work up, the one whose
+// pieces take the fewest steps one after the other in the slots that there are, with three more for a piece's start and end and eight for the join.
+__global__ void __launch_bounds__(PROMPTS_PLAN)
+k_prompts_plan(PromptsP p, int rows, int step, int most) {
+    __shared__ int s_first[PROMPTS_PLAN], s_wave[PROMPTS_PLAN / 64], s_sum[8], s_longest;
+    __shared__ unsigned long long s_all;
+    const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+    auto before = [&](int x, int *all) {   // the sum over smaller threads, and over all
+        int sum = x;
+#pragma unroll
+        for (int j = 1; j < 64; j <<= 1) {
+            const int y = __shfl_up(sum, j);
+            if (lane >= j) sum += y;
+        }
+        __syncthreads();
+        if (lane == 63) s_wave[wave] = sum;
+        __syncthreads();
+        int less = sum - x, total = 0;
+        for (int j = 0; j < PROMPTS_PLAN / 64; ++j) {
+            less += j < wave ? s_wave[j] : 0;
+            total += s_wave[j];
+        }
+        *all = total;
+        return less;
+    };
+    if (i < 8) s_sum[i] = 0;
+    if (i == 0) s_longest = 0, s_all = 0;
+    int tiles;
+    const int mine = i < p.prompts ? (prompts_length(p, i) * p.group + rows - 1) / rows : 0;
+    const int first = before(min(mine, PROMPTS_PLAN + 1), &tiles);
+    tiles = min(tiles, most);   // (starts in no order may give more: there is no room for them)
+    s_first[i] = first;
+    __syncthreads();
+    int prompt = 0, tile = 0, steps = 0;
+    if (i < tiles) {
+#pragma unroll
+        for (int w = PROMPTS_PLAN / 2; w > 0; w /= 2)
+            if (prompt + w < p.prompts && s_first[prompt + w] <= i) prompt += w;
+        const PromptsAt at = prompts_at(p, prompt);
+        const int count = (at.n * p.group + rows - 1) / rows;
+        tile = count - 1 - (i - s_first[prompt]);   // (a prompt's last tiles, which have the most keys, first)
+        steps = (at.past + (min(tile * rows + rows, at.n * p.group) - 1) / p.group + 1 + step - 1) / step;
+        atomicAdd(&s_all, (unsigned long long)steps);
+        atomicMax(&s_longest, steps);
+    }
+    __syncthreads();
+    const int longest = max(s_longest, 1);
+    const int64_t share = max((int64_t)(s_all * p.kv_heads + PROMPTS_SLOTS - 1) / PROMPTS_SLOTS, (int64_t)4);
+    auto length = [&](int j) { return j == 7 ? longest : (int)min((int64_t)longest, j < 4 ? share + share * j / 8 : share * (j - 1) / 2); };   // 1, 9/8, 10/8, 11/8, 3/2, 2, 5/2 shares, and all
+    if (i < tiles)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) atomicAdd(&s_sum[j], (steps + length(j) - 1) / length(j));
+    __syncthreads();
+    int len = longest;
+    int64_t least = INT64_MAX;
+#pragma unroll
+    for (int j = 7; j >= 0; --j) {
+        const int64_t t = ((int64_t)s_sum[j] * p.kv_heads + PROMPTS_SLOTS - 1) / PROMPTS_SLOTS * (length(j) + 3) + (length(j) < longest ? 8 : 0);
+        if (t < least) least = t, len = length(j);
+    }
+    const int count = i < tiles ? (steps + len - 1) / len : 0;
+    int total;
+    const int at = before(count, &total);
+    if (i == 0) p.count[0] = total, p.count[1] = tiles;
+    if (i < tiles) p.splits[i] = {prompt, tile, at, count};
+    for (int j = 0; j < count; ++j) p.pieces[at + j] = {prompt, tile, (int)((int64_t)steps * j / count), (int)((int64_t)steps * (j + 1) / count), count > 1};
+}
+
+// The pieces of a tile and key head: four rows of a wave at a time where heads are of 64, a row's numbers by lanes side by side
+template <class T>
+__global__ void __launch_bounds__(256)
+k_prompts_join(PromptsP p, int rows) {
+    const int kvh = (int)blockIdx.x % p.kv_heads, u = (int)blockIdx.x / p.kv_heads;
+    if (u >= p.count[1]) return;
+    const PromptsSplit s = p.splits[u];
+    if (s.count <= 1) return;
+    const PromptsAt at = prompts_at(p, s.prompt);
+    int lanes = 2;   // of a row, four numbers each
+    while (lanes * 4 < p.dim) lanes *= 2;
+    const int d = (threadIdx.x & (lanes - 1)) * 4, step = 256 / lanes * gridDim.y;
+    for (int r = blockIdx.y * (256 / lanes) + threadIdx.x / lanes; r < rows; r += step) {
+        const int row = s.tile * rows + r, token = row / p.group;
+        if (row >= at.n * p.group || d >= p.dim) continue;
+        float top = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < s.count; ++j) {
+            const int64_t from = ((int64_t)(s.first + j) * p.kv_heads + kvh) * rows + r;
+            const float2 ml = *(const float2 *)(p.part_ml + from * 2);
+            const float4 x = *(const float4 *)(p.part_o + from * p.dim + d);
+            const float m = fmaxf(top, ml.x), a = top == m ? 1.f : __builtin_amdgcn_exp2f(top - m), b = ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
+            top = m;
+            l = l * a + ml.y * b;
+            o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
+        }
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const T y[4] = {(T)(l == 0.f ? 0.f : o.x * f), (T)(l == 0.f ? 0.f : o.y * f), (T)(l == 0.f ? 0.f : o.z * f), (T)(l == 0.f ? 0.f : o.w * f)};
+        __builtin_memcpy((T *)(p.out + (int64_t)(at.start + token) * p.o_row + (kvh * p.group + row - token * p.group) * p.o_head) + d, y, sizeof y);
+    }
+}
+
+// How a call is done: waves of a workgroup, and whether the keys of a tile are shared out
+struct PromptsForm {
+    int waves;
+    bool shared;
+    int64_t tiles, units;   // at most: tiles; tiles, or pieces, and one more
+};
+
+static PromptsForm prompts_form(const tbs_attend_prompts_args &a, int force) {
+    const int group = a.heads / a.kv_heads;
+    auto tiles = [&](int waves) { return (int64_t)a.tokens * group / (32 * waves) + a.prompts; };
+    PromptsForm f = {4, false, 0, 0};
+    const int64_t t = tiles(4), longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0;
+    f.shared = t <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : t * a.kv_heads < 2 * PROMPTS_SLOTS && longest >= 2048);
+    if (!f.shared)
+        while (f.waves > 2 && (tiles(f.waves) + 1) * a.kv_heads < 512) f.waves /= 2;
+    f.tiles = tiles(f.waves);
+    f.units = f.tiles + 1 + (f.shared ? PROMPTS_SLOTS / a.kv_heads : 0);   // (a piece is an equal share of all steps or more)
+    return f;
+}
+
+struct PromptsSpace {
+    int64_t pieces, splits, o, ml, bytes;
+};
+
+static PromptsSpace prompts_space(const tbs_attend_prompts_args &a, const PromptsForm &f) {
+    PromptsSpace s = {};
+    if (!f.shared) return s;
+    const int64_t rows = f.units * a.kv_heads * 32 * f.waves;
+    auto after = [](int64_t at, int64_t n) { return (at + n + 15) / 16 * 16; };
+    s.pieces = 16;
+    s.splits = after(s.pieces, f.units * (int64_t)sizeof(PromptsPiece));
+    s.ml = after(s.splits, PROMPTS_PLAN * (int64_t)sizeof(PromptsSplit));
+    s.o = after(s.ml, rows * 8);
+    s.bytes = after(s.o, rows * a.dim * 4);
+    return s;
+}
 
 template <class T, int DP>
-static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args &a, hipStream_t st) {
-    constexpr int MOST = DP > 128 || sizeof(T) == 4 ? 4 : 8;
-    int waves = MOST;
-    while (waves > 2 && prompts_units(a, 32 * waves) * a.kv_heads < 512) waves /= 2;
-    const int64_t blocks = prompts_units(a, 32 * waves) * a.kv_heads;
+static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args &a, const PromptsForm &f, hipStream_t st) {
+    const int64_t blocks = f.units * a.kv_heads;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(64 * waves);
-    if (waves == 2) hipLaunchKernelGGL((k_prompts<T, DP, 2>), grid, block, 0, st, p);
-    else if (waves == 4) hipLaunchKernelGGL((k_prompts<T, DP, 4>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_prompts<T, DP, MOST>), grid, block, 0, st, p);
+    const dim3 grid((unsigned)blocks), block(64 * f.waves);
+    if (f.shared) {
+        hipLaunchKernelGGL(k_prompts_plan, dim3(1), dim3(PROMPTS_PLAN), 0, st, p, 32 * f.waves, PromptsTile<T, DP>::KEYS, (int)f.tiles);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (f.waves == 2) hipLaunchKernelGGL((k_prompts<T, DP, 2>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_prompts<T, DP, 4>), grid, block, 0, st, p);
+    if (f.shared) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((k_prompts_join<T>), dim3((unsigned)(f.tiles * a.kv_heads), 4), dim3(256), 0, st, p, 32 * f.waves);
+    }
     return hipGetLastError();
 }
 
 template <class T>
-static hipError_t prompts_dims(const PromptsP &p, const tbs_attend_prompts_args &a, hipStream_t st) {
-    if (p.dim <= 32) return prompts_waves<T, 32>(p, a, st);
-    if (p.dim <= 64) return prompts_waves<T, 64>(p, a, st);
-    if (p.dim <= 96) return prompts_waves<T, 96>(p, a, st);
-    if (p.dim <= 128) return prompts_waves<T, 128>(p, a, st);
-    return prompts_waves<T, 256>(p, a, st);
+static hipError_t prompts_dims(const PromptsP &p, const tbs_attend_prompts_args &a, const PromptsForm &f, hipStream_t st) {
+    if (p.dim <= 32) return prompts_waves<T, 32>(p, a, f, st);
+    if (p.dim <= 64) return prompts_waves<T, 64>(p, a, f, st);
+    if (p.dim <= 96) return prompts_waves<T, 96>(p, a, f, st);
+    if (p.dim <= 128) return prompts_waves<T, 128>(p, a, f, st);
+    return prompts_waves<T, 256>(p, a, f, st);
 }
 
 static int prompts_check(const tbs_attend_prompts_args &a) {
@@ -428,10 +722,11 @@ static int prompts_check(const tbs_attend_prompts_args &a) {
 
 extern "C" int64_t tbs_attend_prompts_workspace(const tbs_attend_prompts_args *args) {
     if (!args || prompts_check(*args) != TBS_OK) return TBS_EINVAL;
-    return 0;
+    return args->tokens == 0 ? 0 : prompts_space(*args, prompts_form(*args, 0)).bytes;
 }
 
-extern "C" int tbs_attend_prompts(const tbs_attend_prompts_args *args, void *stream) {
+// force: 0 = by the rule, 1 = a workgroup a tile, 2 = the keys shared out
+static int prompts_call(const tbs_attend_prompts_args *args, int force, void *stream) {
     if (!args) return TBS_EINVAL;
     const tbs_attend_prompts_args &a = *args;
     if (prompts_check(a) != TBS_OK) return TBS_EINVAL;
@@ -451,25 +746,49 @@ extern "C" int tbs_attend_prompts(const tbs_attend_prompts_args *args, void *str
         if ((uintptr_t)x % es) return TBS_EINVAL;
         direct &= (uintptr_t)x % 16 == 0;
     }
+    // (addresses in the cache: a page's number times 32 bits, a place in the page of 32 bits; in a tile of new tokens 32 bits from its first)
+    const int64_t wide[] = {a.k_cache_token * es * a.page, a.v_cache_token * es * a.page, a.k_cache_page * es, a.v_cache_page * es, a.k_row * es * 64, a.v_row * es * 64};
+    for (int i = 0; i < 6; ++i)
+        if ((i >= 4 || (a.past && (i < 2 || a.pages > 1))) && wide[i] > INT32_MAX) {
+            if (i < 4 ? wide[i] > UINT32_MAX : a.tokens > 1) return TBS_EINVAL;
+        }
     // what is written lies neither over itself nor over what others read; queries are read by those who write in their place
     const OpHeads q = {a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head}, out = {a.out, a.tokens, a.heads, a.dim, a.out_row, a.out_head};
     if (op_folded(out) || (!op_same(q, out) && op_overlap(out, q, es)) || op_overlap(out, {a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head}, es) ||
         op_overlap(out, {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head}, es))
         return TBS_EINVAL;
+    const PromptsForm f = prompts_form(a, force);
+    const PromptsSpace space = prompts_space(a, f);
+    if (space.bytes > 0 && (!a.workspace || a.workspace_bytes < space.bytes || (uintptr_t)a.workspace % 16)) return TBS_EINVAL;
     PromptsP p = {};
+    if (f.shared) {
+        char *w = (char *)a.workspace;
+        p.count = (int *)w, p.pieces = (PromptsPiece *)(w + space.pieces), p.splits = (PromptsSplit *)(w + space.splits), p.part_ml = (float *)(w + space.ml), p.part_o = (float *)(w + space.o);
+    }
     p.q = (const char *)a.q, p.k = (const char *)a.k, p.v = (const char *)a.v, p.k_cache = (const char *)a.k_cache, p.v_cache = (const char *)a.v_cache, p.out = (char *)a.out;
     p.starts = a.starts, p.past = a.past, p.tables = a.tables;
     p.q_row = a.q_row * es, p.q_head = a.q_head * es, p.k_row = a.k_row * es, p.k_head = a.k_head * es, p.v_row = a.v_row * es, p.v_head = a.v_head * es;
     p.o_row = a.out_row * es, p.o_head = a.out_head * es;
-    p.kp = a.k_cache_page * es, p.kt = a.k_cache_token * es, p.kh = a.k_cache_head * es, p.vp = a.v_cache_page * es, p.vt = a.v_cache_token * es, p.vh = a.v_cache_head * es;
+    p.kp = (unsigned)(a.k_cache_page * es), p.kt = (unsigned)(a.k_cache_token * es), p.kh = a.k_cache_head * es;
+    p.vp = (unsigned)(a.v_cache_page * es), p.vt = (unsigned)(a.v_cache_token * es), p.vh = a.v_cache_head * es;
     p.ld_tables = a.ld_tables;
     p.tokens = a.tokens, p.prompts = a.prompts, p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = a.heads / a.kv_heads, p.dim = a.dim;
     p.page = a.past ? a.page : 1, p.pages = a.pages, p.width = a.table_width;
+    const unsigned twice = 2 * (unsigned)p.page, lg = 31 - __builtin_clz(twice);
+    p.page_shift = (twice & (twice - 1)) ? lg : 0;
+    p.page_mul = (unsigned)((((uint64_t)1 << (32 + p.page_shift)) / twice) + (p.page_shift ? 1 : 0));
     p.direct = direct;
+    p.runs = direct && a.past && a.page % 16 == 0;
     const float scale = a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.dim);
     p.scale2 = fabsf(scale) * 1.44269504f;
     p.flip = scale < 0.f ? (a.dtype == TBS_F32 ? 0x80000000u : 0x80008000u) : 0;
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = a.dtype == TBS_F32 ? prompts_dims<float>(p, a, st) : a.dtype == TBS_BF16 ? prompts_dims<__bf16>(p, a, st) : prompts_dims<_Float16>(p, a, st);
+    const hipError_t e = a.dtype == TBS_F32 ? prompts_dims<float>(p, a, f, st) : a.dtype == TBS_BF16 ? prompts_dims<__bf16>(p, a, f, st) : prompts_dims<_Float16>(p, a, f, st);
     return e == hipSuccess ? TBS_OK : e == hipErrorInvalidValue ? TBS_EINVAL : TBS_EHIP;
 }
+
+extern "C" int tbs_attend_prompts(const tbs_attend_prompts_args *args, void *stream) { return prompts_call(args, 0, stream); }
+
+// one way of splitting the work, for the tests (not in the header)
+extern "C" int prompts_by(const tbs_attend_prompts_args *args, int force, void *stream) { return prompts_call(args, force, stream); }
+extern "C" int64_t prompts_by_workspace(const tbs_attend_prompts_args *args, int force) { return prompts_space(*args, prompts_form(*args, force)).bytes; }

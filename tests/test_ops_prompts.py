@@ -282,9 +282,35 @@ def _prompts_ref(q, k, v, lens, past, kc, vc, tables, page, scale, dtype):
     return ref, tol + _half_step(ref, dtype) * (1 + 2.0**-6) + 1e-30
 
 
-def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, layout="plain", cache_layout="token", holes=(), scale=None, seed=0, q_scale=1.0, into=None, width=0, shift=0):
+def _prompts_by(force, q, k, v, starts, past=None, k_cache=None, v_cache=None, tables=None, scale=None):
+    """attend_prompts with a workgroup to a tile of queries (force 1) or their keys shared out (2)."""
+    import ctypes
+    from paper_2302_14357_amd import ops
+    L = ops.load_library()
+    out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    a = ops._Prompts(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), starts=starts.data_ptr(), out=out.data_ptr(), q_row=q.stride(0), q_head=q.stride(1), k_row=k.stride(0), k_head=k.stride(1),
+                     v_row=v.stride(0), v_head=v.stride(1), out_row=out.stride(0), out_head=out.stride(1), tokens=q.shape[0], prompts=len(starts) - 1, heads=q.shape[1], kv_heads=k.shape[1],
+                     dim=q.shape[2], dtype=code[q.dtype], scale=scale or 0.0)
+    if past is not None:
+        a.past, a.tables, a.k_cache, a.v_cache = past.data_ptr(), tables.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
+        a.ld_tables, a.table_width, a.pages, a.page = tables.stride(0), tables.shape[1], k_cache.shape[0], k_cache.shape[1]
+        a.k_cache_page, a.k_cache_token, a.k_cache_head = k_cache.stride()[:3]
+        a.v_cache_page, a.v_cache_token, a.v_cache_head = v_cache.stride()[:3]
+    L.prompts_by_workspace.restype = ctypes.c_int64
+    n = L.prompts_by_workspace(ctypes.byref(a), force)
+    assert (n > 0) == (force == 2)
+    work = torch.full((n + 16,), 255, dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = work.data_ptr(), n
+    assert L.prompts_by(ctypes.byref(a), ctypes.c_int(force), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+    assert bool((work[n:] == 255).all())
+    return out
+
+
+def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, layout="plain", cache_layout="token", holes=(), scale=None, seed=0, q_scale=1.0, into=None, width=0, shift=0, force=0):
     """lens: new tokens of every prompt; past: tokens of each in the cache; pad: rows behind the last; holes: (prompt, column) entries that name no page;
-    into: None, "out" (with room around every head) or "q"."""
+    into: None, "out" (with room around every head) or "q"; force: as _prompts_by."""
     from paper_2302_14357_amd import attend_prompts
     g, r = _gen(seed + dim + page + sum(lens)), np.random.default_rng(seed + len(lens))
     tokens = sum(lens) + pad
@@ -322,7 +348,7 @@ def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, lay
         tables = torch.from_numpy(tables)
     starts = _i32(np.concatenate([[0], np.cumsum(lens)]) if len(lens) else [0])
     before = [t.clone() for t in (kd, vd)]
-    plain = attend_prompts(qd, kd, vd, starts, scale=scale, **kw)
+    plain = _prompts_by(force, qd, kd, vd, starts, scale=scale, **kw) if force else attend_prompts(qd, kd, vd, starts, scale=scale, **kw)
     assert torch.equal(kd.nan_to_num(nan=5e4), before[0].nan_to_num(nan=5e4)) and torch.equal(vd.nan_to_num(nan=5e4), before[1].nan_to_num(nan=5e4))
     if into == "out":
         big = torch.full((tokens + 2, heads + 1, dim + 8), 77.0, dtype=dtype, device="cuda")
@@ -334,7 +360,7 @@ def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, lay
     elif into == "q":
         assert attend_prompts(qd, kd, vd, starts, scale=scale, out=qd, **kw) is qd
         assert torch.equal(qd, plain)
-    else:
+    elif not force:
         assert torch.equal(attend_prompts(qd, kd, vd, starts, scale=scale, **kw), plain)
     ref, tol = _prompts_ref(q, k, v, lens, past, kc, vc, tables, page, scale, dtype)
     _close(plain, ref, tol)
@@ -361,6 +387,16 @@ def test_prompts_lengths(lens, dtype):
 @pytest.mark.parametrize("cache_layout", ["token", "head", "both"])
 def test_prompts_behind_a_cache(lens, past, page, dim, cache_layout, dtype):
     _prompts_case(lens, past=past, page=page, heads=6, kv=2, dim=dim, dtype=dtype, cache_layout=cache_layout, pad=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("force", [1, 2])
+@pytest.mark.parametrize("lens,past,dim,heads,kv", [([1], [5000], 64, 4, 4), ([200, 3], [700, 3000], 128, 8, 2), ([900], None, 64, 2, 2), ([1, 0, 40], [0, 9, 2000], 80, 6, 2), ([17, 150], [1500, 33], 256, 2, 1),
+                                                   ([5] * 100 + [600], None, 32, 2, 1), ([0, 0], [4, 5], 64, 2, 2), ([64, 1], [4096, 4095], 96, 3, 1)])
+def test_prompts_both_ways_of_sharing_the_work(lens, past, dim, heads, kv, force, dtype):
+    _prompts_case(lens, past=past, heads=heads, kv=kv, dim=dim, dtype=dtype, pad=3, force=force, page=16)
+    if past:
+        _prompts_case(lens, past=past, heads=heads, kv=kv, dim=dim, dtype=dtype, force=force, page=7, holes=[(0, 0), (len(lens) - 1, 2)] if min(past) > 21 else ())
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -458,6 +494,7 @@ def test_prompts_starts_in_no_order_stay_in_bounds(dtype):
     for starts in ([0, 50, 20, 100], [-5, 40, 1000], [2**31 - 1, -2**31, 100], [100, 0], [60, 60, 60], [0, 100, 0, 100, 0, 100], [30, 60]):
         big = torch.full((300, 2, 64), 77.0, dtype=dtype, device="cuda")
         attend_prompts(q, k, v, _i32(starts), out=big[100:200])
+        _prompts_by(2, q, k, v, _i32(starts))
         assert bool((big[:100] == 77.0).all()) and bool((big[200:] == 77.0).all())
     got = attend_prompts(q, k, v, _i32([30, 60]))   # (rows before the first prompt are nobody's, too)
     assert bool((got[:30] == 0).all()) and bool((got[60:] == 0).all())
