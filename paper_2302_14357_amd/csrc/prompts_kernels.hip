@@ -17,7 +17,6 @@
 #include "op_device.h"
 
 #define PROMPTS_SLACK 8.f
-#define PROMPTS_INLINE __attribute__((always_inline))   // (a function that is called would have everything that it looks at in memory)
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short prompts_b64;
 
 struct PromptsP {
@@ -28,7 +27,6 @@ struct PromptsP {
     unsigned kp, kt, vp, vt;
     int tokens, prompts, heads, kv_heads, group, dim, page, pages, width;
     bool direct;    // everything on 16-byte boundaries
-    bool runs;      // ... and sixteen keys from a multiple of sixteen on in one page
     unsigned page_mul, page_shift;
     float scale2;   // |scale| log2(e)
     unsigned flip;  // sign bits of a word of queries where the scale is negative
@@ -117,16 +115,22 @@ __device__ __forceinline__ const char *prompts_uniform(const char *x) {
     return (const char *)(uintptr_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
 }
 
-// A direct load to LDS from base + offset: no register pair of addresses a lane
-__device__ __forceinline__ void prompts_load_lds(const char *base, unsigned offset, unsigned lds) {
+// Direct loads to LDS, N up to four times 16 bytes a lane, from base + off[i] + 1024 i to lds + 1024 i + 16 lane: the instruction adds its own offset on both sides, so that
+// neither has an address to be made
+template <int N>
+__device__ __forceinline__ void prompts_load_lds(const char *base, unsigned off0, unsigned off1, unsigned off2, unsigned off3, unsigned lds) {
     unsigned m0_was;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(m0_was) : "s"(lds), "v"(offset), "s"(base) : "memory");
+    const unsigned to = __builtin_amdgcn_readfirstlane(lds);
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\ts_mov_b32 m0, %0" : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1) : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %5, %2 offset:2048\n\tglobal_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1), "v"(off2), "v"(off3) : "memory");
 }
-
-template <bool B>
-struct PromptsIs {
-    static constexpr bool value = B;
-};
 
 // The order of N matrix instructions and the R LDS reads that each wants: those of the first A instructions, then an instruction and the reads of the one A
 // behind it.  (All reads first would take 64 registers.)
@@ -141,296 +145,199 @@ __device__ __forceinline__ void prompts_interleave() {
     __builtin_amdgcn_sched_group_barrier(0x008, A < N ? A : N, 0);
 }
 
-// DP: dim rounded up to 32, 64, 96, 128 or 256; NW: waves of 32 rows each
-template <class T, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
-k_prompts(PromptsP p) {
+// What a workgroup does.  DP: dim rounded up to 32, 64, 96, 128 or 256; NW: waves of 32 rows each; SHARED: by the list of pieces (its few scalars more cost 7 % in
+// the loop).  A class whose functions are all inlined: everything in it is in registers.
+#define PROMPTS_INLINE __device__ __forceinline__
+template <class T, int DP, int NW, bool SHARED>
+struct PromptsWork {
     typedef PromptsTile<T, DP> Tile;
-    constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, KB = TK / 32, DB = DP / 32, KS = DP * (int)sizeof(T) / 32, ROWS = 32 * NW;
-    constexpr int CHUNKS = TK * PITCH / 64, MINE = (CHUNKS + NW - 1) / NW;   // loads of 64 pieces, and those of a wave
-    constexpr int VS = sizeof(T) == 4 ? 1 : DB;   // addresses of V
-    constexpr int RUN = 64 / PITCH;   // rows of a load
-    constexpr int KINDS = NW * RUN % 16 == 0 ? 1 : MINE;   // (the permutation repeats every sixteen rows)
-    __shared__ __align__(16) char s_kv[2][2][Tile::BYTES];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int kvh = (int)blockIdx.x % p.kv_heads, unit = (int)blockIdx.x / p.kv_heads;
-    PromptsPiece piece = {0, 0, 0, INT32_MAX, 0};
-    int2 found;
-    if (p.pieces) {
-        const int n = *p.count;
-        if (unit < n) piece = p.pieces[unit];
-        found = unit < n ? make_int2(piece.prompt, piece.tile) : make_int2(-1, n);
-    } else {
-        found = prompts_find(p, unit, ROWS);
-    }
-    if (found.x < 0) {   // rows of no prompt are 0: those before the first and behind the last, shared among the workgroups without a tile
-        const int first = p.prompts > 0 ? prompts_start(p, 0) : p.tokens, last = p.prompts > 0 ? max(prompts_start(p, p.prompts), first) : p.tokens;
-        const int spare = (int)gridDim.x / p.kv_heads - found.y, rows = first + p.tokens - last;
-        for (int i = unit - found.y; i < rows; i += spare) {
-            T *to = (T *)(p.out + (i < first ? i : last + i - first) * p.o_row + kvh * p.group * p.o_head);
-            for (int j = threadIdx.x; j < p.group * p.dim; j += 64 * NW) {
-                const int head = j / p.dim;
-                *(T *)((char *)to + head * p.o_head + (j - head * p.dim) * sizeof(T)) = (T)0.f;
-            }
-        }
-        return;
-    }
-    const int prompt = __builtin_amdgcn_readfirstlane(found.x), tile = __builtin_amdgcn_readfirstlane(found.y);
-    PromptsAt at = prompts_at(p, prompt);
-    at.start = __builtin_amdgcn_readfirstlane(at.start), at.n = __builtin_amdgcn_readfirstlane(at.n), at.past = __builtin_amdgcn_readfirstlane(at.past);   // (in scalar registers)
-    const int *table = p.past ? p.tables + prompt * p.ld_tables : nullptr;
-    const int rows = at.n * p.group, row0 = tile * ROWS;   // (below 2^31: tokens x heads is)
-    const int keys = at.past + (min(row0 + ROWS, rows) - 1) / p.group + 1, first_step = __builtin_amdgcn_readfirstlane(piece.k0), steps = min((keys + TK - 1) / TK, __builtin_amdgcn_readfirstlane(piece.k1));
-    // this lane's query, and the last key that it sees; the first and last of the wave's
-    const int row = row0 + wave * 32 + c, token = row / p.group;
-    const bool live = row < rows;
-    const int sees = live ? at.past + token : -1;
-    const int w0 = row0 + wave * 32, wave_first = w0 + 32 <= rows ? at.past + w0 / p.group : -1, wave_last = w0 < rows ? at.past + (min(w0 + 32, rows) - 1) / p.group : -1;
-    bool holes = false;   // whether some of its pages do not exist
-    if (at.past > 0) {
-        const int from = first_step * TK, to = min(at.past, steps * TK);
-        for (int i = (int)prompts_page(p, from) + threadIdx.x; from < to && i <= (int)prompts_page(p, to - 1); i += 64 * NW) holes |= (unsigned)table[i] >= (unsigned)p.pages;
-        holes = __syncthreads_or(holes);
-    }
+    static constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, DB = DP / 32, KS = DP * (int)sizeof(T) / 32, ROWS = 32 * NW;
+    static constexpr int CHUNKS = TK * PITCH / 64, MINE = (CHUNKS + NW - 1) / NW;   // loads of 64 pieces, and those of a wave
+    static constexpr int RUN = MINE * 64 / PITCH;                                   // rows of a wave's
+    static constexpr bool ALL = DP == PITCH * E;                                    // (dim = DP: no piece is missing)
+    static constexpr int VS = sizeof(T) == 4 ? 1 : DB;                              // addresses of V
+    static constexpr int KB = TK / 32;
+    // (float16: weights up to 2^7 more, so that small ones keep their digits: with the slack's 2^8 at most half its largest number)
+    static constexpr float MORE = __is_same(T, _Float16) ? 7.f : 0.f;
+    static constexpr bool KEY = false, VALUE = true;
+
+    const PromptsP &p;
+    char *kv;   // LDS: keys and values of two tiles
+    int lane, wave, c, h;
+    PromptsAt at;
+    const int *table;
+    int keys, first_step, steps;             // up to the last that a row of the workgroup sees; steps to do
+    int sees, wave_first, wave_last;         // the last key that this lane's query sees; the first and last of the wave's
+    bool holes;                              // whether some of its pages do not exist
+    bool runs;                               // whether a wave's keys of a tile lie in one page, on 16-byte boundaries
     uint4 q[KS];
-    {
-        const int head = kvh * p.group + row - token * p.group;
-        const T *src = (const T *)(p.q + (int64_t)(at.start + (live ? token : 0)) * p.q_row + (live ? head : 0) * p.q_head);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            q[s] = live && (s * 2 + h) * E < p.dim ? op_load16(src + (s * 2 + h) * E) : make_uint4(0, 0, 0, 0);
-            q[s].x ^= p.flip, q[s].y ^= p.flip, q[s].z ^= p.flip, q[s].w ^= p.flip;
-        }
-    }
+    const char *k_new, *v_new, *k_old, *v_old;
+    unsigned lds;
+    unsigned k_off[MINE], v_off[MINE];   // bytes of a lane's pieces from 3072 before the wave's first key, less 1024 times their number among four: in a page, and then among new tokens
+    bool k_in[MINE], v_in[MINE];         // (pieces behind the head's end are not there)
+    int id[MINE], v_id[MINE];            // the pages of the keys and of the values that are asked for next, looked up a tile ahead: of this lane's (a wave's may be one)
+    const char *k_at[KS], *v_at[VS];   // where this lane's fragments begin
+    floatx16 o[DB];
+    float m, l;
+    uint4 w[sizeof(T) == 4 ? 1 : TK / 16];   // a tile's weights (float32: in place of the scores)
+
+    PROMPTS_INLINE PromptsWork(const PromptsP &p_, char *kv_) : p(p_), kv(kv_) {}
 
     // ---- tiles into LDS: a lane's pieces are places of its rows
-    const char *k_new = p.k + (int64_t)at.start * p.k_row + kvh * p.k_head, *v_new = p.v + (int64_t)at.start * p.v_row + kvh * p.v_head;
-    const char *k_old = p.k_cache + kvh * p.kh, *v_old = p.v_cache + kvh * p.vh;
-    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&s_kv[0][0][0];
-    auto row_of = [&](int i, int lane) PROMPTS_INLINE { return ((wave + i * NW) * 64 + lane) / PITCH; };
-    auto piece_of = [&](int i, int lane, bool values) PROMPTS_INLINE {
-        return (((wave + i * NW) * 64 + lane) % PITCH) ^ (values ? Tile::v_swizzle(row_of(i, lane)) : Tile::k_swizzle(row_of(i, lane)));
-    };
-    // (for what is seldom wanted: worked out where it is, not kept in registers)
-    auto again = [&] PROMPTS_INLINE {
-        int x = lane;
+    // (what is seldom wanted is worked out where it is, not kept in registers)
+    static PROMPTS_INLINE int again() {
+        int x = threadIdx.x & 63;
         asm volatile("" : "+v"(x));
         return x;
-    };
-    // Bytes from the first key of a load: among new tokens, and in a page
-    unsigned k_new_off[KINDS], v_new_off[KINDS], k_old_off[KINDS], v_old_off[KINDS];
-    bool k_in[KINDS], v_in[KINDS];   // (pieces behind the head's end are not there)
-#pragma unroll
-    for (int i = 0; i < KINDS; ++i) {
-        const unsigned r = lane / PITCH, ks = piece_of(i, lane, false), vs = piece_of(i, lane, true);
-        k_new_off[i] = r * (unsigned)p.k_row + ks * 16, v_new_off[i] = r * (unsigned)p.v_row + vs * 16;
-        k_old_off[i] = r * p.kt + ks * 16, v_old_off[i] = r * p.vt + vs * 16;
-        k_in[i] = (int)ks * E < p.dim, v_in[i] = (int)vs * E < p.dim;
     }
-    // The pages of the tile that is asked for next, looked up a tile ahead: of this lane's keys, or, where a load's keys lie in one page, lane i has the i-th load's.
-    int id[MINE];
-    auto page_of = [&](int t) PROMPTS_INLINE { return t < at.past ? table[prompts_page(p, t)] : 0; };
-    auto look = [&](int step) PROMPTS_INLINE {
-        const int t0 = step * TK, lane = again();
-        if (t0 >= at.past) return;
-        if (p.runs) {
-            id[0] = lane < MINE ? page_of(t0 + (wave + lane * NW) * RUN) : 0;
+    PROMPTS_INLINE int row_of(int i, int lane) const { return ((wave * MINE + i) * 64 + lane) / PITCH; }
+    PROMPTS_INLINE int piece_of(int i, int lane, bool value) const {
+        return (((wave * MINE + i) * 64 + lane) % PITCH) ^ (value ? Tile::v_swizzle(row_of(i, lane)) : Tile::k_swizzle(row_of(i, lane)));
+    }
+    PROMPTS_INLINE bool takes_part(int i) const { return CHUNKS % NW == 0 || wave * MINE + i < CHUNKS; }
+    // where the pieces of a lane are: keys, or values, `bytes` apart
+    template <bool V>
+    PROMPTS_INLINE void places(unsigned bytes) {
+        const int lane = again();
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) (V ? v_off : k_off)[i] = (row_of(i, lane) - wave * RUN) * bytes + piece_of(i, lane, V) * 16 + (3 - i % 4) * 1024;
+    }
+    PROMPTS_INLINE int page_of(int t) const { return t < at.past ? table[prompts_page(p, t)] : 0; }
+    PROMPTS_INLINE void look(int step) {   // (the values follow the keys a tile later, with the pages of the last look)
+        const int t0 = step * TK;
+        if (t0 >= at.past + TK) return;
+        const int lane = again();
+        int x[MINE];
+        if (runs) {
+            x[0] = page_of(t0 + wave * RUN);
+#pragma unroll
+            for (int i = 1; i < MINE; ++i) x[i] = x[0];
         } else {
 #pragma unroll
-            for (int i = 0; i < MINE; ++i) id[i] = page_of(t0 + row_of(i, lane));
+            for (int i = 0; i < MINE; ++i) x[i] = page_of(t0 + row_of(i, lane));
         }
-    };
-    auto ask = [&](int step) PROMPTS_INLINE {
-        const int t0 = step * TK, buffer = step & 1;
-        const unsigned to = lds + buffer * 2 * Tile::BYTES;
-        const bool fresh = t0 >= at.past;
-        if (fresh ? p.direct && t0 + TK <= keys : p.runs && t0 + TK <= at.past) {   // new tokens or ones of the cache, all there: scalar addresses
-            constexpr bool SAME = KINDS == 1;
-            unsigned n[MINE], ko[KINDS], vo[KINDS];
 #pragma unroll
-            for (int i = 0; i < MINE; ++i) n[i] = fresh ? 0 : (unsigned)__builtin_amdgcn_readlane(id[0], i);   // (all of them before the first load: it would be waited for)
+        for (int i = 0; i < MINE; ++i) v_id[i] = id[i], id[i] = x[i];
+    }
+    template <bool V>
+    PROMPTS_INLINE void load(const char *from, unsigned to) {
+        from -= 3072;   // (offsets are unsigned)
+        constexpr int N = MINE < 4 ? MINE : 4;
+        auto off = [&](int i) __attribute__((always_inline)) { return V ? v_off[i] : k_off[i]; };
 #pragma unroll
-            for (int i = 0; i < KINDS; ++i) ko[i] = fresh ? k_new_off[i] : k_old_off[i], vo[i] = fresh ? v_new_off[i] : v_old_off[i];
+        for (int i = 0; i < MINE; i += N) {
+            if (ALL && p.dim == DP) {
+                if (takes_part(i)) prompts_load_lds<N>(from, off(i), off(N > 1 ? i + 1 : i), off(N > 2 ? i + 2 : i), off(N > 3 ? i + 3 : i), to + i * 1024);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MINE; ++i) {
-                const int chunk = wave + i * NW, t = t0 + chunk * RUN;
-                if (CHUNKS % NW && chunk >= CHUNKS) continue;
-                const char *k, *v;
-                if (fresh) {
-                    k = k_new + (int64_t)(t - at.past) * p.k_row;
-                    v = v_new + (int64_t)(t - at.past) * p.v_row;
-                } else {
-                    const unsigned use = n[i] < (unsigned)p.pages ? n[i] : 0, off = (unsigned)t - prompts_page(p, t) * (unsigned)p.page;   // (a page that does not exist: the first's, masked)
-                    k = k_old + (uint64_t)use * p.kp + off * p.kt;
-                    v = v_old + (uint64_t)use * p.vp + off * p.vt;
-                }
-                k = prompts_uniform(k), v = prompts_uniform(v);
-                if (k_in[SAME ? 0 : i]) prompts_load_lds(k, ko[SAME ? 0 : i], to + chunk * 1024);
-                if (v_in[SAME ? 0 : i]) prompts_load_lds(v, vo[SAME ? 0 : i], to + Tile::BYTES + chunk * 1024);
+                for (int j = 0; j < N; ++j)
+                    if (takes_part(i + j) && (V ? v_in[i + j] : k_in[i + j])) prompts_load_lds<1>(from + j * 1024, off(i + j), 0, 0, 0, to + (i + j) * 1024);
             }
+        }
+    }
+    template <bool V>
+    PROMPTS_INLINE void ask(int step) {
+        const int t0 = step * TK, buffer = step & 1, t = t0 + wave * RUN;
+        const unsigned to = lds + (buffer * 2 + V) * Tile::BYTES + wave * MINE * 1024;
+        const bool fresh = t0 >= at.past;
+        const char *newer = V ? v_new : k_new, *older = V ? v_old : k_old;
+        const int64_t row_bytes = V ? p.v_row : p.k_row;
+        const unsigned page_bytes = V ? p.vp : p.kp, token_bytes = V ? p.vt : p.kt;
+        if (fresh ? p.direct && t0 + TK <= keys : runs && t0 + TK <= at.past) {   // new tokens or ones of the cache, all there: scalar addresses
+            const char *from;
+            if (fresh) {
+                if (t0 < at.past + TK) places<V>((unsigned)row_bytes);   // (the first of the new ones)
+                from = newer + (int64_t)(t - at.past) * row_bytes;
+            } else {
+                const unsigned n = (unsigned)__builtin_amdgcn_readfirstlane(V ? v_id[0] : id[0]), use = n < (unsigned)p.pages ? n : 0;   // (a page that does not exist: the first's, masked)
+                from = older + (uint64_t)use * page_bytes + ((unsigned)t - prompts_page(p, t) * (unsigned)p.page) * token_bytes;
+            }
+            load<V>(prompts_uniform(from), to);
         } else {
             const int lane = again();
             int n[MINE];
             if (!fresh) {
 #pragma unroll
                 for (int i = 0; i < MINE; ++i) {
-                    n[i] = p.runs ? __builtin_amdgcn_readlane(id[0], i) : id[i];
-                    asm volatile("" : "+v"(n[i]));   // (here, before the first load)
+                    n[i] = V ? v_id[i] : id[i];
+                    asm volatile("" : "+v"(n[i]));   // (here, before the first load: it would be waited for)
                 }
             }
 #pragma unroll
             for (int i = 0; i < MINE; ++i) {
-                const int chunk = wave + i * NW;
-                if (CHUNKS % NW && chunk >= CHUNKS) continue;
-                const int t = min(t0 + row_of(i, lane), keys - 1);   // (behind the last: anything that is there)
-                const char *k = k_new + (int64_t)(t - at.past) * p.k_row, *v = v_new + (int64_t)(t - at.past) * p.v_row;
-                if (t < at.past) {
-                    const unsigned off = (unsigned)t - prompts_page(p, t) * (unsigned)p.page, use = (unsigned)n[i] < (unsigned)p.pages ? n[i] : 0;
-                    k = k_old + (uint64_t)use * p.kp + off * p.kt;
-                    v = v_old + (uint64_t)use * p.vp + off * p.vt;
+                if (!takes_part(i)) continue;
+                const int key = min(t0 + row_of(i, lane), keys - 1), piece = piece_of(i, lane, V);   // (behind the last: anything that is there)
+                const char *from = newer + (int64_t)(key - at.past) * row_bytes;
+                if (key < at.past) {
+                    const unsigned use = (unsigned)n[i] < (unsigned)p.pages ? n[i] : 0;
+                    from = older + (uint64_t)use * page_bytes + ((unsigned)key - prompts_page(p, key) * (unsigned)p.page) * token_bytes;
                 }
-                const int ks = piece_of(i, lane, false), vs = piece_of(i, lane, true);
-                if (p.direct) {
-                    if (ks * E < p.dim) op_load_lds(k + ks * 16, to + chunk * 1024);
-                    if (vs * E < p.dim) op_load_lds(v + vs * 16, to + Tile::BYTES + chunk * 1024);
-                } else {
-                    if (ks * E < p.dim) *(uint4 *)(&s_kv[buffer][0][0] + chunk * 1024 + lane * 16) = op_load16((const T *)k + ks * E);
-                    if (vs * E < p.dim) *(uint4 *)(&s_kv[buffer][1][0] + chunk * 1024 + lane * 16) = op_load16((const T *)v + vs * E);
-                }
+                if (piece * E >= p.dim) continue;
+                if (p.direct) op_load_lds(from + piece * 16, __builtin_amdgcn_readfirstlane(to + i * 1024));
+                else *(uint4 *)(kv + (buffer * 2 + V) * Tile::BYTES + (wave * MINE + i) * 1024 + lane * 16) = op_load16((const T *)from + piece * E);
             }
         }
-    };
-    auto landed = [&]() PROMPTS_INLINE {
+    }
+    static PROMPTS_INLINE void landed() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-    };
-    // pieces behind the head's end are 0 in both buffers, and stay so
-    if (p.dim < PITCH * E) {
-        for (int i = threadIdx.x; i < 4 * TK * PITCH; i += 64 * NW) {
-            const int in = i % (TK * PITCH), r = in / PITCH, slot = in % PITCH;
-            if ((slot ^ ((i / (TK * PITCH)) & 1 ? Tile::v_swizzle(r) : Tile::k_swizzle(r))) * E >= p.dim) ((uint4 *)&s_kv[0][0][0])[i] = make_uint4(0, 0, 0, 0);
-        }
     }
 
-    // ---- fragments: where this lane's begin
-    const char *k_at[KS], *v_at[VS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) k_at[s] = &s_kv[0][0][0] + (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
-    const int v_row = sizeof(T) == 4 ? 4 * h : 4 * h + (lane >> 2 & 3);
-    auto v_place = [&](int d) PROMPTS_INLINE {
-        return &s_kv[0][1][0] + (sizeof(T) == 4 ? v_row * PITCH * 16 : (v_row * PITCH + ((d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ Tile::v_swizzle(v_row))) * 16 + (lane & 1) * 8);
-    };
-#pragma unroll
-    for (int d = 0; d < VS; ++d) v_at[d] = v_place(d);
-    // V^T of 16 keys from `key` on (in the order of the weights) and the d-th 32 dimensions
-    auto v_frag = [&](auto apart, int buffer, int key, int d) PROMPTS_INLINE {
+    // ---- fragments
+    PROMPTS_INLINE uint4 k_frag(int step, int b, int j) const {   // 32 keys, two pieces
+        return *(const uint4 *)(k_at[j] + (step & 1) * 2 * Tile::BYTES + b * 32 * PITCH * 16);
+    }
+    PROMPTS_INLINE int v_row() const { return sizeof(T) == 4 ? 4 * h : 4 * h + (lane >> 2 & 3); }
+    PROMPTS_INLINE const char *v_place(int d) const {
+        return kv + Tile::BYTES + (sizeof(T) == 4 ? v_row() * PITCH * 16 : (v_row() * PITCH + ((d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ Tile::v_swizzle(v_row()))) * 16 + (lane & 1) * 8);
+    }
+    // V^T of 16 keys from `key` on (in the order of the weights) and 32 dimensions from `from` on
+    static PROMPTS_INLINE uint4 v_frag(const char *from, int step, int key) {
         uint4 u;
         typedef __attribute__((address_space(3))) prompts_b64 *Lds;
-        const char *from = (apart.value ? v_place(d) : v_at[d]) + buffer * 2 * Tile::BYTES;
+        from += (step & 1) * 2 * Tile::BYTES;
         const prompts_b64 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + key * PITCH * 16)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + (key + 8) * PITCH * 16));
         __builtin_memcpy(&u, &x, 8);
         __builtin_memcpy((char *)&u + 8, &y, 8);
         return u;
-    };
-    auto v_one = [&](int buffer, int key, int d) PROMPTS_INLINE {   // float32: dimension 32 d + c of key `key` + 4 h
-        return *(const float *)(v_at[0] + buffer * 2 * Tile::BYTES + key * PITCH * 16 + (((d * 8 + c / 4) ^ (PITCH >= 16 ? h << 3 : 0)) * 16 + c % 4 * 4));
-    };
-    // which keys of a tile there are (bit i: key i), for all of the wave
-    constexpr unsigned long long WHOLE = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
-    auto there_of = [&](int step) PROMPTS_INLINE {
+    }
+    PROMPTS_INLINE float v_one(int step, int key, int d) const {   // float32: dimension 32 d + c of key `key` + 4 h
+        return *(const float *)(v_at[0] + (step & 1) * 2 * Tile::BYTES + key * PITCH * 16 + (((d * 8 + c / 4) ^ (PITCH >= 16 ? h << 3 : 0)) * 16 + c % 4 * 4));
+    }
+    // which of a tile's keys there are (bit i: key i), for all of the wave
+    static constexpr unsigned long long WHOLE = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
+    PROMPTS_INLINE unsigned long long there_of(int step) const {
         const int t0 = step * TK;
         unsigned long long there = keys - t0 >= TK ? WHOLE : (1ull << (keys - t0)) - 1;
         if (holes && t0 < at.past) {
-            const int t = t0 + (lane & (TK - 1));
+            const int t = t0 + (int)(threadIdx.x & (TK - 1));
             there &= __ballot(t >= at.past || (unsigned)page_of(t) < (unsigned)p.pages);
         }
         return there;
-    };
+    }
     // ... and which of them this lane's query sees
-    auto mine_of = [&](int step, unsigned long long there) PROMPTS_INLINE {
+    PROMPTS_INLINE unsigned long long mine_of(int step, unsigned long long there) const {
         const int last = sees - step * TK;   // (its last key's place)
         return last < 0 ? 0 : last >= 63 ? there : there & ((2ull << last) - 1);
-    };
+    }
+    PROMPTS_INLINE bool mixed(int step, unsigned long long there) const { return there != WHOLE || step * TK + TK - 1 > wave_first; }   // some key is not some query's
 
-    floatx16 o[DB];
-    float m, l;
-    // (float16: weights up to 2^7 more, so that small ones keep their digits: with the slack's 2^8 at most half its largest number)
-    constexpr float MORE = __is_same(T, _Float16) ? 7.f : 0.f;
-
-    // All tiles.  A value that is NaN or infinite reaches, times the weight 0, the queries that do not see it; nothing of this pass is kept then, and in others, of 32
-    // dimensions each (apart: those from 32 d0 on, in o[0]), the keys of a tile that some query does not see all of are added one by one to the queries that see them.
-    auto pass = [&](auto apart, int d0) PROMPTS_INLINE {
-    constexpr int DB = apart.value ? 1 : DP / 32;
-    floatx16 s[KB];
-    uint4 w[sizeof(T) == 4 ? 1 : TK / 16];   // a tile's weights
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] = floatx16{};
-    m = -INFINITY, l = 0.f;
-    // the weights of tile `step` with its values
-    auto values = [&](int step, unsigned long long there) PROMPTS_INLINE {
-        const int buffer = step & 1;
-        if (!apart.value || (there == WHOLE && step * TK + TK - 1 <= wave_first)) {
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_one(buffer, 8 * (i / 4) + i % 4, d0 + d), s[0][i], o[d], 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int i = 0; i < TK / 16; ++i)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(apart, buffer, i * 16, d0 + d), w[i], o[d]);
-                prompts_interleave<TK / 16 * DB, 2, 4>();
-            }
-            return;
-        }
-        const unsigned long long mine = mine_of(step, there);
-#pragma unroll 1
-        for (int key = 0; key < TK; ++key) {
-            const bool seen = mine >> key & 1;
-            if (!__any(seen)) continue;
-            const int half = key >> 2 & 1;   // its place in the fragments: half, and element
-            uint4 x, y = make_uint4(0, 0, 0, 0);
-            float one = 0.f;
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) one = 8 * (i / 4) + i % 4 == (key & ~4) ? s[0][i] : one;
-            } else {
-#pragma unroll
-                for (int i = 0; i < TK / 16; ++i)
-                    if (i == key >> 4) y = w[i];
-            }
-            const int e = (key >> 3 & 1) * 4 + (key & 3);
-            const unsigned keep = h == half ? (e & 1 ? 0xffff0000u : 0xffffu) : 0;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                floatx16 z = {};
-                if constexpr (sizeof(T) == 4) {
-                    const float v = v_one(buffer, key & ~4, d0 + d);
-                    z = __builtin_amdgcn_mfma_f32_32x32x2f32(h == half ? v : 0.f, h == half && seen ? one : 0.f, z, 0, 0, 0);
-                } else {
-                    x = v_frag(apart, buffer, key & ~15, d0 + d);
-                    x.x &= e / 2 == 0 ? keep : 0, x.y &= e / 2 == 1 ? keep : 0, x.z &= e / 2 == 2 ? keep : 0, x.w &= e / 2 == 3 ? keep : 0;
-                    z = op_mma32<T>(x, y, z);
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[d][j] = seen ? o[d][j] + z[j] : o[d][j];
-            }
-        }
-    };
-    auto scores = [&](int step) PROMPTS_INLINE {
-        const int buffer = (step & 1) * 2 * Tile::BYTES;
+    PROMPTS_INLINE void scores(floatx16 (&s)[KB], int step) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < KS; ++j)
 #pragma unroll
-            for (int b = 0; b < KB; ++b) s[b] = op_mma32<T>(*(const uint4 *)(k_at[j] + buffer + b * 32 * PITCH * 16), q[j], j == 0 ? floatx16{} : s[b]);
+            for (int b = 0; b < KB; ++b) s[b] = op_mma32<T>(k_frag(step, b, j), q[j], j == 0 ? floatx16{} : s[b]);
         if constexpr (sizeof(T) == 2) prompts_interleave<KS * KB, 1, 4>();
-    };
-    auto softmax = [&](int step, unsigned long long there) PROMPTS_INLINE {
-        const int t0 = step * TK;
-        if (there != WHOLE || t0 + TK - 1 > wave_first) {
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // Scores into weights.  D: how many times 32 dimensions are in o.
+    template <int D>
+    PROMPTS_INLINE void softmax(floatx16 (&s)[KB], int step, unsigned long long there) {
+        if (mixed(step, there)) {
             const unsigned long long bits = mine_of(step, there) >> (4 * h);
 #pragma unroll
             for (int b = 0; b < KB; ++b)
@@ -442,105 +349,256 @@ k_prompts(PromptsP p) {
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        {
-            typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
-            const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
-        }
+        typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
+        const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);   // (this lane's and its other half's)
+        top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
         if (__any(top > m + PROMPTS_SLACK)) {
             const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
             m = m1;
             l *= a;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < D; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= a;
         }
         const float base = m == -INFINITY ? 0.f : m - MORE;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int i = 0; i < TK / 16; ++i) {
+            T x[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], p.scale2, -base));
-                sum[i & 1] += s[b][i];
+            for (int j = 0; j < 8; ++j) {
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + j], p.scale2, -base));
+                if constexpr (sizeof(T) == 4) s[i / 2][i % 2 * 8 + j] = y;
+                sum[j & 1] += y;
+                x[j] = (T)y;
             }
-        l += sum[0] + sum[1];
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < TK / 16; ++i) {
-                T x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = (T)s[i / 2][i % 2 * 8 + j];
-                __builtin_memcpy(&w[i], x, 16);
-            }
+            if constexpr (sizeof(T) == 2) __builtin_memcpy(&w[i], x, 16);
         }
-    };
+        l += sum[0] + sum[1];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    PROMPTS_INLINE void values(const floatx16 (&s)[KB], int step) {   // the weights with their values
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 16 * KB; ++i)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_one(step, i / 16 * 32 + 8 * (i % 16 / 4) + i % 4, d), s[i / 16][i % 16], o[d], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TK / 16; ++i)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(v_at[d], step, i * 16), w[i], o[d]);
+            prompts_interleave<TK / 16 * DB, 2, 4>();
+        }
+        __builtin_amdgcn_s_setprio(0);
+    }
 
-    look(first_step);
-    ask(first_step);
-    look(first_step + 1);
-    landed();
-    for (int step = first_step; step < steps; ++step) {
+    PROMPTS_INLINE void start() {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = floatx16{};
+        m = -INFINITY, l = 0.f;
+        if (first_step * TK < at.past) places<false>(p.kt), places<true>(p.vt);
+        else if (first_step * TK >= at.past + TK) places<false>((unsigned)p.k_row), places<true>((unsigned)p.v_row);   // (ask() has them with the first new tile)
+    }
+    // a tile's values, and the keys of the next one
+    PROMPTS_INLINE void ask_for(int step) {
+        if (step < steps) ask<true>(step);
         if (step + 1 < steps) {
-            ask(step + 1);
+            ask<false>(step + 1);
             look(step + 2);
         }
-        if (step * TK <= wave_last) {
-            const unsigned long long there = there_of(step);
-            __builtin_amdgcn_s_setprio(1);
-            scores(step);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            softmax(step, there);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            values(step, there);
-            __builtin_amdgcn_s_setprio(0);
-        }
-        if (step + 1 < steps) landed();   // the next tile is there, and everybody has read this one
     }
-    };
-
-    auto store = [&](const floatx16 &x, int d) PROMPTS_INLINE {
-        const float sum = l + __shfl_xor(l, 32), f = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
-        if (!live) return;
-        if (piece.apart) {
-            const int64_t at = ((int64_t)unit * p.kv_heads + kvh) * ROWS + wave * 32 + c;
+    // All tiles.  A value that is NaN or infinite reaches, times the weight 0, the queries that do not see it; nothing of this pass is kept then.
+    PROMPTS_INLINE void pass() {
+        start();
+        floatx16 s[KB];
+        const int mine = min(steps, wave_last < 0 ? 0 : wave_last / TK + 1);   // steps in which the wave has something to do
+        int step = first_step;
+        look(step);
+        ask<false>(step);
+        look(step + 1);
+        landed();
+        ask_for(step);
+        if (step < mine) {
+            scores(s, step);
+            for (;;) {
+                softmax<DB>(s, step, there_of(step));
+                landed();
+                ask_for(step + 1);
+                values(s, step);
+                if (++step >= mine) break;
+                __builtin_amdgcn_sched_barrier(0);
+                scores(s, step);
+            }
+        }
+        for (; step < steps; ++step) {   // (the others have)
+            landed();
+            ask_for(step + 1);
+        }
+    }
+    // The d-th 32 dimensions, in o[0]; the keys of a tile that some query does not see all of are added one by one to the queries that see them.
+    PROMPTS_INLINE void pass_apart(int d) {
+        start();
+        const char *place = v_place(sizeof(T) == 4 ? 0 : d);
+        for (int step = first_step; step < steps; ++step) {
+            look(step);
+            ask<false>(step);
+            look(step + 1);
+            ask<true>(step);
+            landed();
+            if (step * TK <= wave_last) {
+                const unsigned long long there = there_of(step);
+                floatx16 s[KB];
+                scores(s, step);
+                softmax<1>(s, step, there);
+                const unsigned long long mine = mixed(step, there) ? mine_of(step, there) : ~0ull;
+#pragma unroll 1
+                for (int key = 0; key < TK; ++key) {
+                    const bool seen = mine >> key & 1;
+                    if (!__any(seen)) continue;
+                    const int half = key >> 2 & 1;   // its place in the fragments: half, and element
+                    floatx16 z = {};
+                    if constexpr (sizeof(T) == 4) {
+                        float one = 0.f;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (d * 32 + b * 8 + h * 4 < p.dim) *(float4 *)(p.part_o + at * p.dim + d * 32 + b * 8 + h * 4) = make_float4(x[b * 4], x[b * 4 + 1], x[b * 4 + 2], x[b * 4 + 3]);
-            if (h == 0 && d == 0) *(float2 *)(p.part_ml + at * 2) = make_float2(m, sum);
+                        for (int i = 0; i < 16 * KB; ++i) one = i / 16 * 32 + 8 * (i % 16 / 4) + i % 4 == (key & ~4) ? s[i / 16][i % 16] : one;
+                        const float v = v_one(step, key & ~4, d);
+                        z = __builtin_amdgcn_mfma_f32_32x32x2f32(h == half ? v : 0.f, h == half && seen ? one : 0.f, z, 0, 0, 0);
+                    } else {
+                        const int e = (key >> 3 & 1) * 4 + (key & 3);
+                        const unsigned keep = h == half ? (e & 1 ? 0xffff0000u : 0xffffu) : 0;
+                        uint4 x = v_frag(place, step, key & ~15), y = w[0];
+#pragma unroll
+                        for (int i = 1; i < TK / 16; ++i)
+                            if (i == key >> 4) y = w[i];
+                        x.x &= e / 2 == 0 ? keep : 0, x.y &= e / 2 == 1 ? keep : 0, x.z &= e / 2 == 2 ? keep : 0, x.w &= e / 2 == 3 ? keep : 0;
+                        z = op_mma32<T>(x, y, z);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[0][j] = seen ? o[0][j] + z[j] : o[0][j];
+                }
+            }
+            landed();
+        }
+    }
+
+    PROMPTS_INLINE void run() {
+        lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+        const int kvh = (int)blockIdx.x % p.kv_heads, unit = (int)blockIdx.x / p.kv_heads;
+        PromptsPiece piece = {0, 0, 0, INT32_MAX, 0};
+        int2 found;
+        if (SHARED) {
+            const int n = *p.count;
+            if (unit < n) piece = p.pieces[unit];
+            found = unit < n ? make_int2(piece.prompt, piece.tile) : make_int2(-1, n);
+        } else {
+            found = prompts_find(p, unit, ROWS);
+        }
+        if (found.x < 0) {   // rows of no prompt are 0: those before the first and behind the last, shared among the workgroups without a tile
+            const int first = p.prompts > 0 ? prompts_start(p, 0) : p.tokens, last = p.prompts > 0 ? max(prompts_start(p, p.prompts), first) : p.tokens;
+            const int spare = (int)gridDim.x / p.kv_heads - found.y, rows = first + p.tokens - last;
+            for (int i = unit - found.y; i < rows; i += spare) {
+                T *to = (T *)(p.out + (i < first ? i : last + i - first) * p.o_row + kvh * p.group * p.o_head);
+                for (int j = threadIdx.x; j < p.group * p.dim; j += 64 * NW) {
+                    const int head = j / p.dim;
+                    *(T *)((char *)to + head * p.o_head + (j - head * p.dim) * sizeof(T)) = (T)0.f;
+                }
+            }
             return;
         }
-        char *to = p.out + (int64_t)(at.start + token) * p.o_row + (kvh * p.group + row - token * p.group) * p.o_head;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int e = d * 32 + b * 8 + h * 4;   // (dim is a multiple of 8)
-            if (e >= p.dim) continue;
-            T y[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = (T)(sum == 0.f ? 0.f : x[b * 4 + i] * f);
-            __builtin_memcpy((T *)to + e, y, sizeof y);
+        const int prompt = __builtin_amdgcn_readfirstlane(found.x), tile = __builtin_amdgcn_readfirstlane(found.y);
+        at = prompts_at(p, prompt);
+        at.start = __builtin_amdgcn_readfirstlane(at.start), at.n = __builtin_amdgcn_readfirstlane(at.n), at.past = __builtin_amdgcn_readfirstlane(at.past);   // (in scalar registers)
+        table = p.past ? p.tables + prompt * p.ld_tables : nullptr;
+        const int rows = at.n * p.group, row0 = tile * ROWS;   // (below 2^31: tokens x heads is)
+        keys = at.past + (min(row0 + ROWS, rows) - 1) / p.group + 1;
+        first_step = __builtin_amdgcn_readfirstlane(piece.k0), steps = min((keys + TK - 1) / TK, __builtin_amdgcn_readfirstlane(piece.k1));
+        const int row = row0 + wave * 32 + c, token = row / p.group, w0 = row0 + wave * 32;
+        const bool live = row < rows;
+        sees = live ? at.past + token : -1;
+        wave_first = w0 + 32 <= rows ? at.past + w0 / p.group : -1, wave_last = w0 < rows ? at.past + (min(w0 + 32, rows) - 1) / p.group : -1;
+        holes = false, runs = p.direct && p.page % RUN == 0;
+        if (at.past > 0) {
+            const int from = first_step * TK, to = min(at.past, steps * TK);
+            for (int i = (int)prompts_page(p, from) + threadIdx.x; from < to && i <= (int)prompts_page(p, to - 1); i += 64 * NW) holes |= (unsigned)table[i] >= (unsigned)p.pages;
+            holes = __syncthreads_or(holes);
         }
-    };
-    pass(PromptsIs<false>(), 0);
-    float none = 0.f;
+        {
+            const int head = kvh * p.group + row - token * p.group;
+            const T *src = (const T *)(p.q + (int64_t)(at.start + (live ? token : 0)) * p.q_row + (live ? head : 0) * p.q_head);
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+            for (int s = 0; s < KS; ++s) {
+                q[s] = live && (s * 2 + h) * E < p.dim ? op_load16(src + (s * 2 + h) * E) : make_uint4(0, 0, 0, 0);
+                q[s].x ^= p.flip, q[s].y ^= p.flip, q[s].z ^= p.flip, q[s].w ^= p.flip;
+            }
+        }
+        k_new = p.k + (int64_t)at.start * p.k_row + kvh * p.k_head, v_new = p.v + (int64_t)at.start * p.v_row + kvh * p.v_head;
+        k_old = p.k_cache + kvh * p.kh, v_old = p.v_cache + kvh * p.vh;
+        lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)kv;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) none = fmaf(o[d][i], 0.f, none);
-    if (!__syncthreads_or(live && none != 0.f)) {
+        for (int i = 0; i < MINE; ++i) k_in[i] = piece_of(i, lane, false) * E < p.dim, v_in[i] = piece_of(i, lane, true) * E < p.dim;
+        // pieces behind the head's end are 0 in both buffers, and stay so
+        if (p.dim < PITCH * E) {
+            for (int i = threadIdx.x; i < 4 * TK * PITCH; i += 64 * NW) {
+                const int in = i % (TK * PITCH), r = in / PITCH, slot = in % PITCH;
+                if ((slot ^ ((i / (TK * PITCH)) & 1 ? Tile::v_swizzle(r) : Tile::k_swizzle(r))) * E >= p.dim) ((uint4 *)kv)[i] = make_uint4(0, 0, 0, 0);
+            }
+        }
 #pragma unroll
-        for (int d = 0; d < DB; ++d) store(o[d], d);
-    } else {
+        for (int s = 0; s < KS; ++s) k_at[s] = kv + (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
+#pragma unroll
+        for (int d = 0; d < VS; ++d) v_at[d] = v_place(d);
+
+        auto store = [&](const floatx16 &x, int d) __attribute__((always_inline)) {
+            const float sum = l + __shfl_xor(l, 32), f = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
+            if (!live) return;
+            if (SHARED && piece.apart) {
+                const int64_t place = ((int64_t)unit * p.kv_heads + kvh) * ROWS + wave * 32 + c;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (d * 32 + b * 8 + h * 4 < p.dim) *(float4 *)(p.part_o + place * p.dim + d * 32 + b * 8 + h * 4) = make_float4(x[b * 4], x[b * 4 + 1], x[b * 4 + 2], x[b * 4 + 3]);
+                if (h == 0 && d == 0) *(float2 *)(p.part_ml + place * 2) = make_float2(m, sum);
+                return;
+            }
+            char *to = p.out + (int64_t)(at.start + token) * p.o_row + (kvh * p.group + row - token * p.group) * p.o_head;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int e = d * 32 + b * 8 + h * 4;   // (dim is a multiple of 8)
+                if (e >= p.dim) continue;
+                T y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = (T)(sum == 0.f ? 0.f : x[b * 4 + i] * f);
+                __builtin_memcpy((T *)to + e, y, sizeof y);
+            }
+        };
+        pass();
+        float none = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) none = fmaf(o[d][i], 0.f, none);
+        if (!__syncthreads_or(live && none != 0.f)) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) store(o[d], d);
+        } else {
 #pragma unroll 1
-        for (int d = 0; d < DB; ++d) {
-            pass(PromptsIs<true>(), d);
-            store(o[0], d);
-            __syncthreads();
+            for (int d = 0; d < DB; ++d) {
+                pass_apart(d);
+                store(o[0], d);
+                __syncthreads();
+            }
         }
     }
+};
+
+template <class T, int DP, int NW, bool SHARED>
+__global__ void __launch_bounds__(64 * NW, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
+k_prompts(PromptsP p) {
+    __shared__ __align__(16) char s_kv[4 * PromptsTile<T, DP>::BYTES];
+    PromptsWork<T, DP, NW, SHARED> work(p, s_kv);
+    work.run();
 }
 
 #define PROMPTS_PLAN 1024     // threads of the plan; tiles, and prompts, at most
@@ -693,8 +751,9 @@ static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (f.waves == 2) hipLaunchKernelGGL((k_prompts<T, DP, 2>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_prompts<T, DP, 4>), grid, block, 0, st, p);
+    if (f.waves == 2) hipLaunchKernelGGL((k_prompts<T, DP, 2, false>), grid, block, 0, st, p);
+    else if (f.shared) hipLaunchKernelGGL((k_prompts<T, DP, 4, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_prompts<T, DP, 4, false>), grid, block, 0, st, p);
     if (f.shared) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -750,7 +809,7 @@ static int prompts_call(const tbs_attend_prompts_args *args, int force, void *st
     const int64_t wide[] = {a.k_cache_token * es * a.page, a.v_cache_token * es * a.page, a.k_cache_page * es, a.v_cache_page * es, a.k_row * es * 64, a.v_row * es * 64};
     for (int i = 0; i < 6; ++i)
         if ((i >= 4 || (a.past && (i < 2 || a.pages > 1))) && wide[i] > INT32_MAX) {
-            if (i < 4 ? wide[i] > UINT32_MAX : a.tokens > 1) return TBS_EINVAL;
+            if (i < 4 ? wide[i] > UINT32_MAX - 8192ll : a.tokens > 1) return TBS_EINVAL;
         }
     // what is written lies neither over itself nor over what others read; queries are read by those who write in their place
     const OpHeads q = {a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head}, out = {a.out, a.tokens, a.heads, a.dim, a.out_row, a.out_head};
@@ -778,7 +837,6 @@ static int prompts_call(const tbs_attend_prompts_args *args, int force, void *st
     p.page_shift = (twice & (twice - 1)) ? lg : 0;
     p.page_mul = (unsigned)((((uint64_t)1 << (32 + p.page_shift)) / twice) + (p.page_shift ? 1 : 0));
     p.direct = direct;
-    p.runs = direct && a.past && a.page % 16 == 0;
     const float scale = a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.dim);
     p.scale2 = fabsf(scale) * 1.44269504f;
     p.flip = scale < 0.f ? (a.dtype == TBS_F32 ? 0x80000000u : 0x80008000u) : 0;
