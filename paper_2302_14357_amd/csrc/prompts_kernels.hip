@@ -602,14 +602,23 @@ k_prompts(PromptsP p) {
 }
 
 #define PROMPTS_PLAN 1024     // threads of the plan; tiles, and prompts, at most
-#define PROMPTS_SLOTS 512     // workgroups that the chip runs at a time, two a CU
+#define PROMPTS_LENGTHS 16    // lengths of pieces that are looked at
+#define PROMPTS_PIECES 4      // pieces of an equal share at most
+__device__ const int prompts_parts[PROMPTS_LENGTHS] = {16, 18, 20, 22, 25, 28, 32, 36, 40, 44, 50, 56, 64, 96, 128, 0};   // 64ths of a share; 0: whole tiles
 
-// Whose keys are shared, one workgroup: a thread a tile.  A piece is at most `len` steps long; of eight lengths, from an equal share of all work up, the one whose
-// pieces take the fewest steps one after the other in the slots that there are, with three more for a piece's start and end and eight for the join.
+// workgroups of four waves that the chip runs at a time: one to three a CU, by their registers
+static int prompts_slots(const tbs_attend_prompts_args &a) { return 256 * (a.dtype == TBS_F32 ? (a.dim <= 64 ? 2 : 1) : a.dim <= 64 ? 3 : a.dim <= 128 ? 2 : 1); }
+
+// Whose keys are shared, one workgroup: a thread a tile, or prompt.  A piece is at most `len` steps long: of sixteen lengths, from a quarter of an equal share of all work up, the one that
+// is estimated to take the fewest steps one after the other.  That is the turns that the slots take, whole ones, of a mean piece and eight steps for its start, its end and the way
+// of its sums through memory; where one turn is enough, the longest piece; and six steps for the join.  (Measured by the lengths, in shares.  Four chunks of 100 to 512
+// tokens behind 20001 to 60000, 32 heads of 128: 1/4 1153 us, 1/3 1128, 1/2 1304, 2/3 1067, 1 1326, all 2254.  256 tokens behind 100000, 8 heads: 1/4 291, 2/3 270, 1 204, 3/2 242, all 3945.
+// 2100 tokens, 8 heads: 1/4 51, 1/3 42, 1/2 45, 1 52, all 84.  4000 in float32: 1/4 778, 1 803, all 689.)
 __global__ void __launch_bounds__(PROMPTS_PLAN)
-k_prompts_plan(PromptsP p, int rows, int step, int most) {
-    __shared__ int s_first[PROMPTS_PLAN], s_wave[PROMPTS_PLAN / 64], s_sum[8], s_longest;
+k_prompts_plan(PromptsP p, int rows, int step, int most, int slots) {
+    __shared__ int s_first[PROMPTS_PLAN], s_wave[PROMPTS_PLAN / 64], s_sum[PROMPTS_LENGTHS], s_longest;
     __shared__ unsigned long long s_all;
+    __shared__ int4 s_tile[PROMPTS_PLAN];
     const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
     auto before = [&](int x, int *all) {   // the sum over smaller threads, and over all
         int sum = x;
@@ -622,14 +631,14 @@ k_prompts_plan(PromptsP p, int rows, int step, int most) {
         if (lane == 63) s_wave[wave] = sum;
         __syncthreads();
         int less = sum - x, total = 0;
-        for (int j = 0; j < PROMPTS_PLAN / 64; ++j) {
+        for (int j = 0; j < (int)blockDim.x / 64; ++j) {
             less += j < wave ? s_wave[j] : 0;
             total += s_wave[j];
         }
         *all = total;
         return less;
     };
-    if (i < 8) s_sum[i] = 0;
+    if (i < PROMPTS_LENGTHS) s_sum[i] = 0;   // (there is a wave at least)
     if (i == 0) s_longest = 0, s_all = 0;
     int tiles;
     const int mine = i < p.prompts ? (prompts_length(p, i) * p.group + rows - 1) / rows : 0;
@@ -646,30 +655,56 @@ k_prompts_plan(PromptsP p, int rows, int step, int most) {
         const int count = (at.n * p.group + rows - 1) / rows;
         tile = count - 1 - (i - s_first[prompt]);   // (a prompt's last tiles, which have the most keys, first)
         steps = (at.past + (min(tile * rows + rows, at.n * p.group) - 1) / p.group + 1 + step - 1) / step;
-        atomicAdd(&s_all, (unsigned long long)steps);
-        atomicMax(&s_longest, steps);
+    }
+    int64_t all_steps = steps;
+    int most_steps = steps;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) all_steps += __shfl_xor(all_steps, k), most_steps = max(most_steps, __shfl_xor(most_steps, k));
+    if (lane == 0 && most_steps > 0) {
+        atomicAdd(&s_all, (unsigned long long)all_steps);
+        atomicMax(&s_longest, most_steps);
     }
     __syncthreads();
     const int longest = max(s_longest, 1);
-    const int64_t share = max((int64_t)(s_all * p.kv_heads + PROMPTS_SLOTS - 1) / PROMPTS_SLOTS, (int64_t)4);
-    auto length = [&](int j) { return j == 7 ? longest : (int)min((int64_t)longest, j < 4 ? share + share * j / 8 : share * (j - 1) / 2); };   // 1, 9/8, 10/8, 11/8, 3/2, 2, 5/2 shares, and all
-    if (i < tiles)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) atomicAdd(&s_sum[j], (steps + length(j) - 1) / length(j));
+    const int64_t all = (int64_t)s_all, share = max((all * p.kv_heads + slots - 1) / slots, (int64_t)4 * PROMPTS_PIECES);
+    // a lane a length, and a quarter of the wave's tiles
+    const int part = prompts_parts[lane & (PROMPTS_LENGTHS - 1)], length = part ? (int)min((int64_t)longest, (share * part + 63) / 64) : longest;
+    if (wave * 64 < tiles) {
+        int n = 0;
+        for (int k = 0; k < PROMPTS_LENGTHS; ++k) n += (int)((unsigned)(__shfl(steps, (lane & ~(PROMPTS_LENGTHS - 1)) + k) + length - 1) / (unsigned)length);   // (of no tile: none)
+        n += __shfl_xor(n, 16);
+        n += __shfl_xor(n, 32);
+        if (lane < PROMPTS_LENGTHS) atomicAdd(&s_sum[lane], n);
+    }
     __syncthreads();
-    int len = longest;
-    int64_t least = INT64_MAX;
+    const float n = (float)max(s_sum[lane & (PROMPTS_LENGTHS - 1)], 1), turns = n * p.kv_heads / slots;
+    float least = (turns <= 1.f ? length + 8.f : ceilf(turns) * ((float)all / n + 8.f)) + (length < longest ? 6.f : 0.f);
+    int len = length;
 #pragma unroll
-    for (int j = 7; j >= 0; --j) {
-        const int64_t t = ((int64_t)s_sum[j] * p.kv_heads + PROMPTS_SLOTS - 1) / PROMPTS_SLOTS * (length(j) + 3) + (length(j) < longest ? 8 : 0);
-        if (t < least) least = t, len = length(j);
+    for (int k = 1; k < PROMPTS_LENGTHS; k <<= 1) {
+        const float t = __shfl_xor(least, k);
+        const int other = __shfl_xor(len, k);
+        if (t < least || (t == least && other > len)) least = t, len = other;   // (the same for all)
     }
     const int count = i < tiles ? (steps + len - 1) / len : 0;
     int total;
     const int at = before(count, &total);
     if (i == 0) p.count[0] = total, p.count[1] = tiles;
     if (i < tiles) p.splits[i] = {prompt, tile, at, count};
-    for (int j = 0; j < count; ++j) p.pieces[at + j] = {prompt, tile, (int)((int64_t)steps * j / count), (int)((int64_t)steps * (j + 1) / count), count > 1};
+    __syncthreads();
+    s_first[i] = i < tiles ? at : total;   // (a tile's first piece now, and of the others what follows)
+    s_tile[i] = {prompt, tile, steps, count};
+    __syncthreads();
+    for (int q = i; q < total; q += blockDim.x) {
+        int u = 0;
+#pragma unroll
+        for (int w = PROMPTS_PLAN / 2; w > 0; w /= 2)
+            if (u + w < tiles && s_first[u + w] <= q) u += w;
+        const int4 x = s_tile[u];
+        const int j = q - s_first[u];
+        const int even = (int)((unsigned)x.z / (unsigned)x.w), rest = x.z - even * x.w;   // (the first ones have a step more)
+        p.pieces[q] = {x.x, x.y, even * j + min(j, rest), even * (j + 1) + min(j + 1, rest), x.w > 1};
+    }
 }
 
 // The pieces of a tile and key head: four rows of a wave at a time where heads are of 64, a row's numbers by lanes side by side
@@ -689,14 +724,29 @@ k_prompts_join(PromptsP p, int rows) {
         if (row >= at.n * p.group || d >= p.dim) continue;
         float top = -INFINITY, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int j = 0; j < s.count; ++j) {
-            const int64_t from = ((int64_t)(s.first + j) * p.kv_heads + kvh) * rows + r;
-            const float2 ml = *(const float2 *)(p.part_ml + from * 2);
-            const float4 x = *(const float4 *)(p.part_o + from * p.dim + d);
-            const float m = fmaxf(top, ml.x), a = top == m ? 1.f : __builtin_amdgcn_exp2f(top - m), b = ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
+        for (int j0 = 0; j0 < s.count; j0 += 8) {   // eight pieces' sums on their way
+            float2 ml[8];
+            float4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t from = ((int64_t)(s.first + min(j0 + j, s.count - 1)) * p.kv_heads + kvh) * rows + r;
+                ml[j] = *(const float2 *)(p.part_ml + from * 2);
+                x[j] = *(const float4 *)(p.part_o + from * p.dim + d);
+            }
+            float m = top;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, ml[j].x);
+            const float a = top == m ? 1.f : __builtin_amdgcn_exp2f(top - m);
             top = m;
-            l = l * a + ml.y * b;
-            o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
+            l *= a;
+            o = make_float4(o.x * a, o.y * a, o.z * a, o.w * a);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j0 + j >= s.count) continue;
+                const float b = ml[j].x == m ? 1.f : __builtin_amdgcn_exp2f(ml[j].x - m);
+                l += ml[j].y * b;
+                o = make_float4(o.x + x[j].x * b, o.y + x[j].y * b, o.z + x[j].z * b, o.w + x[j].w * b);
+            }
         }
         const float f = l == 0.f ? 0.f : 1.f / l;
         const T y[4] = {(T)(l == 0.f ? 0.f : o.x * f), (T)(l == 0.f ? 0.f : o.y * f), (T)(l == 0.f ? 0.f : o.z * f), (T)(l == 0.f ? 0.f : o.w * f)};
@@ -716,11 +766,11 @@ static PromptsForm prompts_form(const tbs_attend_prompts_args &a, int force) {
     auto tiles = [&](int waves) { return (int64_t)a.tokens * group / (32 * waves) + a.prompts; };
     PromptsForm f = {4, false, 0, 0};
     const int64_t t = tiles(4), longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0;
-    f.shared = t <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : t * a.kv_heads < 2 * PROMPTS_SLOTS && longest >= 2048);
+    f.shared = t <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : t * a.kv_heads < 2 * prompts_slots(a) && longest >= 2048);
     if (!f.shared)
         while (f.waves > 2 && (tiles(f.waves) + 1) * a.kv_heads < 512) f.waves /= 2;
     f.tiles = tiles(f.waves);
-    f.units = f.tiles + 1 + (f.shared ? PROMPTS_SLOTS / a.kv_heads : 0);   // (a piece is an equal share of all steps or more)
+    f.units = f.tiles + 1 + (f.shared ? prompts_slots(a) * PROMPTS_PIECES / a.kv_heads + 1 : 0);   // (a piece is a quarter of an equal share of all steps, or more)
     return f;
 }
 
@@ -747,7 +797,8 @@ static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(64 * f.waves);
     if (f.shared) {
-        hipLaunchKernelGGL(k_prompts_plan, dim3(1), dim3(PROMPTS_PLAN), 0, st, p, 32 * f.waves, PromptsTile<T, DP>::KEYS, (int)f.tiles);
+        hipLaunchKernelGGL(k_prompts_plan, dim3(1), dim3((unsigned)(f.tiles + 63) / 64 * 64), 0, st,   // (tiles: no fewer than prompts)
+                           p, 32 * f.waves, PromptsTile<T, DP>::KEYS, (int)f.tiles, prompts_slots(a));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -757,7 +808,7 @@ static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args
     if (f.shared) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((k_prompts_join<T>), dim3((unsigned)(f.tiles * a.kv_heads), 4), dim3(256), 0, st, p, 32 * f.waves);
+        hipLaunchKernelGGL((k_prompts_join<T>), dim3((unsigned)(f.tiles * a.kv_heads), 16), dim3(256), 0, st, p, 32 * f.waves);
     }
     return hipGetLastError();
 }
