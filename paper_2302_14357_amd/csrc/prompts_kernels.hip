@@ -17,6 +17,7 @@
 #include "op_device.h"
 
 #define PROMPTS_SLACK 8.f
+#define PROMPTS_WAVES 4   // of 32 rows each: a workgroup (two, for more workgroups where tiles are few, took as long or twice as long: fewer loads are on their way)
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short prompts_b64;
 
 struct PromptsP {
@@ -145,16 +146,15 @@ __device__ __forceinline__ void prompts_interleave() {
     __builtin_amdgcn_sched_group_barrier(0x008, A < N ? A : N, 0);
 }
 
-// What a workgroup does.  DP: dim rounded up to 32, 64, 96, 128 or 256; NW: waves of 32 rows each; SHARED: by the list of pieces (its few scalars more cost 7 % in
+// What a workgroup does.  DP: dim rounded up to 32, 64, 80, 96, 128 or 256; SHARED: by the list of pieces (its few scalars more cost 7 % in
 // the loop).  A class whose functions are all inlined: everything in it is in registers.
 #define PROMPTS_INLINE __device__ __forceinline__
-template <class T, int DP, int NW, bool SHARED>
+template <class T, int DP, bool SHARED>
 struct PromptsWork {
     typedef PromptsTile<T, DP> Tile;
-    static constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, DB = DP / 32, KS = DP * (int)sizeof(T) / 32, ROWS = 32 * NW;
+    static constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, DB = (DP + 31) / 32, KS = DP * (int)sizeof(T) / 32, NW = PROMPTS_WAVES, ROWS = 32 * NW;
     static constexpr int CHUNKS = TK * PITCH / 64, MINE = (CHUNKS + NW - 1) / NW;   // loads of 64 pieces, and those of a wave
     static constexpr int RUN = MINE * 64 / PITCH;                                   // rows of a wave's
-    static constexpr bool ALL = DP == PITCH * E;                                    // (dim = DP: no piece is missing)
     static constexpr int VS = sizeof(T) == 4 ? 1 : DB;                              // addresses of V
     static constexpr int KB = TK / 32;
     // (float16: weights up to 2^7 more, so that small ones keep their digits: with the slack's 2^8 at most half its largest number)
@@ -200,7 +200,10 @@ struct PromptsWork {
     PROMPTS_INLINE void places(unsigned bytes) {
         const int lane = again();
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) (V ? v_off : k_off)[i] = (row_of(i, lane) - wave * RUN) * bytes + piece_of(i, lane, V) * 16 + (3 - i % 4) * 1024;
+        for (int i = 0; i < MINE; ++i) {
+            const int piece = piece_of(i, lane, V);   // (dim = DP: places behind the head's end are never looked at, and have its first piece)
+            (V ? v_off : k_off)[i] = (row_of(i, lane) - wave * RUN) * bytes + (piece < Tile::USED ? piece : 0) * 16 + (3 - i % 4) * 1024;
+        }
     }
     PROMPTS_INLINE int page_of(int t) const { return t < at.past ? table[prompts_page(p, t)] : 0; }
     PROMPTS_INLINE void look(int step) {   // (the values follow the keys a tile later, with the pages of the last look)
@@ -226,7 +229,7 @@ struct PromptsWork {
         auto off = [&](int i) __attribute__((always_inline)) { return V ? v_off[i] : k_off[i]; };
 #pragma unroll
         for (int i = 0; i < MINE; i += N) {
-            if (ALL && p.dim == DP) {
+            if (p.dim == DP) {
                 if (takes_part(i)) prompts_load_lds<N>(from, off(i), off(N > 1 ? i + 1 : i), off(N > 2 ? i + 2 : i), off(N > 3 ? i + 3 : i), to + i * 1024);
             } else {
 #pragma unroll
@@ -540,7 +543,7 @@ struct PromptsWork {
 #pragma unroll
         for (int i = 0; i < MINE; ++i) k_in[i] = piece_of(i, lane, false) * E < p.dim, v_in[i] = piece_of(i, lane, true) * E < p.dim;
         // pieces behind the head's end are 0 in both buffers, and stay so
-        if (p.dim < PITCH * E) {
+        if (p.dim < DP) {
             for (int i = threadIdx.x; i < 4 * TK * PITCH; i += 64 * NW) {
                 const int in = i % (TK * PITCH), r = in / PITCH, slot = in % PITCH;
                 if ((slot ^ ((i / (TK * PITCH)) & 1 ? Tile::v_swizzle(r) : Tile::k_swizzle(r))) * E >= p.dim) ((uint4 *)kv)[i] = make_uint4(0, 0, 0, 0);
@@ -578,7 +581,8 @@ struct PromptsWork {
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) none = fmaf(o[d][i], 0.f, none);
+            for (int i = 0; i < 16; ++i)
+                if (d * 32 + i / 4 * 8 < DP) none = fmaf(o[d][i], 0.f, none);   // (behind the head's end there may be anything)
         if (!__syncthreads_or(live && none != 0.f)) {
 #pragma unroll
             for (int d = 0; d < DB; ++d) store(o[d], d);
@@ -593,11 +597,11 @@ struct PromptsWork {
     }
 };
 
-template <class T, int DP, int NW, bool SHARED>
-__global__ void __launch_bounds__(64 * NW, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
+template <class T, int DP, bool SHARED>
+__global__ void __launch_bounds__(64 * PROMPTS_WAVES, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
 k_prompts(PromptsP p) {
     __shared__ __align__(16) char s_kv[4 * PromptsTile<T, DP>::BYTES];
-    PromptsWork<T, DP, NW, SHARED> work(p, s_kv);
+    PromptsWork<T, DP, SHARED> work(p, s_kv);
     work.run();
 }
 
@@ -754,23 +758,23 @@ k_prompts_join(PromptsP p, int rows) {
     }
 }
 
-// How a call is done: waves of a workgroup, and whether the keys of a tile are shared out
+// How a call is done: whether the keys of a tile are shared out, and how many there are at most: tiles; tiles, or pieces, and one more
 struct PromptsForm {
-    int waves;
     bool shared;
-    int64_t tiles, units;   // at most: tiles; tiles, or pieces, and one more
+    int64_t tiles, units;
 };
 
+// Shared out where there are few workgroups for their keys: the plan and the join take about 14 us.  The longest prompt is the largest that the tables can hold, or the mean
+// one.  (A tile a workgroup and shared, bfloat16: one of 1000 tokens, 8 heads of 64, 28 and 21 us; 8 of one token behind 1500, 16 heads on 4 of 128, 52 and 25; 32 of one
+// behind 1000, 32 heads on 8, 43 and 45; two of 1000, 16 heads on 4, 31 and 40.)
 static PromptsForm prompts_form(const tbs_attend_prompts_args &a, int force) {
     const int group = a.heads / a.kv_heads;
-    auto tiles = [&](int waves) { return (int64_t)a.tokens * group / (32 * waves) + a.prompts; };
-    PromptsForm f = {4, false, 0, 0};
-    const int64_t t = tiles(4), longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0;
-    f.shared = t <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : t * a.kv_heads < 2 * prompts_slots(a) && longest >= 2048);
-    if (!f.shared)
-        while (f.waves > 2 && (tiles(f.waves) + 1) * a.kv_heads < 512) f.waves /= 2;
-    f.tiles = tiles(f.waves);
-    f.units = f.tiles + 1 + (f.shared ? prompts_slots(a) * PROMPTS_PIECES / a.kv_heads + 1 : 0);   // (a piece is a quarter of an equal share of all steps, or more)
+    PromptsForm f = {};
+    f.tiles = (int64_t)a.tokens * group / (32 * PROMPTS_WAVES) + a.prompts;
+    const int64_t longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0, blocks = f.tiles * a.kv_heads, slots = prompts_slots(a);
+    const bool few = longest >= 2048 ? blocks < 2 * slots : longest >= 768 && blocks * 4096 < slots * longest;
+    f.shared = f.tiles <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : few);
+    f.units = f.tiles + 1 + (f.shared ? slots * PROMPTS_PIECES / a.kv_heads + 1 : 0);   // (a piece is a quarter of an equal share of all steps, or more)
     return f;
 }
 
@@ -781,7 +785,7 @@ struct PromptsSpace {
 static PromptsSpace prompts_space(const tbs_attend_prompts_args &a, const PromptsForm &f) {
     PromptsSpace s = {};
     if (!f.shared) return s;
-    const int64_t rows = f.units * a.kv_heads * 32 * f.waves;
+    const int64_t rows = f.units * a.kv_heads * 32 * PROMPTS_WAVES;
     auto after = [](int64_t at, int64_t n) { return (at + n + 15) / 16 * 16; };
     s.pieces = 16;
     s.splits = after(s.pieces, f.units * (int64_t)sizeof(PromptsPiece));
@@ -792,34 +796,34 @@ static PromptsSpace prompts_space(const tbs_attend_prompts_args &a, const Prompt
 }
 
 template <class T, int DP>
-static hipError_t prompts_waves(const PromptsP &p, const tbs_attend_prompts_args &a, const PromptsForm &f, hipStream_t st) {
+static hipError_t prompts_launch(const PromptsP &p, const tbs_attend_prompts_args &a, const PromptsForm &f, hipStream_t st) {
     const int64_t blocks = f.units * a.kv_heads;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(64 * f.waves);
+    const dim3 grid((unsigned)blocks), block(64 * PROMPTS_WAVES);
     if (f.shared) {
         hipLaunchKernelGGL(k_prompts_plan, dim3(1), dim3((unsigned)(f.tiles + 63) / 64 * 64), 0, st,   // (tiles: no fewer than prompts)
-                           p, 32 * f.waves, PromptsTile<T, DP>::KEYS, (int)f.tiles, prompts_slots(a));
+                           p, 32 * PROMPTS_WAVES, PromptsTile<T, DP>::KEYS, (int)f.tiles, prompts_slots(a));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (f.waves == 2) hipLaunchKernelGGL((k_prompts<T, DP, 2, false>), grid, block, 0, st, p);
-    else if (f.shared) hipLaunchKernelGGL((k_prompts<T, DP, 4, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_prompts<T, DP, 4, false>), grid, block, 0, st, p);
+    if (f.shared) hipLaunchKernelGGL((k_prompts<T, DP, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_prompts<T, DP, false>), grid, block, 0, st, p);
     if (f.shared) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((k_prompts_join<T>), dim3((unsigned)(f.tiles * a.kv_heads), 16), dim3(256), 0, st, p, 32 * f.waves);
+        hipLaunchKernelGGL((k_prompts_join<T>), dim3((unsigned)(f.tiles * a.kv_heads), 16), dim3(256), 0, st, p, 32 * PROMPTS_WAVES);
     }
     return hipGetLastError();
 }
 
 template <class T>
 static hipError_t prompts_dims(const PromptsP &p, const tbs_attend_prompts_args &a, const PromptsForm &f, hipStream_t st) {
-    if (p.dim <= 32) return prompts_waves<T, 32>(p, a, f, st);
-    if (p.dim <= 64) return prompts_waves<T, 64>(p, a, f, st);
-    if (p.dim <= 96) return prompts_waves<T, 96>(p, a, f, st);
-    if (p.dim <= 128) return prompts_waves<T, 128>(p, a, f, st);
-    return prompts_waves<T, 256>(p, a, f, st);
+    if (p.dim <= 32) return prompts_launch<T, 32>(p, a, f, st);
+    if (p.dim <= 64) return prompts_launch<T, 64>(p, a, f, st);
+    if (p.dim == 80) return prompts_launch<T, 80>(p, a, f, st);
+    if (p.dim <= 96) return prompts_launch<T, 96>(p, a, f, st);
+    if (p.dim <= 128) return prompts_launch<T, 128>(p, a, f, st);
+    return prompts_launch<T, 256>(p, a, f, st);
 }
 
 static int prompts_check(const tbs_attend_prompts_args &a) {
