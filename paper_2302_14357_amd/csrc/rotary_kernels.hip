@@ -47,92 +47,124 @@ __device__ __forceinline__ void rotary_load(T *x, const T *from, int n) {
     __builtin_memcpy(x, &u, 16);
 }
 
-// A workgroup takes `per` tokens: their angles once into LDS, then all their heads by pieces of 16 bytes, `lanes` threads to a head; of the values a
-// copy.  HALF: a pair is i and i + pairs, a thread takes both pieces; otherwise 2 i and 2 i + 1.
-template <class T, bool HALF>
+// A head's row is pieces of 16 bytes: those of its pairs, then those of what is behind them.  A lane has two of every row that it takes.
+struct RotaryPieces {
+    int c[2], n[2], turned;   // first element, elements (none: 0 or fewer); bits of those that turn
+};
+
+template <int E, bool HALF>
+__device__ __forceinline__ RotaryPieces rotary_pieces(const RotaryP &p, int lane) {
+    const int front = 2 * p.pairs, turned = ((HALF ? p.pairs : front) + E - 1) / E, rest = (p.dim - front + E - 1) / E;
+    RotaryPieces x;
+    if (HALF && lane < turned) {   // both members of its pairs
+        x.c[0] = lane * E, x.c[1] = p.pairs + lane * E;
+        x.n[0] = x.n[1] = p.pairs - lane * E;
+        x.turned = 3;
+        return x;
+    }
+    const int count = HALF ? rest : turned + rest, half = (count + 1) / 2, mine = HALF ? lane - turned : lane;
+    x.turned = 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int i = mine + j * half;
+        const bool turns = !HALF && i < turned;
+        x.c[j] = turns || HALF ? i * E + (HALF ? front : 0) : front + (i - turned) * E;
+        x.n[j] = mine < half && i < count ? (turns ? front : p.dim) - x.c[j] : 0;
+        x.turned |= (int)turns << j;
+    }
+    return x;
+}
+
+// A workgroup takes `per` tokens: their angles once into LDS, then all their heads, `lanes` threads to a head, the next head's pieces on their way while
+// one is turned; of the values a copy.  HALF: a pair is i and i + pairs; otherwise 2 i and 2 i + 1.  WHOLE: all of a head turns, and every
+// lane has two whole pieces.
+// Bound by memory: 8000 tokens, heads of 32 + 8 + 8 x 128, bfloat16, with the cache 34 us, 6.2 TB/s of what the caches hold in part (36 without the next
+// head's loads ahead, 37 without WHOLE); 500 tokens of them 5.4 us.  A half of 256 turned, 16 + 4 + 4 heads, 4000 tokens, float16: 23 us (one piece a lane 31).
+template <class T, bool HALF, bool WHOLE>
 __global__ void __launch_bounds__(ROTARY_THREADS)
 k_rotary(RotaryP p) {
     constexpr int E = OpPiece<T>::E;
     __shared__ float2 s_angle[ROTARY_ANGLES];
     const int t0 = (int)blockIdx.x * p.per, mine = min(p.per, p.tokens - t0);
+    const int rows = p.heads + p.kv_heads + (p.slots ? p.kv_heads : 0), all = mine * rows, step = ROTARY_THREADS / p.lanes;
+    const int lane = threadIdx.x & (p.lanes - 1);
+    RotaryPieces at = rotary_pieces<E, HALF>(p, lane);
+    if (WHOLE) at.c[0] = lane * E, at.c[1] = p.pairs + at.c[0];
+    struct Row {
+        T x[2][E];
+        int64_t slot;
+    };
+    auto load = [&](Row &row, int r) {
+        const int u = r / rows, h = r - u * rows, t = t0 + u;
+        const bool is_q = h < p.heads, is_v = h >= p.heads + p.kv_heads;
+        row.slot = p.slots && !is_q ? p.slots[t] : -1;
+        const T *from = (const T *)(is_q ? p.q + t * p.q_row + h * p.q_head : is_v ? p.v + t * p.v_row + (h - p.heads - p.kv_heads) * p.v_head : p.k + t * p.k_row + (h - p.heads) * p.k_head);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (WHOLE || at.n[j] > 0) rotary_load(row.x[j], from + at.c[j], WHOLE ? E : at.n[j]);
+    };
+    int r = threadIdx.x / p.lanes;
+    Row row, next;
+    if (r < all) load(row, r);
     for (int i = threadIdx.x; i < mine * p.pairs; i += ROTARY_THREADS) {
         const int t = i / p.pairs;
         s_angle[i] = rotary_angle((double)p.positions[t0 + t], p.freqs[i - t * p.pairs]);
     }
     __syncthreads();
-    const int turned = HALF ? (p.pairs + E - 1) / E : (2 * p.pairs + E - 1) / E, rest = p.dim - 2 * p.pairs;
-    const int rows = p.heads + p.kv_heads + (p.slots ? p.kv_heads : 0), step = ROTARY_THREADS / p.lanes, lane = threadIdx.x & (p.lanes - 1);
-    for (int r = threadIdx.x / p.lanes; r < mine * rows; r += step) {
+    for (; r < all; r += step) {
+        if (r + step < all) load(next, r + step);
         const int u = r / rows, h = r - u * rows, t = t0 + u;
         const bool is_q = h < p.heads, is_v = h >= p.heads + p.kv_heads;
         const int kvh = is_v ? h - p.heads - p.kv_heads : h - p.heads;
-        char *cache = nullptr;   // where a key or value goes as well
-        if (p.slots && !is_q) {
-            const int64_t slot = p.slots[t];
-            if (slot >= 0 && slot < p.places) {
-                const int64_t page = slot <= UINT32_MAX ? (unsigned)slot / (unsigned)p.page : slot / p.page, off = slot - page * p.page;
-                cache = is_v ? p.v_cache + page * p.vp + off * p.vt + kvh * p.vh : p.k_cache + page * p.kp + off * p.kt + kvh * p.kh;
-            }
-        }
-        T x[E], y[E];
-        if (is_v) {
-            if (!cache) continue;
-            const T *from = (const T *)(p.v + t * p.v_row + kvh * p.v_head);
-            for (int c = lane * E; c < p.dim; c += p.lanes * E) {
-                rotary_load(x, from + c, p.dim - c);
-                rotary_store((T *)cache + c, x, p.dim - c);
-            }
-            continue;
-        }
-        const T *from = (const T *)(is_q ? p.q + t * p.q_row + h * p.q_head : p.k + t * p.k_row + kvh * p.k_head);
-        T *to = (T *)(is_q ? p.q_out + t * p.qo_row + h * p.qo_head : p.k_out + t * p.ko_row + kvh * p.ko_head);
-        if (lane < turned) {
-            const int c = lane * E;
-            const float2 *angle = s_angle + u * p.pairs;
+        const float2 *angle = s_angle + u * p.pairs;
+        if ((WHOLE || at.turned) && !is_v) {
             if constexpr (HALF) {
-                const int n = p.pairs - c;
-                rotary_load(x, from + c, n);
-                rotary_load(y, from + p.pairs + c, n);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const float2 w = angle[min(c + i, p.pairs - 1)];
-                    const float a = op_float(x[i]), b = op_float(y[i]);
-                    x[i] = (T)(a * w.x - b * w.y);
-                    y[i] = (T)(b * w.x + a * w.y);
-                }
-                rotary_store(to + c, x, n);
-                rotary_store(to + p.pairs + c, y, n);
-                if (cache) {
-                    rotary_store((T *)cache + c, x, n);
-                    rotary_store((T *)cache + p.pairs + c, y, n);
+                    const float2 w = angle[WHOLE ? at.c[0] + i : min(at.c[0] + i, p.pairs - 1)];
+                    const float a = op_float(row.x[0][i]), b = op_float(row.x[1][i]);
+                    row.x[0][i] = (T)(a * w.x - b * w.y);
+                    row.x[1][i] = (T)(b * w.x + a * w.y);
                 }
             } else {
-                const int n = 2 * p.pairs - c;
-                rotary_load(x, from + c, n);
 #pragma unroll
-                for (int i = 0; i < E; i += 2) {
-                    const float2 w = angle[min((c + i) / 2, p.pairs - 1)];
-                    const float a = op_float(x[i]), b = op_float(x[i + 1]);
-                    x[i] = (T)(a * w.x - b * w.y);
-                    x[i + 1] = (T)(b * w.x + a * w.y);
-                }
-                rotary_store(to + c, x, n);
-                if (cache) rotary_store((T *)cache + c, x, n);
+                for (int j = 0; j < 2; ++j)
+                    if (WHOLE || at.turned >> j & 1)
+#pragma unroll
+                        for (int i = 0; i < E; i += 2) {
+                            const float2 w = angle[WHOLE ? (at.c[j] + i) / 2 : min((at.c[j] + i) / 2, p.pairs - 1)];
+                            const float a = op_float(row.x[j][i]), b = op_float(row.x[j][i + 1]);
+                            row.x[j][i] = (T)(a * w.x - b * w.y);
+                            row.x[j][i + 1] = (T)(b * w.x + a * w.y);
+                        }
             }
-        } else if ((lane - turned) * E < rest) {   // what is behind the pairs stays as it is
-            const int c = 2 * p.pairs + (lane - turned) * E;
-            rotary_load(x, from + c, p.dim - c);
-            rotary_store(to + c, x, p.dim - c);
-            if (cache) rotary_store((T *)cache + c, x, p.dim - c);
         }
+        if (!is_v) {
+            T *to = (T *)(is_q ? p.q_out + t * p.qo_row + h * p.qo_head : p.k_out + t * p.ko_row + kvh * p.ko_head);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) rotary_store(to + at.c[j], row.x[j], WHOLE ? E : at.n[j]);
+        }
+        if (row.slot >= 0 && row.slot < p.places) {   // where a key or value goes as well
+            const int64_t page = row.slot <= UINT32_MAX ? (unsigned)row.slot / (unsigned)p.page : row.slot / p.page, off = row.slot - page * p.page;
+            T *to = (T *)(is_v ? p.v_cache + page * p.vp + off * p.vt + kvh * p.vh : p.k_cache + page * p.kp + off * p.kt + kvh * p.kh);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) rotary_store(to + at.c[j], row.x[j], WHOLE ? E : at.n[j]);
+        }
+        row = next;
     }
 }
 
 template <class T>
 static void rotary_run(const RotaryP &p, bool half, hipStream_t st) {
     const dim3 grid((unsigned)(((int64_t)p.tokens + p.per - 1) / p.per)), block(ROTARY_THREADS);
-    if (half) hipLaunchKernelGGL((k_rotary<T, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_rotary<T, false>), grid, block, 0, st, p);
+    const bool whole = p.dim == 2 * p.pairs && p.lanes * OpPiece<T>::E == p.pairs;
+    if (whole) {
+        if (half) hipLaunchKernelGGL((k_rotary<T, true, true>), grid, block, 0, st, p);
+        else hipLaunchKernelGGL((k_rotary<T, false, true>), grid, block, 0, st, p);
+    } else {
+        if (half) hipLaunchKernelGGL((k_rotary<T, true, false>), grid, block, 0, st, p);
+        else hipLaunchKernelGGL((k_rotary<T, false, false>), grid, block, 0, st, p);
+    }
 }
 
 extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
@@ -175,9 +207,10 @@ extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
     p.kp = a.k_cache_page * es, p.kt = a.k_cache_token * es, p.kh = a.k_cache_head * es, p.vp = a.v_cache_page * es, p.vt = a.v_cache_token * es, p.vh = a.v_cache_head * es;
     p.places = cached ? (int64_t)a.pages * a.page : 0;
     p.tokens = a.tokens, p.heads = a.heads, p.kv_heads = a.kv_heads, p.dim = a.dim, p.pairs = a.pairs, p.page = cached ? a.page : 1;
-    const int e = (int)(16 / es), pieces = (a.interleaved ? (2 * a.pairs + e - 1) / e : (a.pairs + e - 1) / e) + (a.dim - 2 * a.pairs + e - 1) / e;
+    const int e = (int)(16 / es), turned = ((a.interleaved ? 2 * a.pairs : a.pairs) + e - 1) / e, behind = (a.dim - 2 * a.pairs + e - 1) / e;
+    const int pieces = a.interleaved ? (turned + behind + 1) / 2 : turned + (behind + 1) / 2;   // lanes that a head needs
     p.lanes = 1;
-    while (p.lanes < pieces) p.lanes *= 2;   // (at most 129 pieces)
+    while (p.lanes < pieces) p.lanes *= 2;   // (at most 65)
     const int rows = a.heads + a.kv_heads * (cached ? 2 : 1);
     int64_t per = ((int64_t)ROTARY_THREADS / p.lanes * 4 + rows - 1) / rows;   // four heads a thread
     if (a.pairs > 0 && per > ROTARY_ANGLES / a.pairs) per = ROTARY_ANGLES / a.pairs;
