@@ -1,11 +1,12 @@
 """The N-best lists of a transducer, rescored and continued by a transformer language model under the same beams.
 
-    python examples/continue_nbest.py [--utts 8] [--beam 5] [--steps 20]
+    python examples/continue_nbest.py [--utts 8] [--beam 5] [--steps 20] [--together]
 
 `tbs_decode` gives every utterance up to N token sequences.  A decoder-only transformer (random weights, as everything here is
 synthetic) reads them token by token, all hypotheses of all utterances together, and then goes on under beam search.  One step of the model
 is `linear` (products with bias, activation and residual) and `attend_paged` (one new token per hypothesis over its paged cache); one of
-the search is `beam_select` and `beam_reorder`.  Token 0, the transducer's blank, ends a sequence.
+the search is `beam_select` and `beam_reorder`.  With --together the model reads all tokens of the lists in one pass instead: `page_slots` says where they
+stand and go, `rotary` brings their keys and values into the cache and `attend_prompts` is their attention.  Token 0, the transducer's blank, ends a sequence.
 """
 
 from __future__ import annotations
@@ -19,15 +20,16 @@ import torch.nn.functional as F
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2302_14357_amd import attend_paged, beam_reorder, beam_select, linear  # noqa: E402
+from paper_2302_14357_amd import attend_paged, attend_prompts, beam_reorder, beam_select, linear, page_slots, rotary  # noqa: E402
 
 END = 0
 
 
 class Lm:
-    """Weights of a decoder-only transformer: `layers` blocks of attention (kv_heads key heads) and a feed-forward block, norms before each."""
+    """Weights of a decoder-only transformer: `layers` blocks of attention (kv_heads key heads) and a feed-forward block, norms before each.  `turned`: queries and
+    keys are turned by their positions, instead of a vector that is added for each."""
 
-    def __init__(self, vocab, width=256, layers=2, heads=8, kv_heads=2, dtype=torch.bfloat16, seed=0, device="cuda"):
+    def __init__(self, vocab, width=256, layers=2, heads=8, kv_heads=2, dtype=torch.bfloat16, seed=0, device="cuda", turned=False):
         g = torch.Generator().manual_seed(seed)
         self.heads, self.kv, self.dim, self.dtype, self.width, self.vocab = heads, kv_heads, width // heads, dtype, width, vocab
 
@@ -42,6 +44,24 @@ class Lm:
                             out_bias=bias(width), up=matrix(4 * width, width), up_bias=bias(4 * width), down=matrix(width, 4 * width), down_bias=bias(width))
                        for _ in range(layers)]
         self.head = matrix(vocab, width, 3.0)
+        pairs = self.dim // 2 if turned else 0
+        self.freqs = (10000.0 ** -(torch.arange(pairs, dtype=torch.float64) / max(pairs, 1))).to(device)
+        self.turned = turned
+
+    def enter(self, tokens, at):
+        x = self.embed[tokens.long().clamp(min=0)]
+        return x if self.turned else x + self.place[at]
+
+    def heads_of(self, b, x):
+        return linear(F.layer_norm(x, (self.width,)), b["qkv"], b["qkv_bias"]).view(len(x), -1, self.dim).split((self.heads, self.kv, self.kv), 1)
+
+    def leave(self, b, x, o):
+        x = linear(o.view(len(x), -1), b["out"], b["out_bias"], residual=x)
+        h = linear(F.layer_norm(x, (self.width,)), b["up"], b["up_bias"], act="gelu")
+        return linear(h, b["down"], b["down_bias"], residual=x)
+
+    def logits(self, x):
+        return linear(F.layer_norm(x, (self.width,)), self.head, out_dtype=torch.float32)
 
 
 class Beams:
@@ -58,24 +78,36 @@ class Beams:
 
     def logits(self, tokens):
         """One token per hypothesis -> float32 logits of the next; hypotheses of negative length take no part."""
-        lm, rows = self.lm, len(tokens)
+        lm = self.lm
         self.longest += 1
-        at = self.lens.clamp(min=0).long()
-        x = lm.embed[tokens.long().clamp(min=0)] + lm.place[at]
+        at = self.lens.clamp(min=0)
+        x = lm.enter(tokens, at.long())
         for i, b in enumerate(lm.blocks):
-            qkv = linear(F.layer_norm(x, (lm.width,)), b["qkv"], b["qkv_bias"]).view(rows, -1, lm.dim)
-            q, k, v = qkv.split((lm.heads, lm.kv, lm.kv), 1)
+            q, k, v = lm.heads_of(b, x)
+            if lm.turned:
+                q, k = rotary(q, k, at, lm.freqs)
             o = attend_paged(q, self.caches[2 * i], self.caches[2 * i + 1], self.tables, self.lens, k_new=k, v_new=v, beams=self.beams, max_len=self.longest)
-            x = linear(o.view(rows, -1), b["out"], b["out_bias"], residual=x)
-            h = linear(F.layer_norm(x, (lm.width,)), b["up"], b["up_bias"], act="gelu")
-            x = linear(h, b["down"], b["down_bias"], residual=x)
-        return linear(F.layer_norm(x, (lm.width,)), lm.head, out_dtype=torch.float32)
+            x = lm.leave(b, x, o)
+        return lm.logits(x)
+
+    def read(self, tokens, count, longest):
+        """All tokens of all hypotheses, one after the other, `count` int32 of each, up to `longest` -> float32 logits behind every token."""
+        lm = self.lm
+        self.longest = longest
+        starts, at, slots = page_slots(count, self.tables, page=self.page, tokens=len(tokens))
+        x = lm.enter(tokens, at.long())
+        for i, b in enumerate(lm.blocks):
+            q, k, v = lm.heads_of(b, x)
+            q, k = rotary(q, k, at, lm.freqs, v=v, k_cache=self.caches[2 * i], v_cache=self.caches[2 * i + 1], slots=slots)
+            x = lm.leave(b, x, attend_prompts(q, k, v, starts))
+        return lm.logits(x)
 
 
 @torch.no_grad()
-def continue_nbest(lm, nbest, beams, steps, page=16):
+def continue_nbest(lm, nbest, beams, steps, page=16, together=False):
     """nbest: per utterance up to `beams` (tokens, log score).  Returns the same after `steps` tokens more (fewer for those that end), best first, and how
-    many hypotheses were dropped on the way (beam_reorder's status; they do not come back).  A score is the list's plus the model's logarithms of all tokens, the first one's behind END."""
+    many hypotheses were dropped on the way (beam_reorder's status; they do not come back).  A score is the list's plus the model's logarithms of all tokens, the first one's behind END.
+    `together`: the lists' tokens are read in one pass."""
     device = lm.embed.device
     rows = len(nbest) * beams
     said = [[END] + list(nb[i][0]) if i < len(nb) else [] for nb in nbest for i in range(beams)]
@@ -87,7 +119,16 @@ def continue_nbest(lm, nbest, beams, steps, page=16):
     given, count = given.to(device), torch.tensor([len(s) for s in said], device=device)
     state = Beams(lm, rows, beams, length + steps, page)
     last = torch.empty(rows, lm.vocab, dtype=torch.float32, device=device)
-    for t in range(length):
+    if together:
+        flat = torch.tensor([t for s in said for t in s], device=device)
+        logits = state.read(flat, count.int(), length)
+        last = logits[(count.cumsum(0) - 1).clamp(min=0)]
+        # what the model says of every hypothesis' next tokens, a row of its own for each
+        here = torch.arange(length, device=device) < count[:, None]
+        said_next = torch.zeros(rows, length, dtype=torch.float64, device=device)
+        said_next[here] = torch.log_softmax(logits.double(), 1).gather(1, flat.roll(-1)[:, None])[:, 0]
+        scores = scores + said_next.masked_fill(torch.arange(length, device=device) >= count[:, None] - 1, 0.0).sum(1)
+    for t in range(0 if together else length):
         here = t < count
         state.lens = torch.where(here, t, ~(count.clamp(max=t))).int()
         logits = state.logits(given[:, t])
@@ -130,6 +171,7 @@ def main():
     a.add_argument("--utts", type=int, default=8)
     a.add_argument("--beam", type=int, default=5)
     a.add_argument("--steps", type=int, default=20)
+    a.add_argument("--together", action="store_true")
     a = a.parse_args()
     import dataclasses
     from paper_2302_14357_amd import Tbs
@@ -141,7 +183,7 @@ def main():
               max_rounds_per_segment=6)
     nbest = tbs.decode(tbs.upload_frames(enc), offsets)
     tbs.close()
-    got, dropped = continue_nbest(Lm(shape.vocab), nbest, a.beam, a.steps)
+    got, dropped = continue_nbest(Lm(shape.vocab), nbest, a.beam, a.steps, together=a.together)
     for u, (before, after) in enumerate(zip(nbest, got)):
         print(f"utterance {u}: {len(before)} hypotheses of {min(len(t) for t, _ in before)} to {max(len(t) for t, _ in before)} tokens; now best: "
               f"{list(after[0][0])} ({after[0][1]:.3f})")
