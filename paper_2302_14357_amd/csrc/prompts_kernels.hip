@@ -96,8 +96,10 @@ template <class T, int DP>
 struct PromptsTile {
     static constexpr int E = OpPiece<T>::E, KEYS = sizeof(T) == 4 || DP > 128 ? 32 : 64;
     static constexpr int USED = DP / E;                                       // pieces of a row
-    static constexpr int PITCH = USED <= 4 ? 4 : USED <= 8 ? 8 : USED <= 16 ? 16 : USED <= 32 ? 32 : 64;   // ... in LDS
+    static constexpr int PITCH = USED <= 4 ? 4 : USED <= 8 ? 8 : sizeof(T) == 2 && USED <= 12 ? 12 : USED <= 16 ? 16 : USED <= 32 ? 32 : 64;   // ... in LDS
     static constexpr int BYTES = KEYS * PITCH * 16;                           // of keys, or values
+    static constexpr int SPAN = PITCH >= 16 ? 16 : PITCH == 8 ? 8 : 4;        // pieces that a swizzle changes among each other
+    // (12: 64 bytes a row fewer to load and to keep than with 16; rows of 192 bytes, four of which begin at different quarters of all banks)
     // Keys: 32 rows' pieces of one place.  Values: four rows' two or four pieces side by side (float32: a row's eight, and those of the row four behind).
     static __device__ __forceinline__ int k_swizzle(int row) { return PITCH >= 16 ? row & 15 : PITCH == 8 ? row >> 1 & 7 : row >> 2 & 3; }
     static __device__ __forceinline__ int v_swizzle(int row) {
@@ -127,6 +129,10 @@ __device__ __forceinline__ void prompts_load_lds(const char *base, unsigned off0
     else if constexpr (N == 2)
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\ts_mov_b32 m0, %0"
                      : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1) : "memory");
+    else if constexpr (N == 3)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %5, %2 offset:2048\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1), "v"(off2) : "memory");
     else
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\t"
                      "global_load_lds_dwordx4 %5, %2 offset:2048\n\tglobal_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b32 m0, %0"
@@ -155,7 +161,8 @@ struct PromptsWork {
     static constexpr int E = Tile::E, TK = Tile::KEYS, PITCH = Tile::PITCH, DB = (DP + 31) / 32, KS = DP * (int)sizeof(T) / 32, NW = PROMPTS_WAVES, ROWS = 32 * NW;
     static constexpr int CHUNKS = TK * PITCH / 64, MINE = (CHUNKS + NW - 1) / NW;   // loads of 64 pieces, and those of a wave
     static constexpr int RUN = MINE * 64 / PITCH;                                   // rows of a wave's
-    static constexpr int VS = sizeof(T) == 4 ? 1 : DB;                              // addresses of V
+    // addresses of fragments: the swizzles change 4, 8 or 16 pieces among each other, and what is so many further has the same address and a constant
+    static constexpr int KA = Tile::SPAN / 2 < KS ? Tile::SPAN / 2 : KS, VA = sizeof(T) == 4 ? 1 : Tile::SPAN / 4 < DB ? Tile::SPAN / 4 : DB;
     static constexpr int KB = TK / 32;
     // (float16: weights up to 2^7 more, so that small ones keep their digits: with the slack's 2^8 at most half its largest number)
     static constexpr float MORE = __is_same(T, _Float16) ? 7.f : 0.f;
@@ -176,7 +183,7 @@ struct PromptsWork {
     unsigned k_off[MINE], v_off[MINE];   // bytes of a lane's pieces from 3072 before the wave's first key, less 1024 times their number among four: in a page, and then among new tokens
     bool k_in[MINE], v_in[MINE];         // (pieces behind the head's end are not there)
     int id[MINE], v_id[MINE];            // the pages of the keys and of the values that are asked for next, looked up a tile ahead: of this lane's (a wave's may be one)
-    const char *k_at[KS], *v_at[VS];   // where this lane's fragments begin
+    const char *k_at[KA], *v_at[VA];   // where this lane's fragments begin
     floatx16 o[DB];
     float m, l;
     uint4 w[sizeof(T) == 4 ? 1 : TK / 16];   // a tile's weights (float32: in place of the scores)
@@ -290,7 +297,7 @@ struct PromptsWork {
 
     // ---- fragments
     PROMPTS_INLINE uint4 k_frag(int step, int b, int j) const {   // 32 keys, two pieces
-        return *(const uint4 *)(k_at[j] + (step & 1) * 2 * Tile::BYTES + b * 32 * PITCH * 16);
+        return *(const uint4 *)(k_at[j % KA] + j / KA * Tile::SPAN * 16 + (step & 1) * 2 * Tile::BYTES + b * 32 * PITCH * 16);
     }
     PROMPTS_INLINE int v_row() const { return sizeof(T) == 4 ? 4 * h : 4 * h + (lane >> 2 & 3); }
     PROMPTS_INLINE const char *v_place(int d) const {
@@ -392,7 +399,7 @@ struct PromptsWork {
 #pragma unroll
             for (int i = 0; i < TK / 16; ++i)
 #pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(v_at[d], step, i * 16), w[i], o[d]);
+                for (int d = 0; d < DB; ++d) o[d] = op_mma32<T>(v_frag(v_at[d % VA] + d / VA * Tile::SPAN * 16, step, i * 16), w[i], o[d]);
             prompts_interleave<TK / 16 * DB, 2, 4>();
         }
         __builtin_amdgcn_s_setprio(0);
@@ -550,9 +557,9 @@ struct PromptsWork {
             }
         }
 #pragma unroll
-        for (int s = 0; s < KS; ++s) k_at[s] = kv + (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
+        for (int s = 0; s < KA; ++s) k_at[s] = kv + (c * PITCH + ((s * 2 + h) ^ Tile::k_swizzle(c))) * 16;
 #pragma unroll
-        for (int d = 0; d < VS; ++d) v_at[d] = v_place(d);
+        for (int d = 0; d < VA; ++d) v_at[d] = v_place(d);
 
         auto store = [&](const floatx16 &x, int d) __attribute__((always_inline)) {
             const float sum = l + __shfl_xor(l, 32), f = sum == 0.f ? 0.f : 1.f / sum;   // (no weight at all: 0)
@@ -598,7 +605,7 @@ struct PromptsWork {
 };
 
 template <class T, int DP, bool SHARED>
-__global__ void __launch_bounds__(64 * PROMPTS_WAVES, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
+__global__ void __launch_bounds__(64 * PROMPTS_WAVES, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 80 ? 3 : 2)   // (three at 80: 5 to 9 registers spill, and 16000 tokens take 771 us in place of 863)
 k_prompts(PromptsP p) {
     __shared__ __align__(16) char s_kv[4 * PromptsTile<T, DP>::BYTES];
     PromptsWork<T, DP, SHARED> work(p, s_kv);
@@ -611,7 +618,7 @@ k_prompts(PromptsP p) {
 __device__ const int prompts_parts[PROMPTS_LENGTHS] = {16, 18, 20, 22, 25, 28, 32, 36, 40, 44, 50, 56, 64, 96, 128, 0};   // 64ths of a share; 0: whole tiles
 
 // workgroups of four waves that the chip runs at a time: one to three a CU, by their registers
-static int prompts_slots(const tbs_attend_prompts_args &a) { return 256 * (a.dtype == TBS_F32 ? (a.dim <= 64 ? 2 : 1) : a.dim <= 64 ? 3 : a.dim <= 128 ? 2 : 1); }
+static int prompts_slots(const tbs_attend_prompts_args &a) { return 256 * (a.dtype == TBS_F32 ? (a.dim <= 64 ? 2 : 1) : a.dim <= 64 || a.dim == 80 ? 3 : a.dim <= 128 ? 2 : 1); }
 
 // Whose keys are shared, one workgroup: a thread a tile, or prompt.  A piece is at most `len` steps long: of sixteen lengths, from a quarter of an equal share of all work up, the one that
 // is estimated to take the fewest steps one after the other.  That is the turns that the slots take, whole ones, of a mean piece and eight steps for its start, its end and the way
@@ -764,15 +771,17 @@ struct PromptsForm {
     int64_t tiles, units;
 };
 
-// Shared out where there are few workgroups for their keys: the plan and the join take about 14 us.  The longest prompt is the largest that the tables can hold, or the mean
-// one.  (A tile a workgroup and shared, bfloat16: one of 1000 tokens, 8 heads of 64, 28 and 21 us; 8 of one token behind 1500, 16 heads on 4 of 128, 52 and 25; 32 of one
-// behind 1000, 32 heads on 8, 43 and 45; two of 1000, 16 heads on 4, 31 and 40.)
+// Shared out where there are few workgroups for their keys: the plan and the join take about 14 us, a piece's sums go through memory, and a turn that is not full is waited for.  The
+// longest prompt is the largest that the tables can hold, or the mean one.  (A tile a workgroup and shared, bfloat16, at blocks by slots.  32 heads on 8 of 128, four
+// prompts behind 8000 each: 0.3 235 and 113 us, 0.6 239 and 199, 0.8 275 and 291, 1.1 305 and 341; behind 500 to 8000: 0.6 244 and 140, 0.8 243 and 189, 1.1 265 and 232, 1.3 257 and 278.  One of
+// 4000, nothing before it: 0.5 101 and 89, 0.7 103 and 105, 1.0 106 and 126.  One of 1000, 8 heads of 64: 28 and 21; two of 1000, 16 heads on 4, 31 and 40; 8 of one token behind
+// 1500: 52 and 25.)
 static PromptsForm prompts_form(const tbs_attend_prompts_args &a, int force) {
     const int group = a.heads / a.kv_heads;
     PromptsForm f = {};
     f.tiles = (int64_t)a.tokens * group / (32 * PROMPTS_WAVES) + a.prompts;
     const int64_t longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0, blocks = f.tiles * a.kv_heads, slots = prompts_slots(a);
-    const bool few = longest >= 2048 ? blocks < 2 * slots : longest >= 768 && blocks * 4096 < slots * longest;
+    const bool few = longest >= 768 && blocks * 4096 < slots * std::min<int64_t>(longest, a.past ? 4096 : 2867);
     f.shared = f.tiles <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : few);
     f.units = f.tiles + 1 + (f.shared ? slots * PROMPTS_PIECES / a.kv_heads + 1 : 0);   // (a piece is a quarter of an equal share of all steps, or more)
     return f;
