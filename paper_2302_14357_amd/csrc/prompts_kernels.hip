@@ -14,6 +14,12 @@
 //
 // Weights are rounded to the 16 bits of the values' type: a weight's relative error is half a step of it, as large as the output's own rounding; two
 // numbers a weight would cost half as many matrix instructions again.  Sums, statistics and the weights' sum are float32.
+//
+// Bound by the matrix and the vector units together.  Prompts of 16000 and 7001 tokens, 32 heads on 8 of 128, bfloat16: 2.4 ms, 1.03 PFLOP/s (a large product of the library 1.45),
+// the matrix pipes 50 % busy, the vector units (32 exponentials, roundings and sums a lane of 64 keys) 44 %; two waves a SIMD overlap the two only in part.  16000 tokens, 32 heads
+// on 8 of 64: 1.2 ms, 0.87 PFLOP/s, half as many products for the same exponentials.  4000 in float32, 16 heads on 4 of 128: 600 us, 110 TFLOP/s of 153, the pipes' own order of work.
+// Four waves and 32 queries each: eight in two groups half a tile apart gained 2 %, eight behind one barrier 3 % of long prompts and lost 10 % of a batch's short ones; 64 queries
+// a wave spill; 32 keys a tile 7 % slower at 128; three tiles on their way 12 %; halves of a tile worked on in turn inside a wave 15 %.
 #include "op_device.h"
 
 #define PROMPTS_SLACK 8.f
@@ -135,7 +141,7 @@ __device__ __forceinline__ void prompts_load_lds(const char *base, unsigned off0
                      : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1), "v"(off2) : "memory");
     else
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\tglobal_load_lds_dwordx4 %4, %2 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %5, %2 offset:2048\n\tglobal_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b32 m0, %0"
+                     "global_load_lds_dwordx4 %5, %2 offset:2048\n\tglobal_load_lds_dwordx4 %6, %2 offset:3*1024\n\ts_mov_b32 m0, %0"
                      : "=&s"(m0_was) : "s"(to), "s"(base), "v"(off0), "v"(off1), "v"(off2), "v"(off3) : "memory");
 }
 
@@ -180,7 +186,7 @@ struct PromptsWork {
     uint4 q[KS];
     const char *k_new, *v_new, *k_old, *v_old;
     unsigned lds;
-    unsigned k_off[MINE], v_off[MINE];   // bytes of a lane's pieces from 3072 before the wave's first key, less 1024 times their number among four: in a page, and then among new tokens
+    unsigned k_off[MINE], v_off[MINE];   // bytes of a lane's pieces from 3 KiB before the wave's first key, less 1024 times their number among four: in a page, and then among new tokens
     bool k_in[MINE], v_in[MINE];         // (pieces behind the head's end are not there)
     int id[MINE], v_id[MINE];            // the pages of the keys and of the values that are asked for next, looked up a tile ahead: of this lane's (a wave's may be one)
     const char *k_at[KA], *v_at[VA];   // where this lane's fragments begin
@@ -231,7 +237,7 @@ struct PromptsWork {
     }
     template <bool V>
     PROMPTS_INLINE void load(const char *from, unsigned to) {
-        from -= 3072;   // (offsets are unsigned)
+        from -= 3 * 1024;   // (offsets are unsigned)
         constexpr int N = MINE < 4 ? MINE : 4;
         auto off = [&](int i) __attribute__((always_inline)) { return V ? v_off[i] : k_off[i]; };
 #pragma unroll

@@ -389,7 +389,8 @@ def _prompts_case(lens, *, heads, kv, dim, dtype, past=None, page=16, pad=0, lay
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("heads,kv,dim", [(1, 1, 64), (8, 2, 32), (8, 8, 64), (4, 1, 128), (6, 2, 80), (3, 1, 96), (5, 5, 24), (4, 4, 8), (4, 2, 256), (2, 1, 136), (24, 1, 40), (16, 2, 128)])
+@pytest.mark.parametrize("heads,kv,dim", [(1, 1, 64), (8, 2, 32), (8, 8, 64), (4, 1, 128), (6, 2, 80), (3, 1, 96), (5, 5, 24), (4, 4, 8), (4, 2, 256), (2, 1, 136), (24, 1, 40), (16, 2, 128),
+                                          (4, 2, 72), (2, 1, 88), (3, 3, 16), (2, 1, 104), (2, 1, 200), (6, 3, 80)])
 def test_prompts_heads(heads, kv, dim, dtype):
     _prompts_case([1, 37, 0, 64, 130], heads=heads, kv=kv, dim=dim, dtype=dtype, pad=5)
 
@@ -412,7 +413,8 @@ def test_prompts_behind_a_cache(lens, past, page, dim, cache_layout, dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("force", [1, 2])
 @pytest.mark.parametrize("lens,past,dim,heads,kv", [([1], [5000], 64, 4, 4), ([200, 3], [700, 3000], 128, 8, 2), ([900], None, 64, 2, 2), ([1, 0, 40], [0, 9, 2000], 80, 6, 2), ([17, 150], [1500, 33], 256, 2, 1),
-                                                   ([5] * 100 + [600], None, 32, 2, 1), ([0, 0], [4, 5], 64, 2, 2), ([64, 1], [4096, 4095], 96, 3, 1)])
+                                                   ([5] * 100 + [600], None, 32, 2, 1), ([0, 0], [4, 5], 64, 2, 2), ([64, 1], [4096, 4095], 96, 3, 1), ([70, 9], [900, 1300], 72, 4, 2),
+                                                   ([130], [1000], 88, 4, 1), ([33, 64], [640, 200], 16, 4, 4)])
 def test_prompts_both_ways_of_sharing_the_work(lens, past, dim, heads, kv, force, dtype):
     _prompts_case(lens, past=past, heads=heads, kv=kv, dim=dim, dtype=dtype, pad=3, force=force, page=16)
     if past:
