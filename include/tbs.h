@@ -466,7 +466,7 @@ int tbs_page_slots(const tbs_page_slots_args *args, void *stream);
  * positions[t] * freqs[j] (radians, in float64): (a, b) becomes (a cos - b sin, b cos + a sin), rounded once; elements from 2 * pairs on stay as they are.
  * With slots (then v, k_cache and v_cache as well; otherwise none of them) the turned key and the value of token t are written to token slots[t] % page of page slots[t] / page, if
  * 0 <= slots[t] < pages * page; of tokens with one slot, each 16 bytes are one's.  q_out and k_out may be q and k themselves (same strides) and lie over nothing else that is
- * read; the caches lie over nothing else either.  dim is at most 512. */
+ * read; the caches lie over nothing else either (what is between a cache's first and last number counts).  dim is at most 512. */
 typedef struct tbs_rotary_args {
     const void *q;               /* [tokens, heads, dim]; elements of a head side by side everywhere */
     const void *k, *v;           /* [tokens, kv_heads, dim] */
@@ -488,7 +488,7 @@ int tbs_rotary(const tbs_rotary_args *args, void *stream);
  * infinity reaches no output of a token that does not attend to it.  (Of a value that is infinite and has a weight that 16 bits, or float32, hold as 0 the product is
  * NaN.)  Weights are rounded to the type of the values.  Rows of no prompt, before starts[0] and from starts[prompts] on, are 0.  starts rises from 0 to at most `tokens`; other
  * numbers give wrong rows, nothing worse.  Tokens of the cache beyond table_width * page and on pages outside [0, pages) do not exist; a negative past counts as 0.
- * out may be q itself (same strides) and lies over nothing else that is read.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
+ * out may be q itself (same strides) and lies over nothing else that is read, nor between a cache's first and last number.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
  * a table's tokens with the batch's below 2^31 and 2^30.  Rows and heads on 16-byte boundaries are faster.  The same call gives the same bits.
  * workspace: tbs_attend_prompts_workspace(args) bytes on a 16-byte boundary (0: none), free again when the work is done. */
 typedef struct tbs_attend_prompts_args {

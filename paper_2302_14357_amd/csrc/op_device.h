@@ -149,3 +149,14 @@ static inline bool op_overlap(const OpHeads &a, const OpHeads &b, int64_t size) 
 
 static inline size_t op_dtype_size(int32_t dtype) { return dtype == TBS_F32 ? 4 : 2; }
 static inline bool op_dtype_known(int32_t dtype) { return dtype >= TBS_F32 && dtype <= TBS_F16; }
+
+// [pages, page, heads, dim] by elements: whether all memory between a cache's first and last number meets that of heads (a call that writes the one and reads the other is refused)
+struct OpCache {
+    const void *at;
+    int64_t pages, page, heads, dim, page_stride, token, head;
+};
+static inline bool op_overlap(const OpCache &a, const OpHeads &b, int64_t size) {
+    if (!a.at || !b.at || b.tokens < 1) return false;
+    const int64_t na = ((a.pages - 1) * a.page_stride + (a.page - 1) * a.token + (a.heads - 1) * a.head + a.dim) * size, nb = ((b.tokens - 1) * b.row + (b.heads - 1) * b.head + b.dim) * size;
+    return (uintptr_t)a.at < (uintptr_t)b.at + nb && (uintptr_t)b.at < (uintptr_t)a.at + na;
+}

@@ -886,6 +886,9 @@ static int prompts_call(const tbs_attend_prompts_args *args, int force, void *st
     if (op_folded(out) || (!op_same(q, out) && op_overlap(out, q, es)) || op_overlap(out, {a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head}, es) ||
         op_overlap(out, {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head}, es))
         return TBS_EINVAL;
+    if (a.past && (op_overlap(OpCache{a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head}, out, es) ||
+                   op_overlap(OpCache{a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head}, out, es)))
+        return TBS_EINVAL;
     const PromptsForm f = prompts_form(a, force);
     const PromptsSpace space = prompts_space(a, f);
     if (space.bytes > 0 && (!a.workspace || a.workspace_bytes < space.bytes || (uintptr_t)a.workspace % 16)) return TBS_EINVAL;

@@ -197,7 +197,10 @@ extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
             (a.pages > 1 && (a.k_cache_page < a.dim || a.v_cache_page < a.dim)))
             return TBS_EINVAL;
         const OpHeads v = {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head};
-        if (op_overlap(qo, v, es) || op_overlap(ko, v, es)) return TBS_EINVAL;
+        if (op_overlap(qo, v, es) || op_overlap(ko, v, es) || a.k_cache == a.v_cache) return TBS_EINVAL;
+        for (const OpCache &cache : {OpCache{a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head},
+                                     OpCache{a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head}})
+            if (op_overlap(cache, q, es) || op_overlap(cache, k, es) || op_overlap(cache, v, es) || op_overlap(cache, qo, es) || op_overlap(cache, ko, es)) return TBS_EINVAL;
     }
     RotaryP p = {};
     p.q = (const char *)a.q, p.k = (const char *)a.k, p.v = (const char *)a.v, p.q_out = (char *)a.q_out, p.k_out = (char *)a.k_out;

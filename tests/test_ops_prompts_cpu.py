@@ -57,7 +57,9 @@ def _rotary(ops, **kw):
                                  dict(q_out_row=511), dict(q_out_head=63), dict(k_out_head=0), dict(k_cache_head=63), dict(v_cache_token=63), dict(k_cache_page=63),
                                  # results over what is read, or over each other
                                  dict(q_out=A, q_out_row=640), dict(q_out=A + 2), dict(q_out=B), dict(q_out=B - 7 * 1024 + 2), dict(q_out=D + 2), dict(k_out=A), dict(k_out=B + 2), dict(k_out=D), dict(k_out=E),
-                                 dict(k_out=E + 7 * 1024 - 2)])
+                                 dict(k_out=E + 7 * 1024 - 2),
+                                 # a cache over what is read or written, over the other
+                                 dict(k_cache=A), dict(k_cache=B + 7 * 256 - 2), dict(v_cache=D - 204800 + 2), dict(v_cache=E - 204800 + 2), dict(k_cache=E * 2), dict(k_cache=E * 8)])
 def test_rotary_refuses(bad):
     L, ops = _ops()
     assert L.tbs_rotary(C.byref(_rotary(ops, **bad)), None) == -1
@@ -77,7 +79,8 @@ PLAIN = dict(past=None, tables=None, k_cache=None, v_cache=None)
                                  dict(PLAIN, tables=P), dict(PLAIN, k_cache=P), dict(tokens=-1), dict(tokens=1 << 28), dict(prompts=-1), dict(heads=7), dict(heads=0), dict(kv_heads=0), dict(dim=0), dict(dim=12),
                                  dict(dim=264), dict(page=0), dict(page=65537), dict(pages=0), dict(table_width=0), dict(ld_tables=9), dict(table_width=1 << 20, page=2048, ld_tables=1 << 20),
                                  dict(dtype=3), dict(q=A + 1), dict(k_cache=P + 1), dict(q_row=-1), dict(out_row=511), dict(out_head=63), dict(out_head=0),
-                                 dict(out=A, out_row=640), dict(out=A + 2), dict(out=A - 7 * 1024 + 2), dict(out=B), dict(out=B + 7 * 256 - 2), dict(out=D), dict(out=D - 7 * 1024 + 2)])
+                                 dict(out=A, out_row=640), dict(out=A + 2), dict(out=A - 7 * 1024 + 2), dict(out=B), dict(out=B + 7 * 256 - 2), dict(out=D), dict(out=D - 7 * 1024 + 2), dict(k_cache=E),
+                                 dict(v_cache=E - 204800 + 2), dict(out=E * 4 + 204800 - 2)])
 def test_prompts_refuses(bad):
     L, ops = _ops()
     assert L.tbs_attend_prompts(C.byref(_prompts(ops, **bad)), None) == -1
