@@ -486,7 +486,8 @@ int tbs_rotary(const tbs_rotary_args *args, void *stream);
  *     out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t - max),  and 0 where every score is -inf.
  * Query head h reads key head h / (heads / kv_heads).  The new tokens' keys and values are read from k and v, whether the cache has them already or not.  A NaN or an
  * infinity reaches no output of a token that does not attend to it.  (Of a value that is infinite and has a weight that 16 bits, or float32, hold as 0 the product is
- * NaN.)  Weights are rounded to the type of the values.  Rows of no prompt, before starts[0] and from starts[prompts] on, are 0.  starts rises from 0 to at most `tokens`; other
+ * NaN.)  Weights are rounded to the type of the values.  Values up to 0.99 of the type's largest number have a finite mean, however large the
+ * sum of them.  Rows of no prompt, before starts[0] and from starts[prompts] on, are 0.  starts rises from 0 to at most `tokens`; other
  * numbers give wrong rows, nothing worse.  Tokens of the cache beyond table_width * page and on pages outside [0, pages) do not exist; a negative past counts as 0.
  * out may be q itself (same strides) and lies over nothing else that is read, nor between a cache's first and last number.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
  * a table's tokens with the batch's below 2^31 and 2^30.  Rows and heads on 16-byte boundaries are faster.  The same call gives the same bits.

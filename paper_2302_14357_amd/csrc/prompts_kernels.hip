@@ -350,9 +350,8 @@ struct PromptsWork {
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     }
-    // Scores into weights.  D: how many times 32 dimensions are in o.
-    template <int D>
-    PROMPTS_INLINE void softmax(floatx16 (&s)[KB], int step, unsigned long long there) {
+    // the scores of keys that this lane's query does not see
+    PROMPTS_INLINE void hide(floatx16 (&s)[KB], int step, unsigned long long there) const {
         if (mixed(step, there)) {
             const unsigned long long bits = mine_of(step, there) >> (4 * h);
 #pragma unroll
@@ -360,23 +359,9 @@ struct PromptsWork {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] = bits >> (32 * b + 8 * (i / 4) + i % 4) & 1 ? s[b][i] : -INFINITY;
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
-        const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);   // (this lane's and its other half's)
-        top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
-        if (__any(top > m + PROMPTS_SLACK)) {
-            const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-            m = m1;
-            l *= a;
-#pragma unroll
-            for (int d = 0; d < D; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= a;
-        }
+    }
+    // Scores into weights, 2^(t - m), and these to their sum
+    PROMPTS_INLINE void weigh(floatx16 (&s)[KB]) {
         const float base = m == -INFINITY ? 0.f : m - MORE;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -393,6 +378,27 @@ struct PromptsWork {
         }
         l += sum[0] + sum[1];
         __builtin_amdgcn_sched_barrier(0);
+    }
+    PROMPTS_INLINE void softmax(floatx16 (&s)[KB], int step, unsigned long long there) {
+        hide(s, step, there);
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        typedef unsigned uint2_ __attribute__((ext_vector_type(2)));
+        const uint2_ u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);   // (this lane's and its other half's)
+        top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * p.scale2;
+        if (__any(top > m + PROMPTS_SLACK)) {
+            const float m1 = fmaxf(m, top), a = m1 == m ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+            m = m1;
+            l *= a;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= a;
+        }
+        weigh(s);
     }
     PROMPTS_INLINE void values(const floatx16 (&s)[KB], int step) {   // the weights with their values
         __builtin_amdgcn_s_setprio(1);
@@ -414,7 +420,7 @@ struct PromptsWork {
     PROMPTS_INLINE void start() {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = floatx16{};
-        m = -INFINITY, l = 0.f;
+        l = 0.f;
         if (first_step * TK < at.past) places<false>(p.kt), places<true>(p.vt);
         else if (first_step * TK >= at.past + TK) places<false>((unsigned)p.k_row), places<true>((unsigned)p.v_row);   // (ask() has them with the first new tile)
     }
@@ -426,9 +432,11 @@ struct PromptsWork {
             look(step + 2);
         }
     }
-    // All tiles.  A value that is NaN or infinite reaches, times the weight 0, the queries that do not see it; nothing of this pass is kept then.
+    // All tiles.  A value that is NaN or infinite reaches, times the weight 0, the queries that do not see it, and a sum of weights up to 2^8 and large values may be beyond
+    // float32 where their mean is not: of the outputs of this pass nothing is kept then.
     PROMPTS_INLINE void pass() {
         start();
+        m = -INFINITY;
         floatx16 s[KB];
         const int mine = min(steps, wave_last < 0 ? 0 : wave_last / TK + 1);   // steps in which the wave has something to do
         int step = first_step;
@@ -440,7 +448,7 @@ struct PromptsWork {
         if (step < mine) {
             scores(s, step);
             for (;;) {
-                softmax<DB>(s, step, there_of(step));
+                softmax(s, step, there_of(step));
                 landed();
                 ask_for(step + 1);
                 values(s, step);
@@ -454,7 +462,7 @@ struct PromptsWork {
             ask_for(step + 1);
         }
     }
-    // The d-th 32 dimensions, in o[0]; the keys of a tile that some query does not see all of are added one by one to the queries that see them.
+    // The d-th 32 dimensions, in o[0], with the reference that m is; keys are added one by one to the queries that see them.
     PROMPTS_INLINE void pass_apart(int d) {
         start();
         const char *place = v_place(sizeof(T) == 4 ? 0 : d);
@@ -468,7 +476,8 @@ struct PromptsWork {
                 const unsigned long long there = there_of(step);
                 floatx16 s[KB];
                 scores(s, step);
-                softmax<1>(s, step, there);
+                hide(s, step, there);
+                weigh(s);
                 const unsigned long long mine = mixed(step, there) ? mine_of(step, there) : ~0ull;
 #pragma unroll 1
                 for (int key = 0; key < TK; ++key) {
@@ -600,6 +609,10 @@ struct PromptsWork {
 #pragma unroll
             for (int d = 0; d < DB; ++d) store(o[d], d);
         } else {
+            // With the weights' sum in the reference they are parts of 1, and no sum of them is larger than the largest value.  (float16, whose small weights would
+            // lose digits: parts of 2^15, its values are 2^16 at most.)
+            m += __builtin_amdgcn_logf(l + __shfl_xor(l, 32)) - (__is_same(T, _Float16) ? 15.f : 0.f);   // (the logarithm to 2; -inf where there is no weight)
+            asm volatile("" : "+v"(h), "+v"(lane));   // (nothing of what follows is worked out ahead of the first pass, whose registers are few)
 #pragma unroll 1
             for (int d = 0; d < DB; ++d) {
                 pass_apart(d);
@@ -765,7 +778,17 @@ k_prompts_join(PromptsP p, int rows) {
                 o = make_float4(o.x + x[j].x * b, o.y + x[j].y * b, o.z + x[j].z * b, o.w + x[j].w * b);
             }
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
+        float f = l == 0.f ? 0.f : 1.f / l;
+        if (!(fabsf(o.x) < INFINITY && fabsf(o.y) < INFINITY && fabsf(o.z) < INFINITY && fabsf(o.w) < INFINITY)) {   // a sum beyond float32, where the mean may not be: each piece by its share
+            o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int j = 0; j < s.count; ++j) {
+                const int64_t from = ((int64_t)(s.first + j) * p.kv_heads + kvh) * rows + r;
+                const float mj = p.part_ml[from * 2], b = (mj == top ? 1.f : __builtin_amdgcn_exp2f(mj - top)) * f;
+                const float4 x = *(const float4 *)(p.part_o + from * p.dim + d);
+                o = make_float4(o.x + x.x * b, o.y + x.y * b, o.z + x.z * b, o.w + x.w * b);
+            }
+            f = 1.f;
+        }
         const T y[4] = {(T)(l == 0.f ? 0.f : o.x * f), (T)(l == 0.f ? 0.f : o.y * f), (T)(l == 0.f ? 0.f : o.z * f), (T)(l == 0.f ? 0.f : o.w * f)};
         __builtin_memcpy((T *)(p.out + (int64_t)(at.start + token) * p.o_row + (kvh * p.group + row - token * p.group) * p.o_head) + d, y, sizeof y);
     }

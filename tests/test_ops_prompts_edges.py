@@ -1,0 +1,45 @@
+"""The operators that bring prompts into the paged cache, at calls that the other tests do not make: the largest values, results in the place of what is
+read, strides of results, rows far apart, workspaces of short calls."""
+
+import math
+
+import pytest
+import torch
+
+from test_ops_prompts import _close, _gen, _i32, _prompts_by, _prompts_ref, _randn
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("size", [0.99, 1 / 300])
+def test_prompts_of_the_largest_values(size, dim, dtype):
+    """A mean of large values is no larger than they are, however large a sum of them is; next to them ordinary ones keep their digits.  (With scores of 0 and values of a 300th
+    of the largest number the sums of a few keys are finite, those of all are not.)"""
+    from paper_2302_14357_amd import attend_prompts
+    g = _gen(dim)
+    lens, past, page, heads, kv = [1, 70, 300], [0, 40, 900], 16, 4, 2
+    q = _randn(g, sum(lens), heads, dim, dtype=dtype) if size > 0.5 else torch.zeros(sum(lens), heads, dim, dtype=dtype)
+    k = _randn(g, sum(lens), kv, dim, dtype=dtype)
+    width = 57
+    tables = torch.arange(3 * width, dtype=torch.int32).view(3, width)
+    kc = _randn(g, 3 * width, page, kv, dim, dtype=dtype)
+
+    def values(*shape):
+        x = (torch.rand(*shape, generator=g, dtype=torch.float64) * 0.25 + 0.75) * size * torch.finfo(dtype).max
+        x[..., 1::4] *= torch.randint(0, 2, x[..., 1::4].shape, generator=g) * 2 - 1
+        x[..., 2::4] = torch.randn(x[..., 2::4].shape, generator=g)
+        return x.to(dtype)
+
+    v, vc = values(sum(lens), kv, dim), values(3 * width, page, kv, dim)
+    v[:, 1] = _randn(g, sum(lens), dim, dtype=dtype)   # (the other key head has ordinary ones)
+    vc[:, :, 1] = _randn(g, 3 * width, page, dim, dtype=dtype)
+    starts = _i32([0, 1, 71, 371])
+    for cached in (False, True):
+        kw = dict(past=_i32(past), k_cache=kc.cuda(), v_cache=vc.cuda(), tables=tables.cuda()) if cached else {}
+        ref, tol = _prompts_ref(q, k, v, lens, past if cached else None, kc, vc, tables, page, None, dtype)
+        for got in (attend_prompts(q.cuda(), k.cuda(), v.cuda(), starts, **kw), *(_prompts_by(f, q.cuda(), k.cuda(), v.cuda(), starts, **kw) for f in (1, 2))):
+            _close(got, ref, tol)
