@@ -150,11 +150,55 @@ static inline bool op_overlap(const OpHeads &a, const OpHeads &b, int64_t size) 
 static inline size_t op_dtype_size(int32_t dtype) { return dtype == TBS_F32 ? 4 : 2; }
 static inline bool op_dtype_known(int32_t dtype) { return dtype >= TBS_F32 && dtype <= TBS_F16; }
 
-// [pages, page, heads, dim] by elements: whether all memory between a cache's first and last number meets that of heads (a call that writes the one and reads the other is refused)
+// [pages, page, heads, dim] by elements
 struct OpCache {
     const void *at;
     int64_t pages, page, heads, dim, page_stride, token, head;
 };
+// Its dimensions of more than one place, from the longest stride on, and its numbers
+struct OpStrides {
+    int64_t count[3], stride[3], dim;
+    int n;
+    int64_t extent(int i) const {   // from the first number to behind the last, of the dimensions from the i-th on
+        int64_t e = dim;
+        for (; i < n; ++i) e += (count[i] - 1) * stride[i];
+        return e;
+    }
+};
+static inline OpStrides op_strides(const OpCache &a, int64_t size) {
+    OpStrides x = {};
+    x.dim = a.dim * size;
+    const int64_t count[] = {a.pages, a.page, a.heads}, stride[] = {a.page_stride, a.token, a.head};
+    for (int i = 0; i < 3; ++i) {
+        if (count[i] <= 1) continue;
+        int at = x.n++;
+        for (; at > 0 && x.stride[at - 1] < stride[i] * size; --at) x.count[at] = x.count[at - 1], x.stride[at] = x.stride[at - 1];
+        x.count[at] = count[i], x.stride[at] = stride[i] * size;
+    }
+    return x;
+}
+// whether its numbers may lie over each other
+static inline bool op_folded(const OpCache &a, int64_t size) {
+    const OpStrides x = op_strides(a, size);
+    for (int i = 0; i < x.n; ++i)
+        if (x.stride[i] < x.extent(i + 1)) return true;
+    return false;
+}
+// Whether numbers of b, which begins d bytes behind a, lie over numbers of a, neither of them folded: while both have a dimension alike, by the places whose distance can make
+// up for d (two at most); otherwise all memory between first and last
+static inline bool op_meet(const OpStrides &a, const OpStrides &b, int i, int64_t d) {
+    const int64_t na = a.extent(i), nb = b.extent(i);
+    if (d >= na || -d >= nb) return false;
+    if (i == a.n || i == b.n || a.count[i] != b.count[i] || a.stride[i] != b.stride[i]) return true;
+    const int64_t s = a.stride[i], q = d / s;
+    for (int64_t k = q - 1; k <= q + 1; ++k)
+        if (k > -a.count[i] && k < a.count[i] && op_meet(a, b, i + 1, d - k * s)) return true;
+    return false;
+}
+static inline bool op_overlap(const OpCache &a, const OpCache &b, int64_t size) {
+    return op_meet(op_strides(a, size), op_strides(b, size), 0, (int64_t)((uintptr_t)b.at - (uintptr_t)a.at));
+}
+// whether all memory between a cache's first and last number meets that of heads (a call that writes the one and reads the other is refused)
 static inline bool op_overlap(const OpCache &a, const OpHeads &b, int64_t size) {
     if (!a.at || !b.at || b.tokens < 1) return false;
     const int64_t na = ((a.pages - 1) * a.page_stride + (a.page - 1) * a.token + (a.heads - 1) * a.head + a.dim) * size, nb = ((b.tokens - 1) * b.row + (b.heads - 1) * b.head + b.dim) * size;

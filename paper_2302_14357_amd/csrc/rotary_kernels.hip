@@ -197,9 +197,10 @@ extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
             (a.pages > 1 && (a.k_cache_page < a.dim || a.v_cache_page < a.dim)))
             return TBS_EINVAL;
         const OpHeads v = {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head};
-        if (op_overlap(qo, v, es) || op_overlap(ko, v, es) || a.k_cache == a.v_cache) return TBS_EINVAL;
-        for (const OpCache &cache : {OpCache{a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head},
-                                     OpCache{a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head}})
+        const OpCache kc = {a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head},
+                      vc = {a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head};
+        if (op_overlap(qo, v, es) || op_overlap(ko, v, es) || op_folded(kc, es) || op_folded(vc, es) || op_overlap(kc, vc, es)) return TBS_EINVAL;
+        for (const OpCache &cache : {kc, vc})
             if (op_overlap(cache, q, es) || op_overlap(cache, k, es) || op_overlap(cache, v, es) || op_overlap(cache, qo, es) || op_overlap(cache, ko, es)) return TBS_EINVAL;
     }
     RotaryP p = {};

@@ -43,3 +43,28 @@ def test_prompts_of_the_largest_values(size, dim, dtype):
         ref, tol = _prompts_ref(q, k, v, lens, past if cached else None, kc, vc, tables, page, None, dtype)
         for got in (attend_prompts(q.cuda(), k.cuda(), v.cuda(), starts, **kw), *(_prompts_by(f, q.cuda(), k.cuda(), v.cuda(), starts, **kw) for f in (1, 2))):
             _close(got, ref, tol)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("layout", ["halves", "halves_by_head", "heads", "tokens"])
+def test_rotary_keys_and_values_in_one_tensor(layout, dtype):
+    """Caches between each other's first and last number that share none: the same entries as in tensors of their own."""
+    from paper_2302_14357_amd import rotary
+    g = _gen(7)
+    pages, page, kv, dim = 5, 4, 3, 24
+    q, k, v = (_randn(g, 17, n, dim, dtype=dtype).cuda() for n in (6, kv, kv))
+    at = torch.arange(17, dtype=torch.int32).cuda()
+    freqs = 0.7 ** torch.arange(12, dtype=torch.float64).cuda()
+    slots = torch.randperm(pages * page, generator=g)[:17].cuda()
+    kw = dict(v=v, slots=slots)
+    apart = [torch.full((pages, page, kv, dim), 77.0, dtype=dtype, device="cuda") for _ in range(2)]
+    want = rotary(q, k, at, freqs, k_cache=apart[0], v_cache=apart[1], **kw)
+    both = torch.full((pages * 2 * page * kv * dim,), 77.0, dtype=dtype, device="cuda")
+    halves = both.view(pages, 2, page * kv * dim)
+    kc, vc = {"halves": lambda: [halves[:, i].view(pages, page, kv, dim) for i in range(2)],
+              "halves_by_head": lambda: [halves[:, 0].view(pages, page, kv, dim), halves[:, 1].view(pages, kv, page, dim).transpose(1, 2)],
+              "heads": lambda: [both.view(pages, page, 2, kv, dim)[:, :, i] for i in range(2)],
+              "tokens": lambda: [both.view(pages, page, kv, 2, dim)[:, :, :, i] for i in range(2)]}[layout]()
+    got = rotary(q, k, at, freqs, k_cache=kc, v_cache=vc, **kw)
+    for x, y in zip((*want, *apart), (*got, kc, vc)):
+        assert torch.equal(x, y)
