@@ -433,14 +433,15 @@ int tbs_beam_reorder(const tbs_beam_reorder_args *args, void *stream);
  * Pages are the next ones of the list free_pages behind the *taken first: prompt after prompt, the shared ones, then those of its first row, and so on.  Entries
  * behind a row's pages are -1.  out_lens[beams * i] is lens[i] and those of the prompt's other rows are -1: places without a hypothesis yet, as tbs_beam_reorder takes them.
  * A prompt whose pages end behind the list's end, or that wants more than table_width of them, has no pages and lengths of -1 (and so has every later one that wants
- * any, where the list is too short).  *out_taken: the pages taken now, of all calls (a negative *taken counts as 0).  prompts * beams is below 2^31. */
+ * any, where the list is too short).  *out_taken: the pages taken now, of all calls (a negative *taken counts as 0).  What is written lies neither over itself nor over
+ * what is read.  prompts * beams is below 2^31. */
 typedef struct tbs_page_tables_args {
     const int32_t *lens;         /* [prompts] */
     const int32_t *free_pages;   /* [free_count] page numbers */
     const int32_t *taken;        /* one number */
     int32_t *tables;             /* [prompts * beams, table_width], row stride ld_tables */
     int32_t *out_lens;           /* [prompts * beams] */
-    int32_t *out_taken;          /* one number, not the one that is read */
+    int32_t *out_taken;          /* one number */
     int64_t ld_tables;
     int32_t prompts, beams, page, table_width, room, free_count;   /* page up to 65536, room up to 2^30 */
 } tbs_page_tables_args;

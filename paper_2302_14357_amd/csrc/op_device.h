@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "tbs.h"
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 op_bf16x8;
@@ -115,6 +117,22 @@ static inline bool op_overlap(OpRows a, OpRows b) {
         const int64_t s = i * a.ld - d;   // row i of a, from b's first byte
         const int64_t first = floor_div(s - b.width, b.ld) + 1, last = floor_div(s + a.width - 1, b.ld);
         if ((first > 0 ? first : 0) <= (last < b.rows ? last : b.rows - 1)) return true;
+    }
+    return false;
+}
+
+// rows of 32-bit or longer numbers that a call reads or writes as they are (none: at nothing)
+static inline OpRows op_rows(const void *at, int64_t rows, int64_t ld, int64_t cols, int64_t size) {
+    return {at, at && cols > 0 ? rows : 0, (rows > 1 ? ld : cols) * size, cols * size};
+}
+// whether what is written lies over itself or over what is read
+static inline bool op_written_over(std::initializer_list<OpRows> written, std::initializer_list<OpRows> read) {
+    for (const OpRows *w = written.begin(); w != written.end(); ++w) {
+        if (w->rows < 1) continue;
+        for (const OpRows *x = written.begin(); x != w; ++x)
+            if (x->rows > 0 && op_overlap(*w, *x)) return true;
+        for (const OpRows &x : read)
+            if (x.rows > 0 && op_overlap(*w, x)) return true;
     }
     return false;
 }

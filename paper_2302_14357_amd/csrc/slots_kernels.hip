@@ -208,8 +208,13 @@ extern "C" int tbs_page_tables(const tbs_page_tables_args *args, void *stream) {
     if (a.prompts < 0 || a.beams < 1 || a.beams > 65535 || a.page < 1 || a.page > 65536 || a.table_width < 1 || a.room < 0 || a.room > (1 << 30) || a.free_count < 0 ||
         (int64_t)a.table_width * a.page > (1 << 30) || (int64_t)a.prompts * a.beams > INT32_MAX)
         return TBS_EINVAL;
-    if (!a.taken || !a.out_taken || a.taken == a.out_taken) return TBS_EINVAL;
+    if (!a.taken || !a.out_taken) return TBS_EINVAL;
     if (a.prompts > 0 && (!a.lens || (!a.free_pages && a.free_count > 0) || !a.tables || !a.out_lens || a.ld_tables < a.table_width)) return TBS_EINVAL;
+    // (a workgroup reads the lengths of others' prompts, and the whole list may be its own)
+    const int64_t rows = (int64_t)a.prompts * a.beams;
+    if (op_written_over({op_rows(a.tables, rows, a.ld_tables, a.table_width, 4), op_rows(a.out_lens, 1, rows, rows, 4), op_rows(a.out_taken, 1, 1, 1, 4)},
+                        {op_rows(a.lens, 1, a.prompts, a.prompts, 4), op_rows(a.free_pages, 1, a.free_count, a.free_count, 4), op_rows(a.taken, 1, 1, 1, 4)}))
+        return TBS_EINVAL;
     const hipStream_t st = (hipStream_t)stream;
     TablesP p = {a.lens, a.free_pages, a.taken, a.tables, a.out_lens, a.out_taken, a.ld_tables, a.prompts, a.beams, a.page, a.table_width, a.room, a.free_count, 1};
     p.per = a.prompts / 1024 < 1 ? 1 : a.prompts / 1024 < TABLES_PER ? a.prompts / 1024 : TABLES_PER;

@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_ops_prompts_cpu import E, _ops, _rotary
+from test_ops_prompts_cpu import A, E, P, _ops, _rotary, _tables
 
 K = E * 4                                                                        # the keys' cache of _rotary: 50 pages of 16 tokens, 2 heads of 64, 2 bytes a number
 TURN = dict(k_cache_page=4096, k_cache_token=256, k_cache_head=128, v_cache_page=4096, v_cache_token=256, v_cache_head=128)   # (places between the heads for the other cache's)
@@ -18,3 +18,16 @@ TURN = dict(k_cache_page=4096, k_cache_token=256, k_cache_head=128, v_cache_page
 def test_rotary_refuses_caches_over_each_other(bad):
     L, ops = _ops()
     assert L.tbs_rotary(C.byref(_rotary(ops, **bad)), None) == -1
+
+
+# lens [4], free_pages [100], taken [1], tables [8, 10], out_lens [8], out_taken [1], each in memory of its own
+APART = dict(lens=P, free_pages=P + 1024, taken=P + 2048, tables=A, out_lens=A + 1024, out_taken=A + 2048)
+
+
+@pytest.mark.parametrize("bad", [dict(out_lens=P), dict(out_lens=P - 28), dict(out_lens=P + 12), dict(tables=P), dict(tables=P - 316), dict(out_taken=P + 12), dict(out_taken=P), dict(tables=P + 1020),
+                                 dict(out_lens=P + 1024 + 396), dict(out_taken=P + 1024 + 396), dict(out_lens=P + 2048), dict(tables=P + 2048 - 316), dict(out_taken=P + 2048), dict(out_lens=A),
+                                 dict(out_lens=A + 316), dict(out_taken=A + 320 - 4), dict(out_taken=A + 1024 + 28), dict(beams=1, out_lens=P), dict(tables=P - 200, ld_tables=25, beams=1)])
+def test_tables_refuses_results_over_what_is_read(bad):
+    """Every workgroup reads the lengths of all prompts before its own: a result in their place would be one of those."""
+    L, ops = _ops()
+    assert L.tbs_page_tables(C.byref(_tables(ops, **dict(APART, **bad))), None) == -1
