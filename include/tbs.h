@@ -450,7 +450,7 @@ int tbs_page_tables(const tbs_page_tables_args *args, void *stream);
 /* Where the tokens of a packed batch stand and go.  The batch holds lens[i] new tokens of prompt i, prompt after prompt; past[i] tokens came before them.
  * starts[i] is the first token of prompt i and starts[prompts] the first behind all (each at most `tokens`); token t of prompt i has the position
  * past[i] + t - starts[i] and the slot tables[i, position / page] * page + position % page, -1 where the table has no page for it.  Tokens of no prompt: position and
- * slot -1.  Negative lens and past count as 0. */
+ * slot -1.  Negative lens and past count as 0.  What is written lies neither over itself nor over what is read. */
 typedef struct tbs_page_slots_args {
     const int32_t *lens;     /* [prompts] */
     const int32_t *past;     /* [prompts] or NULL: none have any */

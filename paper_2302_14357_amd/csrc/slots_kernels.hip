@@ -228,6 +228,10 @@ extern "C" int tbs_page_slots(const tbs_page_slots_args *args, void *stream) {
     const tbs_page_slots_args &a = *args;
     if (a.prompts < 0 || a.tokens < 0 || a.page < 1 || a.page > 65536 || a.table_width < 1 || (int64_t)a.table_width * a.page > (1 << 30)) return TBS_EINVAL;
     if (!a.starts || (a.prompts > 0 && (!a.lens || !a.tables || a.ld_tables < a.table_width)) || (a.tokens > 0 && (!a.positions || !a.slots))) return TBS_EINVAL;
+    // (every workgroup reads the lengths)
+    if (op_written_over({op_rows(a.starts, 1, (int64_t)a.prompts + 1, (int64_t)a.prompts + 1, 4), op_rows(a.positions, 1, a.tokens, a.tokens, 4), op_rows(a.slots, 1, a.tokens, a.tokens, 8)},
+                        {op_rows(a.lens, 1, a.prompts, a.prompts, 4), op_rows(a.past, 1, a.prompts, a.prompts, 4), op_rows(a.tables, a.prompts, a.ld_tables, a.table_width, 4)}))
+        return TBS_EINVAL;
     const SlotsP p = {a.lens, a.past, a.tables, a.starts, a.positions, a.slots, a.ld_tables, a.prompts, a.tokens, a.table_width, a.page};
     const unsigned blocks = (unsigned)((a.tokens + (int64_t)SLOTS_TOKENS - 1) / SLOTS_TOKENS) + 1;
     hipLaunchKernelGGL(k_page_slots, dim3(blocks), dim3(SLOTS_THREADS), 0, (hipStream_t)stream, p);

@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_ops_prompts_cpu import A, E, P, _ops, _rotary, _tables
+from test_ops_prompts_cpu import A, E, P, _ops, _rotary, _slots, _tables
 
 K = E * 4                                                                        # the keys' cache of _rotary: 50 pages of 16 tokens, 2 heads of 64, 2 bytes a number
 TURN = dict(k_cache_page=4096, k_cache_token=256, k_cache_head=128, v_cache_page=4096, v_cache_token=256, v_cache_head=128)   # (places between the heads for the other cache's)
@@ -31,3 +31,14 @@ def test_tables_refuses_results_over_what_is_read(bad):
     """Every workgroup reads the lengths of all prompts before its own: a result in their place would be one of those."""
     L, ops = _ops()
     assert L.tbs_page_tables(C.byref(_tables(ops, **dict(APART, **bad))), None) == -1
+
+
+# lens [4], past [4], tables [4, 10], starts [5], positions [50], slots [50]
+PLACES = dict(lens=P, past=P + 1024, tables=P + 2048, starts=A, positions=A + 1024, slots=A + 2048)
+
+
+@pytest.mark.parametrize("bad", [dict(starts=P), dict(starts=P - 16), dict(starts=P + 1036), dict(positions=P - 196), dict(positions=P + 2048 + 156), dict(slots=P + 12), dict(slots=P + 1032), dict(slots=P + 2048 - 392),
+                                 dict(positions=A), dict(slots=A + 1024 + 196), dict(starts=A + 2048 + 396), dict(starts=P + 2048, ld_tables=20), dict(past=None, starts=P)])
+def test_slots_refuses_results_over_what_is_read(bad):
+    L, ops = _ops()
+    assert L.tbs_page_slots(C.byref(_slots(ops, **dict(PLACES, **bad))), None) == -1
