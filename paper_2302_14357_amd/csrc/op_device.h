@@ -142,6 +142,8 @@ struct OpHeads {
     const void *at;
     int64_t tokens, heads, dim, row, head;
 };
+// rows of `bytes` bytes, `ld` apart, among heads of numbers of `size` (none: at nothing)
+static inline OpHeads op_plain(const void *at, int64_t rows, int64_t ld, int64_t bytes, int64_t size) { return {at, at && bytes > 0 ? rows : 0, 1, bytes / size, ld / size, 0}; }
 static inline bool op_same(const OpHeads &a, const OpHeads &b) {
     return a.at == b.at && (a.row == b.row || a.tokens <= 1) && (a.head == b.head || a.heads <= 1);
 }

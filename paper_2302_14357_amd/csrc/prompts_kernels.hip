@@ -907,7 +907,8 @@ static int prompts_call(const tbs_attend_prompts_args *args, int force, void *st
     // what is written lies neither over itself nor over what others read; queries are read by those who write in their place
     const OpHeads q = {a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head}, out = {a.out, a.tokens, a.heads, a.dim, a.out_row, a.out_head};
     if (op_folded(out) || (!op_same(q, out) && op_overlap(out, q, es)) || op_overlap(out, {a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head}, es) ||
-        op_overlap(out, {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head}, es))
+        op_overlap(out, {a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head}, es) || op_overlap(out, op_plain(a.starts, 1, 0, 4ll * a.prompts + 4, es), es) ||
+        op_overlap(out, op_plain(a.past, 1, 0, 4ll * a.prompts, es), es) || op_overlap(out, op_plain(a.tables, a.prompts, a.ld_tables * 4, 4ll * a.table_width, es), es))
         return TBS_EINVAL;
     if (a.past && (op_overlap(OpCache{a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head}, out, es) ||
                    op_overlap(OpCache{a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head}, out, es)))

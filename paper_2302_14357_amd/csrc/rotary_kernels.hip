@@ -192,6 +192,9 @@ extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
     if (op_folded(qo) || op_folded(ko) || op_overlap(qo, ko, es) || op_overlap(qo, k, es) || op_overlap(ko, q, es) || (!op_same(q, qo) && op_overlap(qo, q, es)) ||
         (!op_same(k, ko) && op_overlap(ko, k, es)))
         return TBS_EINVAL;
+    const OpHeads plain[] = {op_plain(a.positions, 1, 0, 4ll * a.tokens, es), op_plain(a.freqs, 1, 0, 8ll * a.pairs, es), op_plain(a.slots, 1, 0, 8ll * a.tokens, es)};
+    for (const OpHeads &x : plain)
+        if (op_overlap(qo, x, es) || op_overlap(ko, x, es)) return TBS_EINVAL;
     if (cached) {
         if ((a.kv_heads > 1 && (a.k_cache_head < a.dim || a.v_cache_head < a.dim)) || (a.page > 1 && (a.k_cache_token < a.dim || a.v_cache_token < a.dim)) ||
             (a.pages > 1 && (a.k_cache_page < a.dim || a.v_cache_page < a.dim)))
@@ -200,8 +203,11 @@ extern "C" int tbs_rotary(const tbs_rotary_args *args, void *stream) {
         const OpCache kc = {a.k_cache, a.pages, a.page, a.kv_heads, a.dim, a.k_cache_page, a.k_cache_token, a.k_cache_head},
                       vc = {a.v_cache, a.pages, a.page, a.kv_heads, a.dim, a.v_cache_page, a.v_cache_token, a.v_cache_head};
         if (op_overlap(qo, v, es) || op_overlap(ko, v, es) || op_folded(kc, es) || op_folded(vc, es) || op_overlap(kc, vc, es)) return TBS_EINVAL;
-        for (const OpCache &cache : {kc, vc})
+        for (const OpCache &cache : {kc, vc}) {
             if (op_overlap(cache, q, es) || op_overlap(cache, k, es) || op_overlap(cache, v, es) || op_overlap(cache, qo, es) || op_overlap(cache, ko, es)) return TBS_EINVAL;
+            for (const OpHeads &x : plain)
+                if (op_overlap(cache, x, es)) return TBS_EINVAL;
+        }
     }
     RotaryP p = {};
     p.q = (const char *)a.q, p.k = (const char *)a.k, p.v = (const char *)a.v, p.q_out = (char *)a.q_out, p.k_out = (char *)a.k_out;

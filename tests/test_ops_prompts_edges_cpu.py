@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_ops_prompts_cpu import A, E, P, _ops, _rotary, _slots, _tables
+from test_ops_prompts_cpu import A, E, P, _ops, _prompts, _rotary, _slots, _tables
 
 K = E * 4                                                                        # the keys' cache of _rotary: 50 pages of 16 tokens, 2 heads of 64, 2 bytes a number
 TURN = dict(k_cache_page=4096, k_cache_token=256, k_cache_head=128, v_cache_page=4096, v_cache_token=256, v_cache_head=128)   # (places between the heads for the other cache's)
@@ -42,3 +42,24 @@ PLACES = dict(lens=P, past=P + 1024, tables=P + 2048, starts=A, positions=A + 10
 def test_slots_refuses_results_over_what_is_read(bad):
     L, ops = _ops()
     assert L.tbs_page_slots(C.byref(_slots(ops, **dict(PLACES, **bad))), None) == -1
+
+
+@pytest.mark.parametrize("name", ["q_out", "k_out", "k_cache", "v_cache"])
+@pytest.mark.parametrize("bad", [dict(positions=1022), dict(positions=-26), dict(freqs=1022), dict(freqs=-254), dict(slots=1022), dict(slots=-54)])
+def test_rotary_refuses_results_over_positions_frequencies_and_slots(name, bad):
+    """(addresses from the result's first byte: its first row is longer than that of any)"""
+    L, ops = _ops()
+    at = dict(q_out=E, k_out=E * 2, k_cache=K, v_cache=E * 8)[name]
+    for k, v in bad.items():
+        assert L.tbs_rotary(C.byref(_rotary(ops, **{k: at + min(v, 254 if name != "q_out" else v)})), None) == -1
+    if name[1] == "_" and "cache" not in name:   # without a cache as well
+        plain = dict(v=None, slots=None, k_cache=None, v_cache=None)
+        for k, v in bad.items():
+            if k != "slots":
+                assert L.tbs_rotary(C.byref(_rotary(ops, **dict(plain, **{k: at + min(v, 254)}))), None) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(starts=E), dict(starts=E - 14), dict(starts=E + 7166), dict(past=E - 10), dict(past=E + 7166), dict(tables=E - 118), dict(tables=E + 7166), dict(tables=E - 1000, ld_tables=250)])
+def test_prompts_refuses_results_over_starts_past_and_tables(bad):
+    L, ops = _ops()
+    assert L.tbs_attend_prompts(C.byref(_prompts(ops, **bad)), None) == -1
