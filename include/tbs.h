@@ -466,7 +466,7 @@ int tbs_page_slots(const tbs_page_slots_args *args, void *stream);
 /* Rotary positions, and keys and values into the cache.  Pair j < pairs of a head, its elements j and pairs + j (interleaved: 2 j and 2 j + 1), is turned by the angle
  * positions[t] * freqs[j] (radians, in float64): (a, b) becomes (a cos - b sin, b cos + a sin), rounded once; elements from 2 * pairs on stay as they are.
  * With slots (then v, k_cache and v_cache as well; otherwise none of them) the turned key and the value of token t are written to token slots[t] % page of page slots[t] / page, if
- * 0 <= slots[t] < pages * page; of tokens with one slot, each 16 bytes are one's.  q_out and k_out may be q and k themselves (same strides) and lie over nothing else that is
+ * 0 <= slots[t] < pages * page; of tokens with one slot each number there is one's, open whose.  q_out and k_out may be q and k themselves (same strides) and lie over nothing else that is
  * read; the caches lie over nothing else either (what is between a cache's first and last number counts) and neither over themselves nor over each other (keys and values in turn in
  * one tensor are fine, with strides alike from the longest on down to where they part).  dim is at most 512. */
 typedef struct tbs_rotary_args {

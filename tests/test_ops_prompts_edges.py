@@ -68,3 +68,20 @@ def test_rotary_keys_and_values_in_one_tensor(layout, dtype):
     got = rotary(q, k, at, freqs, k_cache=kc, v_cache=vc, **kw)
     for x, y in zip((*want, *apart), (*got, kc, vc)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,pairs,shift", [(64, 32, 0), (64, 20, 0), (64, 32, 1), (40, 17, 3), (7, 3, 0)])
+def test_rotary_tokens_with_one_slot_mix_whole_numbers(dim, pairs, shift, interleaved, dtype):
+    """Of tokens that name one slot every number is one's, also where pieces of 16 bytes begin inside each other's; no neighbour of the slot is touched."""
+    from paper_2302_14357_amd import rotary
+    g = _gen(pairs)
+    q, k, v = (_randn(g, 300, n, dim, dtype=dtype).cuda() for n in (2, 2, 2))
+    kc, vc = (torch.full((shift + 12 * 2 * dim,), 77.0, dtype=dtype, device="cuda")[shift:].view(3, 4, 2, dim) for _ in range(2))
+    slots = torch.full((300,), 5).cuda()
+    slots[17] = 6
+    _, turned = rotary(q, k, torch.arange(300, dtype=torch.int32).cuda(), 0.9 ** torch.arange(pairs, dtype=torch.float64).cuda(), interleaved=interleaved, v=v, k_cache=kc, v_cache=vc, slots=slots)
+    for cache, new in ((kc.view(12, 2, dim), turned), (vc.view(12, 2, dim), v)):
+        assert bool((cache[5] == new[slots == 5]).any(0).all())
+        assert torch.equal(cache[6], new[17]) and bool((cache[[0, 1, 2, 3, 4, 7, 8, 9, 10, 11]] == 77.0).all())
