@@ -85,3 +85,53 @@ def test_rotary_tokens_with_one_slot_mix_whole_numbers(dim, pairs, shift, interl
     for cache, new in ((kc.view(12, 2, dim), turned), (vc.view(12, 2, dim), v)):
         assert bool((cache[5] == new[slots == 5]).any(0).all())
         assert torch.equal(cache[6], new[17]) and bool((cache[[0, 1, 2, 3, 4, 7, 8, 9, 10, 11]] == 77.0).all())
+
+
+def _rotary_call(q, k, v, at, freqs, slots, kc, vc, q_out, k_out, interleaved):
+    """tbs_rotary itself, with outputs of the caller's."""
+    import ctypes
+    from paper_2302_14357_amd import ops
+    L = ops.load_library()
+    a = ops._Rotary(q=q.data_ptr(), k=k.data_ptr(), positions=at.data_ptr(), freqs=freqs.data_ptr(), q_out=q_out.data_ptr(), k_out=k_out.data_ptr(), tokens=q.shape[0], heads=q.shape[1],
+                    kv_heads=k.shape[1], dim=q.shape[2], pairs=len(freqs), interleaved=int(interleaved), dtype=DTYPES.index(q.dtype))
+    a.q_row, a.q_head, a.k_row, a.k_head = *q.stride()[:2], *k.stride()[:2]
+    a.q_out_row, a.q_out_head, a.k_out_row, a.k_out_head = *q_out.stride()[:2], *k_out.stride()[:2]
+    if slots is not None:
+        a.v, a.slots, a.k_cache, a.v_cache, a.pages, a.page = v.data_ptr(), slots.data_ptr(), kc.data_ptr(), vc.data_ptr(), kc.shape[0], kc.shape[1]
+        a.v_row, a.v_head = v.stride()[:2]
+        a.k_cache_page, a.k_cache_token, a.k_cache_head = kc.stride()[:3]
+        a.v_cache_page, a.v_cache_token, a.v_cache_head = vc.stride()[:3]
+    assert L.tbs_rotary(ctypes.byref(a), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,pairs", [(64, 32), (80, 16), (64, 20), (37, 17), (512, 256), (512, 255), (128, 64), (16, 0)])
+@pytest.mark.parametrize("cached", [False, True])
+def test_rotary_in_place_and_with_strides(cached, dim, pairs, interleaved, dtype):
+    """Queries and keys turned where they are, beside their values in one tensor, and results with places between heads and tokens: bit for bit those of a call that makes its own."""
+    from paper_2302_14357_amd import rotary
+    g = _gen(dim + pairs)
+    for tokens, heads, kv, shift in ((1, 1, 1, 0), (9, 4, 2, 0), (2100, 3, 1, 0), (70, 5, 5, 1)):
+        x = _randn(g, tokens, heads + 2 * kv, dim, dtype=dtype)
+        room = torch.empty(x.numel() + shift, dtype=dtype, device="cuda")[shift:].view(x.shape).copy_(x)
+        q, k, v = room[:, :heads], room[:, heads:heads + kv], room[:, heads + kv:]
+        at = torch.randint(0, 5000, (tokens,), generator=g, dtype=torch.int32).cuda()
+        freqs = 10000.0 ** -(torch.arange(pairs, dtype=torch.float64) / max(pairs, 1)).cuda()
+        slots = torch.randperm(tokens + 9, generator=g)[:tokens].cuda()
+        caches = [[torch.full((tokens // 7 + 2, 7, kv, dim), 77.0, dtype=dtype, device="cuda") for _ in range(2)] for _ in range(3)]
+        kw = dict(v=v, slots=slots, k_cache=caches[0][0], v_cache=caches[0][1]) if cached else {}
+        want = rotary(q, k, at, freqs, interleaved=interleaved, **kw)
+        # results with room around every head
+        big = torch.full((tokens + 2, heads + kv + 1, dim + 3), 77.0, dtype=dtype, device="cuda")
+        q2, k2 = big[1:tokens + 1, :heads, :dim], big[1:tokens + 1, heads:heads + kv, 1:dim + 1]
+        _rotary_call(q, k, v, at, freqs, slots if cached else None, *caches[1], q2, k2, interleaved)
+        assert torch.equal(q2, want[0]) and torch.equal(k2, want[1]) and torch.equal(room.cpu(), x)
+        q2.fill_(77.0), k2.fill_(77.0)
+        assert bool((big == 77.0).all())
+        # in place
+        _rotary_call(q, k, v, at, freqs, slots if cached else None, *caches[2], q, k, interleaved)
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v.cpu(), x[:, heads + kv:])
+        for i in (1, 2):
+            assert torch.equal(caches[i][0], caches[0][0]) and torch.equal(caches[i][1], caches[0][1])
