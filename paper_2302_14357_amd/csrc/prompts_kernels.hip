@@ -100,7 +100,7 @@ __device__ __forceinline__ int2 prompts_find(const PromptsP &p, int unit, int ro
 
 template <class T, int DP>
 struct PromptsTile {
-    static constexpr int E = OpPiece<T>::E, KEYS = sizeof(T) == 4 || DP > 128 ? 32 : 64;
+    static constexpr int E = OpPiece<T>::E, KEYS = sizeof(T) == 4 || DP > 128 ? 32 : 64;   // (prompts_form() counts with them)
     static constexpr int USED = DP / E;                                       // pieces of a row
     static constexpr int PITCH = USED <= 4 ? 4 : USED <= 8 ? 8 : sizeof(T) == 2 && USED <= 12 ? 12 : USED <= 16 ? 16 : USED <= 32 ? 32 : 64;   // ... in LDS
     static constexpr int BYTES = KEYS * PITCH * 16;                           // of keys, or values
@@ -634,6 +634,7 @@ k_prompts(PromptsP p) {
 #define PROMPTS_PLAN 1024     // threads of the plan; tiles, and prompts, at most
 #define PROMPTS_LENGTHS 16    // lengths of pieces that are looked at
 #define PROMPTS_PIECES 4      // pieces of an equal share at most
+#define PROMPTS_LEAST 4       // steps of a piece at least, where a tile has more than one
 __device__ const int prompts_parts[PROMPTS_LENGTHS] = {16, 18, 20, 22, 25, 28, 32, 36, 40, 44, 50, 56, 64, 96, 128, 0};   // 64ths of a share; 0: whole tiles
 
 // workgroups of four waves that the chip runs at a time: one to three a CU, by their registers
@@ -696,7 +697,7 @@ k_prompts_plan(PromptsP p, int rows, int step, int most, int slots) {
     }
     __syncthreads();
     const int longest = max(s_longest, 1);
-    const int64_t all = (int64_t)s_all, share = max((all * p.kv_heads + slots - 1) / slots, (int64_t)4 * PROMPTS_PIECES);
+    const int64_t all = (int64_t)s_all, share = max((all * p.kv_heads + slots - 1) / slots, (int64_t)PROMPTS_LEAST * PROMPTS_PIECES);
     // a lane a length, and a quarter of the wave's tiles
     const int part = prompts_parts[lane & (PROMPTS_LENGTHS - 1)], length = part ? (int)min((int64_t)longest, (share * part + 63) / 64) : longest;
     if (wave * 64 < tiles) {
@@ -812,7 +813,11 @@ static PromptsForm prompts_form(const tbs_attend_prompts_args &a, int force) {
     const int64_t longest = a.past ? (int64_t)a.table_width * a.page : a.prompts > 0 ? a.tokens / a.prompts : 0, blocks = f.tiles * a.kv_heads, slots = prompts_slots(a);
     const bool few = longest >= 768 && blocks * 4096 < slots * std::min<int64_t>(longest, a.past ? 4096 : 2867);
     f.shared = f.tiles <= PROMPTS_PLAN && a.prompts > 0 && (force ? force == 2 : few);
-    f.units = f.tiles + 1 + (f.shared ? slots * PROMPTS_PIECES / a.kv_heads + 1 : 0);   // (a piece is a quarter of an equal share of all steps, or more)
+    f.units = f.tiles + 1;
+    if (f.shared) {   // a piece is a quarter of an equal share of all steps, or more, and four steps or a whole tile
+        const int64_t keys = (a.past ? (int64_t)a.table_width * a.page : 0) + a.tokens, step = PROMPTS_LEAST * (a.dtype == TBS_F32 || a.dim > 128 ? 32 : 64);
+        f.units += std::min<int64_t>(slots * PROMPTS_PIECES / a.kv_heads + 1, f.tiles * ((keys + step - 1) / step - 1));
+    }
     return f;
 }
 

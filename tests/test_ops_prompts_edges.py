@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from test_ops_prompts import _close, _gen, _i32, _prompts_by, _prompts_ref, _randn
+from test_ops_prompts import _close, _gen, _i32, _prompts_by, _prompts_case, _prompts_ref, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -43,6 +43,14 @@ def test_prompts_of_the_largest_values(size, dim, dtype):
         ref, tol = _prompts_ref(q, k, v, lens, past if cached else None, kc, vc, tables, page, None, dtype)
         for got in (attend_prompts(q.cuda(), k.cuda(), v.cuda(), starts, **kw), *(_prompts_by(f, q.cuda(), k.cuda(), v.cuda(), starts, **kw) for f in (1, 2))):
             _close(got, ref, tol)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [32, 64, 128, 256])
+@pytest.mark.parametrize("lens,past", [([1], [127]), ([1], [255]), ([1], [256]), ([4], [1020]), ([1], [1504]), ([1] * 8, [1504, 3, 0, 700, 255, 256, 1023, 1]), ([130, 1], [896, 1024])])
+def test_prompts_pieces_of_short_calls(lens, past, dim, dtype):
+    """Keys shared out where the workspace has room for as many pieces of four steps as there may be, and none more (what lies behind it stays)."""
+    _prompts_case(lens, past=past, heads=4, kv=2, dim=dim, dtype=dtype, pad=3, force=2)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -63,3 +63,15 @@ def test_rotary_refuses_results_over_positions_frequencies_and_slots(name, bad):
 def test_prompts_refuses_results_over_starts_past_and_tables(bad):
     L, ops = _ops()
     assert L.tbs_attend_prompts(C.byref(_prompts(ops, **bad)), None) == -1
+
+
+@pytest.mark.parametrize("call,most", [(dict(tokens=1, prompts=1, heads=32, kv_heads=8, dim=128, page=16, table_width=94, pages=94), 4 << 20),
+                                       (dict(tokens=8, prompts=8, heads=8, kv_heads=8, dim=64, page=16, table_width=94, pages=800), 14 << 20),
+                                       (dict(tokens=1000, prompts=1, heads=8, kv_heads=8, dim=64, past=None), 10 << 20),
+                                       (dict(tokens=1, prompts=1, heads=1, kv_heads=1, dim=256, page=16, table_width=64, pages=64, dtype=0), 2 << 20),
+                                       (dict(tokens=256, prompts=1, heads=8, kv_heads=8, dim=128, page=64, table_width=1600, pages=1600), 170 << 20)])
+def test_prompts_workspace_is_as_large_as_the_call(call, most):
+    """Pieces are four steps of 32 or 64 keys or more: a short table makes few of them, and a long one no more than the chip has places for."""
+    L, ops = _ops()
+    n = L.tbs_attend_prompts_workspace(C.byref(_prompts(ops, **call)))
+    assert 0 < n <= most, n
