@@ -318,7 +318,7 @@ int tbs_gemm_bf16(const void *A, const void *B, const float *bias, float *C, int
  * causal attention.  Every argument block is read before the call returns; all
  * pointers in it are DEVICE and borrowed until the work enqueued on `stream` is done.  Kernels run on the current device, nothing is
  * allocated or synchronised, and the calls may be captured into a graph.  Blocks are zeroed by the caller first: fields that are not named
- * are 0.  Strides count elements.  Sums, softmax statistics and scores are held in float32 or more; each output is rounded once. */
+ * are 0.  Strides count elements; those of heads, tokens and pages are at most 2^26.  Sums, softmax statistics and scores are held in float32 or more; each output is rounded once. */
 enum tbs_dtype { TBS_F32 = 0, TBS_BF16 = 1, TBS_F16 = 2 };
 enum tbs_act { TBS_ACT_NONE = 0, TBS_ACT_RELU = 1, TBS_ACT_TANH = 2, TBS_ACT_GELU = 3 /* 0.5 y (1 + erf(y / sqrt 2)) */,
                TBS_ACT_SILU = 4 };
@@ -492,7 +492,8 @@ int tbs_rotary(const tbs_rotary_args *args, void *stream);
  * sum of them.  Rows of no prompt, before starts[0] and from starts[prompts] on, are 0.  starts rises from 0 to at most `tokens`; other
  * numbers give wrong rows, nothing worse.  Tokens of the cache beyond table_width * page and on pages outside [0, pages) do not exist; a negative past counts as 0.
  * out may be q itself (same strides) and lies over nothing else that is read, nor between a cache's first and last number.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
- * a table's tokens with the batch's below 2^31 and 2^30.  Rows and heads on 16-byte boundaries are faster.  The same call gives the same bits.
+ * a table's tokens with the batch's below 2^31 and 2^30, a page's stride and `page` tokens' below 4 GiB.  Rows and heads on 16-byte boundaries, and keys and values of new tokens less than 32 MiB apart,
+ * are faster.  The same call gives the same bits.
  * workspace: tbs_attend_prompts_workspace(args) bytes on a 16-byte boundary (0: none), free again when the work is done. */
 typedef struct tbs_attend_prompts_args {
     const void *q;                       /* [tokens, heads, dim]; elements of a head side by side everywhere */

@@ -903,12 +903,12 @@ static int prompts_call(const tbs_attend_prompts_args *args, int force, void *st
         if ((uintptr_t)x % es) return TBS_EINVAL;
         direct &= (uintptr_t)x % 16 == 0;
     }
-    // (addresses in the cache: a page's number times 32 bits, a place in the page of 32 bits; in a tile of new tokens 32 bits from its first)
-    const int64_t wide[] = {a.k_cache_token * es * a.page, a.v_cache_token * es * a.page, a.k_cache_page * es, a.v_cache_page * es, a.k_row * es * 64, a.v_row * es * 64};
-    for (int i = 0; i < 6; ++i)
-        if ((i >= 4 || (a.past && (i < 2 || a.pages > 1))) && wide[i] > INT32_MAX) {
-            if (i < 4 ? wide[i] > UINT32_MAX - 8192ll : a.tokens > 1) return TBS_EINVAL;
-        }
+    // Addresses in the cache: a page's number times 32 bits, a place in the page of 32 bits.
+    const int64_t wide[] = {a.k_cache_token * es * a.page, a.v_cache_token * es * a.page, a.k_cache_page * es, a.v_cache_page * es};
+    for (int i = 0; i < (a.past ? a.pages > 1 ? 4 : 2 : 0); ++i)
+        if (wide[i] > UINT32_MAX - 8192ll) return TBS_EINVAL;
+    // ... and of direct loads from new tokens 32 bits from a tile's first; rows that are further apart than that go through registers
+    if (a.tokens > 1 && (a.k_row * es * 64 > INT32_MAX || a.v_row * es * 64 > INT32_MAX)) direct = false;
     // what is written lies neither over itself nor over what others read; queries are read by those who write in their place
     const OpHeads q = {a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head}, out = {a.out, a.tokens, a.heads, a.dim, a.out_row, a.out_head};
     if (op_folded(out) || (!op_same(q, out) && op_overlap(out, q, es)) || op_overlap(out, {a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head}, es) ||

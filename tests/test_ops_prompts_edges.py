@@ -143,3 +143,23 @@ def test_rotary_in_place_and_with_strides(cached, dim, pairs, interleaved, dtype
         assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v.cpu(), x[:, heads + kv:])
         for i in (1, 2):
             assert torch.equal(caches[i][0], caches[0][0]) and torch.equal(caches[i][1], caches[0][1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("which", ["k", "v", "both"])
+def test_prompts_rows_far_apart(which, dtype):
+    """New tokens' keys or values 32 MiB apart and more: the bits of a call on rows side by side."""
+    from paper_2302_14357_amd import attend_prompts
+    g = _gen(4)
+    tokens, heads, kv, dim = 140, 4, 2, 64
+    far = torch.empty(tokens, 2**25 // dtype.itemsize + 8, dtype=dtype, device="cuda")
+    assert far.stride(0) * far.element_size() * 64 > 2**31
+    q, k, v = (_randn(g, tokens, n, dim, dtype=dtype).cuda() for n in (heads, kv, kv))
+    kf, vf = (far[:, i:i + kv * dim].view(tokens, kv, dim).copy_(x) if which in (n, "both") else x for i, n, x in ((0, "k", k), (kv * dim, "v", v)))
+    starts = _i32([0, 7, tokens])
+    kc, vc = (_randn(g, 12, 16, kv, dim, dtype=dtype).cuda() for _ in range(2))
+    cached = dict(past=_i32([70, 30]), k_cache=kc, v_cache=vc, tables=_i32([[0, 1, 2, 3, 4, 5], [6, 7, 8, 9, 10, 11]]))
+    for kw in ({}, cached):
+        assert torch.equal(attend_prompts(q, kf, vf, starts, **kw), attend_prompts(q, k, v, starts, **kw))
+        for force in (1, 2):
+            assert torch.equal(_prompts_by(force, q, kf, vf, starts, **kw), _prompts_by(force, q, k, v, starts, **kw))
