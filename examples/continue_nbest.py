@@ -119,7 +119,7 @@ def continue_nbest(lm, nbest, beams, steps, page=16, together=False):
     given, count = given.to(device), torch.tensor([len(s) for s in said], device=device)
     state = Beams(lm, rows, beams, length + steps, page)
     last = torch.empty(rows, lm.vocab, dtype=torch.float32, device=device)
-    if together:
+    if together and length > 0:   # (lists may all be empty)
         flat = torch.tensor([t for s in said for t in s], device=device)
         logits = state.read(flat, count.int(), length)
         last = logits[(count.cumsum(0) - 1).clamp(min=0)]

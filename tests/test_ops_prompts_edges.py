@@ -1,7 +1,8 @@
 """The operators that bring prompts into the paged cache, at calls that the other tests do not make: the largest values, results in the place of what is
-read, strides of results, rows far apart, workspaces of short calls."""
+read, strides of results, rows far apart, workspaces of short calls, empty lists."""
 
-import math
+import os
+import sys
 
 import pytest
 import torch
@@ -9,6 +10,8 @@ import torch
 from test_ops_prompts import _close, _gen, _i32, _prompts_by, _prompts_case, _prompts_ref, _randn
 
 pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
 
 DTYPES = [torch.float32, torch.bfloat16, torch.float16]
 
@@ -163,3 +166,13 @@ def test_prompts_rows_far_apart(which, dtype):
         assert torch.equal(attend_prompts(q, kf, vf, starts, **kw), attend_prompts(q, k, v, starts, **kw))
         for force in (1, 2):
             assert torch.equal(_prompts_by(force, q, kf, vf, starts, **kw), _prompts_by(force, q, k, v, starts, **kw))
+
+
+@pytest.mark.parametrize("together", [False, True])
+def test_lists_that_are_all_empty(together):
+    """No hypothesis of any utterance: nothing is read and nothing found."""
+    from continue_nbest import Lm, continue_nbest
+    lm = Lm(40, width=64, layers=1, heads=4, kv_heads=2, dtype=torch.float32, seed=3)
+    assert continue_nbest(lm, [[], []], 4, 5, page=4, together=together) == ([[], []], 0)
+    got, _ = continue_nbest(lm, [[], [((3, 5), -1.0)], []], 4, 5, page=4, together=together)
+    assert got[0] == got[2] == [] and got[1]
