@@ -493,7 +493,7 @@ int tbs_rotary(const tbs_rotary_args *args, void *stream);
  * numbers give wrong rows, nothing worse.  Tokens of the cache beyond table_width * page and on pages outside [0, pages) do not exist; a negative past counts as 0.
  * out may be q itself (same strides) and lies over nothing else that is read, nor between a cache's first and last number.  dim is a multiple of 8 up to 256, heads a multiple of kv_heads, tokens * heads and
  * a table's tokens with the batch's below 2^31 and 2^30, a page's stride and `page` tokens' below 4 GiB.  Rows and heads on 16-byte boundaries, and keys and values of new tokens less than 32 MiB apart,
- * are faster.  The same call gives the same bits.
+ * are faster, and some thousand prompts a call at most: every workgroup goes through all of them.  The same call gives the same bits.
  * workspace: tbs_attend_prompts_workspace(args) bytes on a 16-byte boundary (0: none), free again when the work is done. */
 typedef struct tbs_attend_prompts_args {
     const void *q;                       /* [tokens, heads, dim]; elements of a head side by side everywhere */

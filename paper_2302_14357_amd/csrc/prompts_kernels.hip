@@ -9,15 +9,18 @@
 //  - scores: S^T = K Q^T, keys the rows, so that a lane has 16 of 32 keys' scores of one query, the other half's lane the others;
 //  - output: O^T = V^T P^T.  The order of the keys in the sum is free, so the weights go into the instruction as the scores' came out; V's fragments
 //    come from LDS by the reads that transpose 4 x 16 blocks, from the rows that this order names.
-// Keys and values of a tile go to LDS by direct loads, the next tile's while this one is worked on.  Pieces of 16 bytes of a row are permuted by bits
+// Keys and values of a tile go to LDS by direct loads, those of new tokens while the tile before is worked on.  Behind a cache that holds in part only: the number of a later tile's page is
+// looked up behind these loads and copied at once (look()), and what waits for it waits for them too.  Pieces of 16 bytes of a row are permuted by bits
 // of the row, so that a fragment's reads are all LDS banks once.
 //
-// Weights are rounded to the 16 bits of the values' type: a weight's relative error is half a step of it, as large as the output's own rounding; two
+// Weights are rounded to the 16 bits of the values' type: a weight's relative error is half a step of it, as large as the output's own rounding.  Where values are independent the two add up
+// to sqrt(2) times the one (measured against 64 bits: 1.17 to 1.41 times the error that float32 weights leave); a mean of like values hardly has the weights' part.  Two
 // numbers a weight would cost half as many matrix instructions again.  Sums, statistics and the weights' sum are float32.
 //
 // Bound by the matrix and the vector units together.  Prompts of 16000 and 7001 tokens, 32 heads on 8 of 128, bfloat16: 2.4 ms, 1.03 PFLOP/s (a large product of the library 1.45),
 // the matrix pipes 50 % busy, the vector units (32 exponentials, roundings and sums a lane of 64 keys) 44 %; two waves a SIMD overlap the two only in part.  16000 tokens, 32 heads
-// on 8 of 64: 1.2 ms, 0.87 PFLOP/s, half as many products for the same exponentials.  4000 in float32, 16 heads on 4 of 128: 600 us, 110 TFLOP/s of 153, the pipes' own order of work.
+// on 8 of 64: 1.2 ms, 0.87 PFLOP/s, half as many products for the same exponentials.  4000 in float32, 16 heads on 4 of 128: 600 us, 110 TFLOP/s of 153 (where
+// the rest goes is not known).
 // Four waves and 32 queries each: eight in two groups half a tile apart gained 2 %, eight behind one barrier 3 % of long prompts and lost 10 % of a batch's short ones; 64 queries
 // a wave spill; 32 keys a tile 7 % slower at 128; three tiles on their way 12 %; halves of a tile worked on in turn inside a wave 15 %.
 #include "op_device.h"
@@ -70,7 +73,8 @@ __device__ __forceinline__ PromptsAt prompts_at(const PromptsP &p, int i) {
 }
 
 // The tile `unit` of `rows` rows among all prompts' tiles, by every wave for itself: its prompt and its number in the prompt, a prompt's last first
-// (they have the most keys); prompt -1 for one behind all of them, and then the number of tiles.
+// (they have the most keys); prompt -1 for one behind all of them, and then the number of tiles.  Every workgroup adds all prompts up, so that the time grows as prompts times tiles: of prompts of
+// one token, 8 heads of 64, 512 take 42 us, 4096 970 and 16384 14600.
 __device__ __forceinline__ int2 prompts_find(const PromptsP &p, int unit, int rows) {
     const int lane = threadIdx.x & 63;
     auto tiles = [&](int i) { return (prompts_length(p, i) * p.group + rows - 1) / rows; };   // (below 2^31: tokens x heads is)
@@ -158,7 +162,7 @@ __device__ __forceinline__ void prompts_interleave() {
     __builtin_amdgcn_sched_group_barrier(0x008, A < N ? A : N, 0);
 }
 
-// What a workgroup does.  DP: dim rounded up to 32, 64, 80, 96, 128 or 256; SHARED: by the list of pieces (its few scalars more cost 7 % in
+// What a workgroup does.  DP: dim rounded up to 32, 64, 96, 128 or 256, or 80 itself; SHARED: by the list of pieces (its few scalars more cost 7 % in
 // the loop).  A class whose functions are all inlined: everything in it is in registers.
 #define PROMPTS_INLINE __device__ __forceinline__
 template <class T, int DP, bool SHARED>
@@ -624,7 +628,7 @@ struct PromptsWork {
 };
 
 template <class T, int DP, bool SHARED>
-__global__ void __launch_bounds__(64 * PROMPTS_WAVES, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 80 ? 3 : 2)   // (three at 80: 5 to 9 registers spill, and 16000 tokens take 771 us in place of 863)
+__global__ void __launch_bounds__(64 * PROMPTS_WAVES, DP > 128 || sizeof(T) == 4 ? 1 : DP <= 80 ? 3 : 2)   // (three at 80: 4 to 9 registers spill, and 16000 tokens take 771 us in place of 863; float32's shared form at 256 spills 36)
 k_prompts(PromptsP p) {
     __shared__ __align__(16) char s_kv[4 * PromptsTile<T, DP>::BYTES];
     PromptsWork<T, DP, SHARED> work(p, s_kv);
@@ -637,7 +641,8 @@ k_prompts(PromptsP p) {
 #define PROMPTS_LEAST 4       // steps of a piece at least, where a tile has more than one
 __device__ const int prompts_parts[PROMPTS_LENGTHS] = {16, 18, 20, 22, 25, 28, 32, 36, 40, 44, 50, 56, 64, 96, 128, 0};   // 64ths of a share; 0: whole tiles
 
-// workgroups of four waves that the chip runs at a time: one to three a CU, by their registers
+// workgroups of four waves that the chip runs at a time, one to three a CU, as the plan and the choice of the form count them.  (Registers allow four at 32 in 16 bits, three at 32 in float32 and
+// two of the shared form at 80 in float32, of which the measured rules know nothing.)
 static int prompts_slots(const tbs_attend_prompts_args &a) { return 256 * (a.dtype == TBS_F32 ? (a.dim <= 64 ? 2 : 1) : a.dim <= 64 || a.dim == 80 ? 3 : a.dim <= 128 ? 2 : 1); }
 
 // Whose keys are shared, one workgroup: a thread a tile, or prompt.  A piece is at most `len` steps long: of sixteen lengths, from a quarter of an equal share of all work up, the one that

@@ -78,7 +78,7 @@ __device__ __forceinline__ RotaryPieces rotary_pieces(const RotaryP &p, int lane
 // A workgroup takes `per` tokens: their angles once into LDS, then all their heads, `lanes` threads to a head, the next head's pieces on their way while
 // one is turned; of the values a copy.  HALF: a pair is i and i + pairs; otherwise 2 i and 2 i + 1.  WHOLE: all of a head turns, and every
 // lane has two whole pieces.
-// Bound by memory: 8000 tokens, heads of 32 + 8 + 8 x 128, bfloat16, with the cache 34 us, 6.2 TB/s of what the caches hold in part (36 without the next
+// Bound by memory: 8000 tokens, heads of 32 + 8 + 8 x 128, bfloat16, with the cache 42 to 45 us, 4.7 to 5.1 TB/s (on inputs that the caches hold in part 34; 36 without the next
 // head's loads ahead, 37 without WHOLE); 500 tokens of them 5.4 us.  A half of 256 turned, 16 + 4 + 4 heads, 4000 tokens, float16: 23 us (one piece a lane 31).
 template <class T, bool HALF, bool WHOLE>
 __global__ void __launch_bounds__(ROTARY_THREADS)
